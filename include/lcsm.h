@@ -44,6 +44,12 @@ extern "C" {
 #define LCSM_EDONE (-4)   /* all L positions have been emitted; nothing was queued */
 #define LCSM_ESTATE (-5)  /* call out of sequence, or the context is faulted (see lcsm_reset) */
 
+/* Element types of the operators that take more than fp32 (lcsm_ssm.h,
+ * lcsm_norm.h, lcsm_q4.h). */
+#define LCSM_F32 0
+#define LCSM_BF16 1
+#define LCSM_F16 2
+
 /* Tile kinds reported by lcsm_plan_tile. */
 #define LCSM_TILE_NONE 0    /* no gray tile after this step (t = L-1) */
 #define LCSM_TILE_DIRECT 1  /* direct Toeplitz kernel */

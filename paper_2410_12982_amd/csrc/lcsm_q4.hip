@@ -1,0 +1,478 @@
+// Matrix-vector products with 4-bit weights and group scales (lcsm_q4.h).
+//
+// The codes are kept as tiles of 16 outputs x 128 inputs, 16 bytes a lane: lane
+// l's word j holds the eight codes of output l % 16 for the inputs 32 j + 8 (l
+// / 16) ..+7, which is the lane's share of a 16x16x32 matrix product's right
+// operand.  The eight lie so that a rotation brings two of them under the
+// exponent of 16.0 in the two halves of the word: 16 + code is exact in bf16
+// and in fp16, and costs an and-or.  A product of x with ones gives the sum of
+// x, in the same lanes, for what has to come off again: 16 + zero.  fp32 rows
+// are taken apart into three bf16 values that hold all of their bits.
+#include <math.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <new>
+#include <type_traits>
+
+#include "lcsm_elem.h"
+#include "lcsm_q4.h"
+
+namespace lcsm {
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
+typedef f16_t v8h __attribute__((ext_vector_type(8)));
+
+constexpr int kTileN = 16, kTileK = 128;  // weights of a tile
+constexpr int kMaxWaves = 16;
+
+struct Q4Call {
+  int rows, N, K, group, ng, kb;  // kb: tiles along K
+  int scale_dtype;
+  const void *x, *codes, *scales;
+  const uint8_t* zeros;  // NULL: 8
+  const float* bias;     // NULL: none
+  void* y;
+  size_t x_stride, y_stride;
+};
+
+// ---- what multiplies: the element's matrix operand, and x as one or three of them
+
+template <class E>
+struct Mat {  // fp16
+  typedef v8h V;
+  static constexpr int PARTS = 1, ROT = 29;
+  static constexpr unsigned BASE = 0x4C004C00u, MASK = 0x03C003C0u;  // codes at bits 6 and 22
+  static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+struct MatBf {
+  typedef v8bf V;
+  static constexpr int PARTS = 1, ROT = 0;
+  static constexpr unsigned BASE = 0x41804180u, MASK = 0x00780078u;  // codes at bits 3 and 19
+  static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mat<bf16_t> : MatBf {};
+template <>
+struct Mat<float> : MatBf {
+  static constexpr int PARTS = 3;
+};
+
+template <class E>
+__device__ __forceinline__ typename Mat<E>::V weights(unsigned w) {
+  typedef Mat<E> T;
+  v4u r;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const unsigned k = __builtin_rotateright32(w, (4 * t + T::ROT) % 32);
+    r[t] = (k & T::MASK) | T::BASE;
+  }
+  return __builtin_bit_cast(typename T::V, r);
+}
+
+// Inputs k .. k+7 of a row, zeros past K and for rows that there are not.
+template <class E>
+__device__ __forceinline__ void load_x(const E* row, int k, int K, bool vec, bool live, E (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (E)0.f;
+  if (!live) return;
+  if (vec && k + 8 <= K) {
+    struct alignas(16) Pack {
+      E e[8];
+    };
+    const Pack p = *reinterpret_cast<const Pack*>(row + k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p.e[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < K) v[i] = row[k + i];
+  }
+}
+
+template <class E>
+__device__ __forceinline__ void operand(const E (&v)[8], typename Mat<E>::V (&a)[Mat<E>::PARTS]) {
+  if constexpr (std::is_same<E, float>::value) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bf16_t hi = (bf16_t)v[i];
+      const float r1 = v[i] - (float)hi;
+      const bf16_t mid = (bf16_t)r1;
+      a[0][i] = hi;
+      a[1][i] = mid;
+      a[2][i] = (bf16_t)(r1 - (float)mid);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[0][i] = v[i];
+  }
+}
+
+__device__ __forceinline__ float scale_at(const void* p, int dtype, size_t i) {
+  if (dtype == LCSM_BF16) return (float)static_cast<const bf16_t*>(p)[i];
+  if (dtype == LCSM_F16) return (float)static_cast<const f16_t*>(p)[i];
+  return static_cast<const float*>(p)[i];
+}
+
+// A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
+// every so many'th tile along K, their sums meet in LDS and are added in a
+// fixed order.  SPG: 32-input products a scale (4: a scale for the whole tile).
+template <class E, int SPG, int RT, int NT>
+__global__ __launch_bounds__(kMaxWaves * 64) void k_q4(Q4Call c, bool vec) {
+  typedef Mat<E> T;
+  extern __shared__ float part[];  // [waves][NT][RT][16 rows][16 outputs]
+  const int lane = (int)threadIdx.x & 63, wv = (int)threadIdx.x >> 6, nw = (int)blockDim.x >> 6;
+  const int q = lane >> 4, col = lane & 15;
+  const int nt0 = (int)blockIdx.x * NT, r0 = (int)blockIdx.y * 16 * RT;
+  const int nts = (c.N + kTileN - 1) / kTileN;
+  const unsigned one = std::is_same<E, f16_t>::value ? 0x3C003C00u : 0x3F803F80u;
+  const typename T::V ones = __builtin_bit_cast(typename T::V, (v4u){one, one, one, one});
+  v4f y[NT][RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) y[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
+  const v4f none = {0.f, 0.f, 0.f, 0.f};
+
+  for (int kb = wv; kb < c.kb; kb += nw) {
+    v4u w[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int nt = min(nt0 + t, nts - 1);
+      w[t] = static_cast<const v4u*>(c.codes)[((size_t)nt * c.kb + kb) * 64 + lane];
+    }
+    v4f acc[NT][RT], sum[RT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      typename T::V a[RT][T::PARTS];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int row = r0 + 16 * r + col;
+        E v[8];
+        load_x<E>(static_cast<const E*>(c.x) + (size_t)row * c.x_stride, kb * kTileK + 32 * j + 8 * q,
+                  c.K, vec, row < c.rows, v);
+        operand<E>(v, a[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (j % SPG == 0) sum[r] = none;
+#pragma unroll
+        for (int p = 0; p < T::PARTS; ++p) sum[r] = T::mul(a[r][p], ones, sum[r]);
+      }
+      const int g = SPG == 4 ? kb * kTileK / c.group : kb * (4 / SPG) + j / SPG;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const typename T::V b = weights<E>(w[t][j]);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          if (j % SPG == 0) acc[t][r] = none;
+#pragma unroll
+          for (int p = 0; p < T::PARTS; ++p) acc[t][r] = T::mul(a[r][p], b, acc[t][r]);
+        }
+        if (j % SPG == SPG - 1 && g < c.ng) {
+          const size_t at = ((size_t)min(nt0 + t, nts - 1) * c.ng + g) * kTileN + col;
+          const float s = scale_at(c.scales, c.scale_dtype, at);
+          const float z = c.zeros ? 16.f + (float)c.zeros[at] : 24.f;
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[t][r][e] = fmaf(s, fmaf(-z, sum[r][e], acc[t][r][e]), y[t][r][e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        part[(((wv * NT + t) * RT + r) * 16 + 4 * q + e) * 16 + col] = y[t][r][e];
+  __syncthreads();
+  constexpr int OUT = NT * RT * 256;
+  for (int o = (int)threadIdx.x; o < OUT; o += (int)blockDim.x) {
+    const int t = o / (RT * 256), r = o / 16 % (RT * 16), n = (nt0 + t) * kTileN + o % 16;
+    const int row = r0 + r;
+    if (n >= c.N || row >= c.rows) continue;
+    float v = c.bias ? c.bias[n] : 0.f;
+    for (int w = 0; w < nw; ++w) v += part[w * OUT + o];
+    static_cast<E*>(c.y)[(size_t)row * c.y_stride + n] = (E)v;
+  }
+}
+
+// The codes of one lane's 16 bytes: a thread per 32-bit word.
+__global__ __launch_bounds__(256) void k_q4_codes(const uint8_t* __restrict__ src, unsigned* __restrict__ dst,
+                                                  int M, int N, int K, int nts, int kb) {
+  const size_t n = (size_t)M * nts * kb * 256, step = (size_t)gridDim.x * 256;
+  const size_t bytes = ((size_t)K + 1) / 2;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+    const int j = (int)(i % 4), lane = (int)(i / 4 % 64);
+    const size_t tile = i / 256, tk = tile % kb, tn = tile / kb % nts, m = tile / kb / nts;
+    const size_t out = tn * kTileN + lane % 16, k0 = tk * kTileK + 32 * j + 8 * (lane / 16);
+    unsigned w = 0;
+    for (int e = 0; e < 8; ++e) {
+      const size_t k = k0 + e;
+      unsigned v = 0;
+      if (out < (size_t)N && k < (size_t)K) v = src[(m * N + out) * bytes + k / 2] >> (4 * (k & 1)) & 15u;
+      w |= v << (4 * (e / 2) + 16 * (e & 1));
+    }
+    dst[i] = w << 3 | w >> 29;
+  }
+}
+
+// [M][N][ng] values of SZ bytes as [M][tile][ng][16].
+template <class T>
+__global__ __launch_bounds__(256) void k_q4_groups(const T* __restrict__ src, T* __restrict__ dst, int M, int N,
+                                                   int ng, int nts, T mask) {
+  const size_t n = (size_t)M * nts * ng * 16, step = (size_t)gridDim.x * 256;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+    const size_t g = i / 16 % ng, tn = i / 16 / ng % nts, m = i / 16 / ng / nts, out = tn * 16 + i % 16;
+    dst[i] = out < (size_t)N ? (T)(src[(m * N + out) * ng + g] & mask) : (T)0;
+  }
+}
+
+// A wave per group of a row: the largest magnitude, then the codes of two
+// neighbouring weights a lane at a time.
+__global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w, int rows, int K, int group,
+                                                     int ng, int scale_dtype, uint8_t* __restrict__ codes,
+                                                     void* __restrict__ scales) {
+  const int lane = (int)threadIdx.x & 63;
+  const size_t i = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (i >= (size_t)rows * ng) return;
+  const size_t row = i / ng;
+  const int k0 = (int)(i % ng) * group, k1 = min(k0 + group, K);
+  const float* p = w + row * K;
+  float most = 0.f;
+  for (int k = k0 + lane; k < k1; k += 64) most = fmaxf(most, fabsf(p[k]));
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+  float s = __fdiv_rn(most, 7.f);
+  if (scale_dtype == LCSM_BF16) s = (float)(bf16_t)s;
+  if (scale_dtype == LCSM_F16) s = (float)(f16_t)s;
+  if (lane == 0) {
+    if (scale_dtype == LCSM_BF16) static_cast<bf16_t*>(scales)[i] = (bf16_t)s;
+    if (scale_dtype == LCSM_F16) static_cast<f16_t*>(scales)[i] = (f16_t)s;
+    if (scale_dtype == LCSM_F32) static_cast<float*>(scales)[i] = s;
+  }
+  auto code = [&](int k) -> unsigned {
+    if (k >= k1 || s == 0.f) return 8u;
+    return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(p[k], s)) + 8.f, 0.f), 15.f);
+  };
+  const size_t bytes = ((size_t)K + 1) / 2;
+  for (int k = k0 + 2 * lane; k < k1; k += 128)  // groups begin at even k
+    codes[row * bytes + k / 2] = (uint8_t)(code(k) | code(k + 1) << 4);
+}
+
+template <class E, int SPG, int RT, int NT>
+hipError_t launch(const Q4Call& c, hipStream_t st) {
+  const bool vec = ((uintptr_t)c.x & 15) == 0 && c.x_stride * sizeof(E) % 16 == 0;
+  const int waves = c.kb < 8 ? c.kb : 8;
+  const dim3 grid((unsigned)(((c.N + 15) / 16 + NT - 1) / NT), (unsigned)((c.rows + 16 * RT - 1) / (16 * RT)));
+  hipLaunchKernelGGL((k_q4<E, SPG, RT, NT>), grid, dim3(64 * waves), (size_t)waves * NT * RT * 1024, st, c, vec);
+  return hipGetLastError();
+}
+
+template <class E, int SPG>
+hipError_t launch_rows(const Q4Call& c, hipStream_t st) {
+  if (c.rows <= 16) return launch<E, SPG, 1, 1>(c, st);
+  if (c.rows <= 32) return launch<E, SPG, 2, 1>(c, st);
+  return launch<E, SPG, 4, 1>(c, st);
+}
+
+template <class E>
+hipError_t launch_q4(const Q4Call& c, hipStream_t st) {
+  if (c.group == 32) return launch_rows<E, 1>(c, st);
+  if (c.group == 64) return launch_rows<E, 2>(c, st);
+  return launch_rows<E, 4>(c, st);
+}
+
+unsigned blocks(size_t n) {
+  const size_t b = (n + 255) / 256;
+  return (unsigned)(b < 16384 ? b : 16384);
+}
+
+}  // namespace
+}  // namespace lcsm
+
+struct lcsm_q4 {
+  lcsm_q4_shape s;
+  int nts, kb, ng;
+  hipStream_t stream;
+  char* mem;
+  void* owned;
+  char *codes, *scales;
+  uint8_t* zeros;
+  float* bias;
+  bool faulted;
+  char msg[256];
+};
+
+namespace {
+
+struct Plan {
+  int nts, kb, ng;
+  size_t codes, scales, zeros, bias, total;
+};
+
+bool group_ok(int g) { return g == 32 || g == 64 || (g > 0 && g % 128 == 0); }
+
+bool q4_plan(const lcsm_q4_shape* s, Plan* p) {
+  if (!s || s->M < 1 || s->M > 16384 || s->N < 1 || s->K < 1 || s->N > (1 << 24) || s->K > (1 << 24) ||
+      !group_ok(s->group) || !lcsm::dtype_ok(s->scale_dtype))
+    return false;
+  for (int r : s->reserved)
+    if (r) return false;
+  if ((double)s->N * s->K > 1099511627776.0) return false;
+  p->nts = (s->N + 15) / 16;
+  p->kb = (s->K + 127) / 128;
+  p->ng = (int)(((long long)s->K + s->group - 1) / s->group);
+  const size_t M = (size_t)s->M, groups = M * p->nts * p->ng * 16;
+  size_t at = 0;
+  auto take = [&](size_t* where, size_t bytes) {
+    *where = at;
+    at = (at + bytes + 255) / 256 * 256;
+  };
+  take(&p->codes, M * p->nts * p->kb * 1024);
+  take(&p->scales, groups * lcsm::dtype_size(s->scale_dtype));
+  take(&p->zeros, groups);
+  take(&p->bias, M * s->N * sizeof(float));
+  p->total = at;
+  return true;
+}
+
+int q4_fail(lcsm_q4* c, int code, const char* what, hipError_t e = hipSuccess) {
+  if (e != hipSuccess) {
+    snprintf(c->msg, sizeof(c->msg), "%s: %s", what, hipGetErrorString(e));
+    c->faulted = true;
+    return LCSM_EDEVICE;
+  }
+  snprintf(c->msg, sizeof(c->msg), "%s", what);
+  return code;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lcsm_q4_workspace_bytes(const lcsm_q4_shape* shape, size_t* bytes) {
+  Plan p;
+  if (!bytes || !q4_plan(shape, &p)) return LCSM_EINVAL;
+  *bytes = p.total;
+  return LCSM_OK;
+}
+
+int lcsm_q4_init(lcsm_q4** out, const lcsm_q4_shape* shape, const void* codes, const void* scales,
+                 const void* zeros, const float* bias, void* stream, void* workspace,
+                 size_t workspace_bytes) {
+  if (!out) return LCSM_EINVAL;
+  *out = nullptr;
+  Plan p;
+  if (!codes || !scales || !q4_plan(shape, &p)) return LCSM_EINVAL;
+  if (workspace && ((uintptr_t)workspace & 255)) return LCSM_EINVAL;
+  if (workspace && workspace_bytes < p.total) return LCSM_ENOMEM;
+  lcsm_q4* c = new (std::nothrow) lcsm_q4();
+  if (!c) return LCSM_ENOMEM;
+  c->s = *shape;
+  c->nts = p.nts;
+  c->kb = p.kb;
+  c->ng = p.ng;
+  c->stream = (hipStream_t)stream;
+  if (workspace) {
+    c->mem = (char*)workspace;
+  } else {
+    if (hipMalloc(&c->owned, p.total) != hipSuccess) {
+      (void)hipGetLastError();
+      delete c;
+      return LCSM_ENOMEM;
+    }
+    c->mem = (char*)c->owned;
+  }
+  c->codes = c->mem + p.codes;
+  c->scales = c->mem + p.scales;
+  c->zeros = zeros ? (uint8_t*)(c->mem + p.zeros) : nullptr;
+  c->bias = bias ? (float*)(c->mem + p.bias) : nullptr;
+  const int M = shape->M, N = shape->N;
+  const size_t words = (size_t)M * p.nts * p.kb * 256, groups = (size_t)M * p.nts * p.ng * 16;
+  hipLaunchKernelGGL(lcsm::k_q4_codes, dim3(lcsm::blocks(words)), dim3(256), 0, c->stream,
+                     (const uint8_t*)codes, (unsigned*)c->codes, M, N, shape->K, p.nts, p.kb);
+  if (shape->scale_dtype == LCSM_F32)
+    hipLaunchKernelGGL(lcsm::k_q4_groups<uint32_t>, dim3(lcsm::blocks(groups)), dim3(256), 0, c->stream,
+                       (const uint32_t*)scales, (uint32_t*)c->scales, M, N, p.ng, p.nts, 0xffffffffu);
+  else
+    hipLaunchKernelGGL(lcsm::k_q4_groups<uint16_t>, dim3(lcsm::blocks(groups)), dim3(256), 0, c->stream,
+                       (const uint16_t*)scales, (uint16_t*)c->scales, M, N, p.ng, p.nts, (uint16_t)0xffff);
+  if (zeros)
+    hipLaunchKernelGGL(lcsm::k_q4_groups<uint8_t>, dim3(lcsm::blocks(groups)), dim3(256), 0, c->stream,
+                       (const uint8_t*)zeros, c->zeros, M, N, p.ng, p.nts, (uint8_t)15);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && bias)
+    e = hipMemcpyAsync(c->bias, bias, (size_t)M * N * sizeof(float), hipMemcpyDeviceToDevice, c->stream);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    (void)hipStreamSynchronize(c->stream);
+    if (c->owned) (void)hipFree(c->owned);
+    delete c;
+    return LCSM_EDEVICE;
+  }
+  *out = c;
+  return LCSM_OK;
+}
+
+int lcsm_q4_matvec(lcsm_q4* ctx, int layer, int rows, int dtype, const void* x, size_t x_stride,
+                   void* y, size_t y_stride) {
+  if (!ctx) return LCSM_EINVAL;
+  const lcsm_q4_shape& s = ctx->s;
+  if (layer < 0 || layer >= s.M) return q4_fail(ctx, LCSM_EINVAL, "layer out of range");
+  if (rows < 0 || !lcsm::dtype_ok(dtype)) return q4_fail(ctx, LCSM_EINVAL, "rows below zero or unknown type");
+  if (rows > 0) {
+    if (!x || !y) return q4_fail(ctx, LCSM_EINVAL, "null input or output pointer");
+    if (x_stride < (size_t)s.K || y_stride < (size_t)s.N)
+      return q4_fail(ctx, LCSM_EINVAL, "a row stride is shorter than the row");
+    if (rows > 65535 * 64) return q4_fail(ctx, LCSM_EINVAL, "too many rows");
+  }
+  if (ctx->faulted) return LCSM_ESTATE;
+  if (!rows) return LCSM_OK;
+  const size_t m = (size_t)layer, groups = (size_t)ctx->nts * ctx->ng * 16;
+  const lcsm::Q4Call c{rows, s.N, s.K, s.group, ctx->ng, ctx->kb, s.scale_dtype, x,
+                       ctx->codes + m * ctx->nts * ctx->kb * 1024,
+                       ctx->scales + m * groups * lcsm::dtype_size(s.scale_dtype),
+                       ctx->zeros ? ctx->zeros + m * groups : nullptr,
+                       ctx->bias ? ctx->bias + m * s.N : nullptr, y, x_stride, y_stride};
+  const hipError_t e = lcsm::with_dtype(dtype, [&](auto v) { return lcsm::launch_q4<decltype(v)>(c, ctx->stream); });
+  return e == hipSuccess ? LCSM_OK : q4_fail(ctx, LCSM_EDEVICE, "product launch", e);
+}
+
+int lcsm_q4_quantize(const float* w, int rows, int K, int group, int scale_dtype, void* codes,
+                     void* scales, void* stream) {
+  if (rows < 0 || K < 1 || K > (1 << 24) || !group_ok(group) || !lcsm::dtype_ok(scale_dtype)) return LCSM_EINVAL;
+  if (!rows) return LCSM_OK;
+  if (!w || !codes || !scales) return LCSM_EINVAL;
+  const int ng = (int)(((long long)K + group - 1) / group);
+  const size_t b = ((size_t)rows * ng + 3) / 4;
+  if (b > 0x7fffffffu) return LCSM_EINVAL;
+  hipLaunchKernelGGL(lcsm::k_q4_quantize, dim3((unsigned)b), dim3(256), 0, (hipStream_t)stream, w, rows, K, group,
+                     ng, scale_dtype, (uint8_t*)codes, scales);
+  return hipGetLastError() == hipSuccess ? LCSM_OK : LCSM_EDEVICE;
+}
+
+int lcsm_q4_reset(lcsm_q4* ctx) {
+  if (!ctx) return LCSM_EINVAL;
+  ctx->faulted = false;
+  ctx->msg[0] = 0;
+  return LCSM_OK;
+}
+
+void lcsm_q4_destroy(lcsm_q4* ctx) {
+  if (!ctx) return;
+  (void)hipStreamSynchronize(ctx->stream);
+  if (ctx->owned) (void)hipFree(ctx->owned);
+  delete ctx;
+}
+
+const char* lcsm_q4_last_error(const lcsm_q4* ctx) { return ctx ? ctx->msg : ""; }
+
+}  // extern "C"

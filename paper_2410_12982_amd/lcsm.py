@@ -1,4 +1,5 @@
-"""Python binding of the C ABI in ``include/lcsm.h``, ``lcsm_base.h``, ``lcsm_dd.h`` and ``lcsm_synth.h`` (ctypes).
+"""Python binding of the C ABI in ``include/lcsm.h``, ``lcsm_base.h``, ``lcsm_dd.h``, ``lcsm_synth.h``, ``lcsm_ssm.h``,
+``lcsm_norm.h`` and ``lcsm_q4.h`` (ctypes).
 
 Argument marshalling only: every step of the computation runs in the HIP
 kernels of ``liblcsm.so``.  PyTorch supplies device memory (the workspace and
@@ -64,6 +65,36 @@ class Options(ctypes.Structure):
                 ("reserved", ctypes.c_int * 2)]
 
 
+class SsmShape(ctypes.Structure):
+    """``lcsm_ssm_shape``."""
+    _fields_ = [(k, ctypes.c_int) for k in ("M", "slots", "H", "P", "N", "G", "W", "dtype", "max_tokens")] + [
+        ("reserved", ctypes.c_int * 3)]
+
+
+class SsmIo(ctypes.Structure):
+    """``lcsm_ssm_io``."""
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("xbc", "dt", "z", "y")]
+                + [(k, ctypes.c_size_t) for k in ("xbc_stride", "dt_stride", "z_stride", "y_stride")]
+                + [(k, ctypes.c_void_p) for k in ("src", "dst")])
+
+
+class NormShape(ctypes.Structure):
+    """``lcsm_norm_shape``."""
+    _fields_ = ([(k, ctypes.c_int) for k in ("M", "D", "post", "pre", "act", "groups", "dtype", "res_dtype")]
+                + [("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("reserved", ctypes.c_int * 2)])
+
+
+class NormIo(ctypes.Structure):
+    """``lcsm_norm_io``."""
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("o", "g", "r", "r_out", "n")]
+                + [(k, ctypes.c_size_t) for k in ("o_stride", "g_stride", "r_stride", "r_out_stride", "n_stride")])
+
+
+class Q4Shape(ctypes.Structure):
+    """``lcsm_q4_shape``."""
+    _fields_ = [(k, ctypes.c_int) for k in ("M", "N", "K", "group", "scale_dtype")] + [("reserved", ctypes.c_int * 3)]
+
+
 _c_int_p = ctypes.POINTER(ctypes.c_int)
 _vp = ctypes.c_void_p
 
@@ -124,6 +155,34 @@ _SIGS = {
     "lcsm_synth_position": (ctypes.c_int, [_vp, _c_int_p]),
     "lcsm_synth_destroy": (None, [_vp]),
     "lcsm_synth_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_ssm.h
+    "lcsm_ssm_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(SsmShape), ctypes.POINTER(ctypes.c_size_t)]),
+    "lcsm_ssm_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(SsmShape)] + [_vp] * 7
+                      + [ctypes.c_size_t]),
+    "lcsm_ssm_step_layer": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.POINTER(SsmIo)]),
+    "lcsm_ssm_prompt_layer": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp,
+                                             ctypes.POINTER(SsmIo)]),
+    "lcsm_ssm_state": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.POINTER(_vp)]),
+    "lcsm_ssm_window": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.POINTER(_vp)]),
+    "lcsm_ssm_reset": (ctypes.c_int, [_vp]),
+    "lcsm_ssm_destroy": (None, [_vp]),
+    "lcsm_ssm_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_norm.h
+    "lcsm_norm_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(NormShape)] + [_vp] * 6),
+    "lcsm_norm_block": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.POINTER(NormIo)]),
+    "lcsm_norm_reset": (ctypes.c_int, [_vp]),
+    "lcsm_norm_destroy": (None, [_vp]),
+    "lcsm_norm_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_q4.h
+    "lcsm_q4_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(Q4Shape), ctypes.POINTER(ctypes.c_size_t)]),
+    "lcsm_q4_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(Q4Shape)] + [_vp] * 6
+                     + [ctypes.c_size_t]),
+    "lcsm_q4_matvec": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, ctypes.c_size_t,
+                                      _vp, ctypes.c_size_t]),
+    "lcsm_q4_quantize": (ctypes.c_int, [_vp] + [ctypes.c_int] * 4 + [_vp] * 3),
+    "lcsm_q4_reset": (ctypes.c_int, [_vp]),
+    "lcsm_q4_destroy": (None, [_vp]),
+    "lcsm_q4_last_error": (ctypes.c_char_p, [_vp]),
 }
 
 for _name, (_res, _args) in _SIGS.items():
@@ -694,3 +753,306 @@ class Synth:
             self.close()
         except Exception:
             pass
+
+
+# ---- the gated state space layer: element types beyond fp32
+
+F32, BF16, F16 = 0, 1, 2
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTS = {"none": 0, "silu": 1, "sigmoid": 2}
+
+
+def _dtype_code(dtype):
+    if dtype not in DTYPES:
+        raise ValueError(f"{dtype} is not one of float32, bfloat16, float16")
+    return DTYPES[dtype]
+
+
+def _weight(tensor, shape, name, device, dtype=_F32):
+    """A parameter as a contiguous tensor (None stays None)."""
+    if tensor is None:
+        return None
+    if not (tensor.dtype is dtype and tuple(tensor.shape) == shape and tensor.device == device):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {shape} on {device}")
+    return tensor.contiguous()
+
+
+def _handed_over(stream, device, tensors):
+    """Tensors whose copies are queued on ``stream``: where that is not torch's
+    current stream their memory must not be used anew before it has passed."""
+    if torch.cuda.current_stream(device).cuda_stream != stream.cuda_stream:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _cuda_device(device):
+    """A CUDA device with its index, so that it equals the tensors' devices."""
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("a CUDA device is needed")
+    return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+
+
+class _LayerContext:
+    """What the contexts of the gated layer's operators share: the order of
+    streams, the checks of rows, errors and release."""
+    _kind = ""
+
+    def _open(self, device, stream):
+        self.device = device
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self._order = _Order(self.stream, device)
+        self._ctx = _vp()
+        self._last_error = getattr(_lib, f"lcsm_{self._kind}_last_error")
+        self._destroy = getattr(_lib, f"lcsm_{self._kind}_destroy")
+        self._reset = getattr(_lib, f"lcsm_{self._kind}_reset")
+
+    def _check(self, r, where):
+        if r:
+            raise LcsmError(r, where, self._last_error(self._ctx).decode() if self._ctx else "")
+
+    def _rows(self, tensor, rows, width, dtype, name):
+        """(address, stride between rows) of a tensor [rows, width] whose rows are contiguous."""
+        if tensor.dtype is dtype and tensor.shape == (rows, width) and tensor.device == self.device:
+            a, b = tensor.stride()
+            if b == 1 or width == 1 or rows == 0:
+                return tensor.data_ptr(), a if rows > 1 else width
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {(rows, width)} on {self.device} "
+                         "with contiguous rows")
+
+    def reset(self):
+        self._order()
+        self._check(self._reset(self._ctx), f"lcsm_{self._kind}_reset")
+
+    def close(self):
+        if getattr(self, "_ctx", None):
+            self._destroy(self._ctx)
+            self._ctx = _vp()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Ssm(_LayerContext):
+    """Selective state space mixers of M layers with their short convolutions
+    (``include/lcsm_ssm.h``), for prompts and for single tokens.
+
+    ``conv_w`` [M, C, W] and ``A`` [M, H], fp32 CUDA tensors, are needed;
+    ``conv_bias`` [M, C], ``skip`` and ``dt_bias`` [M, H] are zero where not
+    given.  C = H P + 2 groups states.  ``slots`` sequences' states are held
+    (``state(layer)`` [slots, H, P, states] fp32, ``window(layer)`` [slots,
+    W - 1, C]).  ``max_tokens``: tokens of the largest prompt call.
+    """
+    _kind = "ssm"
+
+    def __init__(self, conv_w, A, slots, groups, states, conv_bias=None, skip=None, dt_bias=None,
+                 dtype=torch.bfloat16, max_tokens=0, stream=None):
+        if not (conv_w.is_cuda and conv_w.dim() == 3 and A.dim() == 2):
+            raise ValueError("conv_w must be a CUDA tensor [M, C, W] and A one [M, H]")
+        (M, C, W), H = (int(v) for v in conv_w.shape), int(A.shape[1])
+        G, N = int(groups), int(states)
+        if H < 1 or (C - 2 * G * N) < H or (C - 2 * G * N) % H:
+            raise ValueError("conv_w's channels are not H * P + 2 * groups * states")
+        P = (C - 2 * G * N) // H
+        self.M, self.C, self.W, self.H, self.P, self.N, self.G = M, C, W, H, P, N, G
+        self.D, self.slots, self.dtype, self.max_tokens = H * P, int(slots), dtype, int(max_tokens)
+        self._shape = SsmShape(M, self.slots, H, P, N, G, W, _dtype_code(dtype), self.max_tokens)
+        dev = conv_w.device
+        params = [_weight(t, s, n, dev) for t, s, n in
+                  ((conv_w, (M, C, W), "conv_w"), (conv_bias, (M, C), "conv_bias"), (A, (M, H), "A"),
+                   (skip, (M, H), "skip"), (dt_bias, (M, H), "dt_bias"))]
+        nbytes = ctypes.c_size_t(0)
+        r = _lib.lcsm_ssm_workspace_bytes(ctypes.byref(self._shape), ctypes.byref(nbytes))
+        if r:
+            raise LcsmError(r, "lcsm_ssm_workspace_bytes")
+        self._open(dev, stream)
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)
+        self._order()
+        r = _lib.lcsm_ssm_init(ctypes.byref(self._ctx), ctypes.byref(self._shape),
+                               *(t.data_ptr() if t is not None else None for t in params),
+                               self.stream.cuda_stream, self.workspace.data_ptr(), nbytes.value)
+        if r:
+            raise LcsmError(r, "lcsm_ssm_init")
+        _handed_over(self.stream, dev, params)
+        self._io = SsmIo()
+        self._io_ref = ctypes.byref(self._io)
+        self._states = [self._view("lcsm_ssm_state", m, torch.float32, (self.slots, H, P, N)) for m in range(M)]
+        self._windows = [self._view("lcsm_ssm_window", m, dtype, (self.slots, W - 1, C)) for m in range(M)]
+
+    def _view(self, where, layer, dtype, shape):
+        p = _vp()
+        self._check(getattr(_lib, where)(self._ctx, layer, ctypes.byref(p)), where)
+        off, n = p.value - self.workspace.data_ptr(), dtype.itemsize
+        for v in shape:
+            n *= v
+        return self.workspace[off:off + n].view(dtype).view(shape)
+
+    def _slots(self, t, n, name):
+        if t is None:
+            return None
+        if t.dtype is torch.int32 and t.shape == (n,) and t.device == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
+
+    def _fill(self, rows, n, xbc, dt, z, y, src, dst):
+        io, dtype = self._io, self.dtype
+        if y is None:
+            y = torch.empty((rows, self.D), dtype=dtype, device=self.device)
+        io.xbc, io.xbc_stride = self._rows(xbc, rows, self.C, dtype, "xbc")
+        io.dt, io.dt_stride = self._rows(dt, rows, self.H, dtype, "dt")
+        io.z, io.z_stride = (None, 0) if z is None else self._rows(z, rows, self.D, dtype, "z")
+        io.y, io.y_stride = self._rows(y, rows, self.D, dtype, "y")
+        io.src, io.dst = self._slots(src, n, "src"), self._slots(dst, n, "dst")
+        self._order()
+        return y
+
+    def step(self, layer, xbc, dt, z=None, y=None, src=None, dst=None):
+        """One token of each of n sequences: xbc [n, C], dt [n, H], z and y [n, D].  ``src``, ``dst``: int32 [n], the
+        slots that states are read from (-1: zero) and written to (-1: not kept); None: slot i for sequence i."""
+        n = xbc.shape[0]
+        y = self._fill(n, n, xbc, dt, z, y, src, dst)
+        r = _lib.lcsm_ssm_step_layer(self._ctx, layer, n, self._io_ref)
+        if r:
+            self._check(r, "lcsm_ssm_step_layer")
+        return y
+
+    def prompt(self, layer, xbc, dt, z=None, y=None, offsets=None, src=None, dst=None):
+        """The tokens of n sequences one after another, xbc [T, C] and so on: sequence i is rows offsets[i] ..
+        offsets[i+1] (int32 [n + 1]; None: one sequence of all rows)."""
+        T, n = xbc.shape[0], 1
+        if offsets is not None:
+            n = offsets.shape[0] - 1
+            offsets = self._slots(offsets, n + 1, "offsets")
+        y = self._fill(T, n, xbc, dt, z, y, src, dst)
+        r = _lib.lcsm_ssm_prompt_layer(self._ctx, layer, T, n, offsets, self._io_ref)
+        if r:
+            self._check(r, "lcsm_ssm_prompt_layer")
+        return y
+
+    def state(self, layer):
+        """The states of a layer, a view [slots, H, P, N] of the workspace."""
+        return self._states[layer]
+
+    def window(self, layer):
+        """The last W - 1 tokens' channels of a layer, a view [slots, W - 1, C] of the workspace, oldest first."""
+        return self._windows[layer]
+
+
+class Norm(_LayerContext):
+    """The norms after a block and before the next one, fused with the block's gate, its residual scale and the sum
+    (``include/lcsm_norm.h``).  ``post``, ``pre``: "none", "rms" or "layer"; ``act``: "none", "silu" or "sigmoid".
+    Weights are fp32 CUDA tensors [M, D] or None (ones or zeros); M layers if any is given, else ``layers``."""
+    _kind = "norm"
+
+    def __init__(self, D, post="rms", pre="rms", act="none", groups=1, alpha=1.0, eps=1e-5, post_weight=None,
+                 post_bias=None, scale=None, pre_weight=None, pre_bias=None, dtype=torch.bfloat16, res_dtype=None,
+                 layers=1, device="cuda:0", stream=None):
+        given = [t for t in (post_weight, post_bias, scale, pre_weight, pre_bias) if t is not None]
+        dev = _cuda_device(given[0].device if given else device)
+        self.M, self.D = int(given[0].shape[0] if given else layers), int(D)
+        self.dtype, self.res_dtype = dtype, dtype if res_dtype is None else res_dtype
+        self.act = act
+        ws = [_weight(t, (self.M, self.D), n, dev) for t, n in
+              ((post_weight, "post_weight"), (post_bias, "post_bias"), (scale, "scale"), (pre_weight, "pre_weight"),
+               (pre_bias, "pre_bias"))]
+        shape = NormShape(self.M, self.D, NORMS[post], NORMS[pre], ACTS[act], int(groups), _dtype_code(dtype),
+                          _dtype_code(self.res_dtype), float(alpha), float(eps))
+        self._open(dev, stream)
+        self._order()
+        r = _lib.lcsm_norm_init(ctypes.byref(self._ctx), ctypes.byref(shape),
+                                *(t.data_ptr() if t is not None else None for t in ws), self.stream.cuda_stream)
+        if r:
+            raise LcsmError(r, "lcsm_norm_init")
+        _handed_over(self.stream, dev, ws)
+        self._io = NormIo()
+        self._io_ref = ctypes.byref(self._io)
+
+    def block(self, layer, o, res, gate=None, res_out=None, out=None):
+        """(r', n) of the rows o (None: no block before), res and gate, all [rows, D].  ``res_out`` and ``out`` receive
+        them where given; False: that one is not wanted (None is returned for it)."""
+        rows, D, io = res.shape[0], self.D, self._io
+        if res_out is None:
+            res_out = torch.empty((rows, D), dtype=self.res_dtype, device=self.device)
+        if out is None:
+            out = torch.empty((rows, D), dtype=self.dtype, device=self.device)
+        io.r, io.r_stride = self._rows(res, rows, D, self.res_dtype, "res")
+        io.o, io.o_stride = (None, 0) if o is None else self._rows(o, rows, D, self.dtype, "o")
+        io.g, io.g_stride = (None, 0) if gate is None else self._rows(gate, rows, D, self.dtype, "gate")
+        io.r_out, io.r_out_stride = ((None, 0) if res_out is False
+                                     else self._rows(res_out, rows, D, self.res_dtype, "res_out"))
+        io.n, io.n_stride = (None, 0) if out is False else self._rows(out, rows, D, self.dtype, "out")
+        self._order()
+        r = _lib.lcsm_norm_block(self._ctx, layer, rows, self._io_ref)
+        if r:
+            self._check(r, "lcsm_norm_block")
+        return (None if res_out is False else res_out), (None if out is False else out)
+
+
+class Q4(_LayerContext):
+    """Matrices of 4-bit weights with group scales (``include/lcsm_q4.h``): ``codes`` uint8 [M, N, ceil(K/2)], ``scales``
+    [M, N, ceil(K/group)], ``zeros`` uint8 of the same shape or None, ``bias`` fp32 [M, N] or None.  They are laid out
+    anew and need not be kept."""
+    _kind = "q4"
+
+    def __init__(self, codes, scales, K, group, zeros=None, bias=None, stream=None):
+        if not (codes.is_cuda and codes.dim() == 3 and scales.dim() == 3):
+            raise ValueError("codes must be a CUDA tensor [M, N, ceil(K/2)] and scales one [M, N, ceil(K/group)]")
+        self.M, self.N, self.K, self.group = int(codes.shape[0]), int(codes.shape[1]), int(K), int(group)
+        M, N, dev = self.M, self.N, codes.device
+        if self.K < 1 or self.group < 1:
+            raise ValueError("K and group must be positive")
+        shape = Q4Shape(M, N, self.K, self.group, _dtype_code(scales.dtype))
+        per = (M, N, -(-self.K // self.group))
+        params = [_weight(codes, (M, N, (self.K + 1) // 2), "codes", dev, torch.uint8),
+                  _weight(scales, per, "scales", dev, scales.dtype), _weight(zeros, per, "zeros", dev, torch.uint8),
+                  _weight(bias, (M, N), "bias", dev)]
+        nbytes = ctypes.c_size_t(0)
+        r = _lib.lcsm_q4_workspace_bytes(ctypes.byref(shape), ctypes.byref(nbytes))
+        if r:
+            raise LcsmError(r, "lcsm_q4_workspace_bytes")
+        self._open(dev, stream)
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)
+        self._order()
+        r = _lib.lcsm_q4_init(ctypes.byref(self._ctx), ctypes.byref(shape),
+                              *(t.data_ptr() if t is not None else None for t in params),
+                              self.stream.cuda_stream, self.workspace.data_ptr(), nbytes.value)
+        if r:
+            raise LcsmError(r, "lcsm_q4_init")
+        _handed_over(self.stream, dev, params)
+
+    def matvec(self, layer, x, y=None):
+        """y [rows, N] = x [rows, K] times the layer's matrix, in x's type."""
+        rows, dtype = x.shape[0], x.dtype
+        if y is None:
+            y = torch.empty((rows, self.N), dtype=dtype, device=self.device)
+        px, sx = self._rows(x, rows, self.K, dtype, "x")
+        py, sy = self._rows(y, rows, self.N, dtype, "y")
+        self._order()
+        r = _lib.lcsm_q4_matvec(self._ctx, layer, rows, _dtype_code(dtype), px, sx, py, sy)
+        if r:
+            self._check(r, "lcsm_q4_matvec")
+        return y
+
+    @staticmethod
+    def quantize(w, group, scale_dtype=torch.bfloat16):
+        """(codes, scales) of fp32 weights [..., N, K] (lcsm_q4_quantize), on torch's current stream."""
+        if not (w.is_cuda and w.dtype is _F32 and w.dim() >= 2):
+            raise ValueError("w must be a CUDA fp32 tensor [..., N, K]")
+        group = int(group)
+        if group < 1:
+            raise ValueError("group must be positive")
+        w = w.contiguous()
+        K, lead = int(w.shape[-1]), tuple(w.shape[:-1])
+        codes = torch.empty(lead + ((K + 1) // 2,), dtype=torch.uint8, device=w.device)
+        scales = torch.empty(lead + (-(-K // group),), dtype=scale_dtype, device=w.device)
+        rows = w.numel() // K if K else 0
+        r = _lib.lcsm_q4_quantize(w.data_ptr(), rows, K, group, _dtype_code(scale_dtype), codes.data_ptr(),
+                                  scales.data_ptr(), torch.cuda.current_stream(w.device).cuda_stream)
+        if r:
+            raise LcsmError(r, "lcsm_q4_quantize")
+        return codes, scales
