@@ -151,6 +151,48 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
   return hipGetLastError();
 }
 
+// How a prompt call is cut: segments of `per` chunks so that about
+// kSsmWorkgroups workgroups of the widest kind are on their way; sequences that
+// are that many by themselves are not cut.
+constexpr int kSsmWorkgroups = 512;
+
+int head_groups(int H, int G, int P) {
+  const int items = H / G * ((P + 31) / 32), nw = items < kSsmWaves ? items : kSsmWaves;
+  return G * ((items + nw - 1) / nw);
+}
+// Upper bound of the segments of a call that is cut: fewer than `want` pieces
+// of all chunks and one more for each of fewer than `want` sequences; `cuts`:
+// chunks and sequences of the largest call.
+size_t most_segments(int H, int G, int P, size_t cuts) {
+  const size_t most = 2 * (size_t)kSsmWorkgroups / head_groups(H, G, P) + 2;
+  return most < cuts ? most : cuts;
+}
+
+hipError_t launch_prompt(const SsmCall& c, int dtype, char* bc, float* states, float* decay, hipStream_t st) {
+  SsmScratch w{};
+  w.bc = bc;
+  w.states = states;
+  w.decay = decay;
+  w.blocks = c.T / kSsmQ + c.n;  // a sequence's last chunk may be short
+  const int wgs = head_groups(c.H, c.G, c.P), want = kSsmWorkgroups / wgs;
+  w.per = want > c.n ? (w.blocks + want - 1) / want : w.blocks;
+  w.segments = want > c.n ? w.blocks / w.per + c.n : c.n;
+  const size_t e = dtype_size(dtype);
+  auto two = [&](const void* p, size_t stride) { return !p || ((uintptr_t)p % (2 * e) == 0 && stride % 2 == 0); };
+  w.pair = c.P % 2 == 0 && two(c.xbc, c.xbc_stride) && two(c.z, c.z_stride) && two(c.y, c.y_stride);
+  w.quads = c.N % 4 == 0;
+  if (c.T == 0) w.blocks = 0;
+  hipError_t r = dtype == LCSM_F32 ? ssm_prompt_f32(c, w, st)
+                 : dtype == LCSM_BF16 ? ssm_prompt_bf16(c, w, st) : ssm_prompt_f16(c, w, st);
+  if (r != hipSuccess || c.W == 1) return r;
+  const dim3 grid((unsigned)((c.C + 255) / 256), (unsigned)c.n);
+  with_dtype(dtype, [&](auto v) {
+    hipLaunchKernelGGL(k_ssm_window<decltype(v)>, grid, dim3(256), 0, st, c);
+    return 0;
+  });
+  return hipGetLastError();
+}
+
 }  // namespace
 }  // namespace lcsm
 
@@ -161,7 +203,8 @@ struct lcsm_ssm {
   char* mem;
   void* owned;
   float *state, *conv_w, *conv_b, *A, *skip, *dt_bias;
-  char* window;
+  char *window, *bc;
+  float *states, *decay;
   size_t zero_floats;  // states and windows, from `state` on
   bool faulted;
   char msg[256];
@@ -172,7 +215,7 @@ namespace {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
-  size_t state, window, conv_w, conv_b, A, skip, dt_bias, total;
+  size_t state, window, conv_w, conv_b, A, skip, dt_bias, bc, states, decay, total;
 };
 
 bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
@@ -199,6 +242,15 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   take(&p->A, M * H * 4);
   take(&p->skip, M * H * 4);
   take(&p->dt_bias, M * H * 4);
+  if (s->max_tokens) {
+    const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
+    const size_t segments = lcsm::most_segments(s->H, s->G, s->P, blocks + s->slots);
+    if ((double)blocks * s->G * lcsm::ssm_block_bytes(s->N) + (double)segments * D * s->N * 4 > 70368744177664.0)
+      return false;
+    take(&p->bc, blocks * s->G * lcsm::ssm_block_bytes(s->N));
+    take(&p->states, segments * (size_t)D * s->N * 4);
+    take(&p->decay, segments * H * 4);
+  }
   p->total = at;
   return true;
 }
@@ -279,6 +331,11 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
   c->A = (float*)(c->mem + p.A);
   c->skip = (float*)(c->mem + p.skip);
   c->dt_bias = (float*)(c->mem + p.dt_bias);
+  if (shape->max_tokens) {
+    c->bc = c->mem + p.bc;
+    c->states = (float*)(c->mem + p.states);
+    c->decay = (float*)(c->mem + p.decay);
+  }
   const size_t MC = (size_t)shape->M * c->C, MH = (size_t)shape->M * shape->H;
   const struct {
     float* dst;
@@ -324,9 +381,7 @@ int lcsm_ssm_prompt_layer(lcsm_ssm* ctx, int layer, int T, int n, const int* off
   int r = ssm_call(ctx, layer, T, n, io, &k);
   if (r || !n) return r;
   k.offsets = offsets;
-  hipError_t e = lcsm::with_dtype(ctx->s.dtype, [&](auto v) {
-    return lcsm::launch_scan<decltype(v)>(k, ctx->stream);
-  });
+  hipError_t e = lcsm::launch_prompt(k, ctx->s.dtype, ctx->bc, ctx->states, ctx->decay, ctx->stream);
   return e == hipSuccess ? LCSM_OK : ssm_fail(ctx, LCSM_EDEVICE, "prompt launch", e);
 }
 

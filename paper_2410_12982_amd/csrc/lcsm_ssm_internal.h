@@ -36,4 +36,36 @@ __device__ __forceinline__ void ssm_rows(const SsmCall& c, int i, int& t0, int& 
   }
 }
 
+// ---- prompts in chunks (lcsm_ssm_prompt.h)
+
+constexpr int kSsmQ = 64;     // positions of a chunk
+constexpr int kSsmWaves = 4;  // waves of a workgroup, 32 channels of a head each
+
+// Operands of one chunk and group for NT blocks of 32 states, in bytes; a
+// fragment of 64 lanes is 1024.  C: [position / 16][state block], B: [state /
+// 16][position block], G = tril(C B^T): the six blocks of 16 x 32 positions
+// that are not above the diagonal; all low parts PART (GPART) after the high
+// ones.
+template <int NT>
+struct SsmBlock {
+  static constexpr int PART = 4096 * NT, GPART = 6144;
+  static constexpr int C = 0, B = 2 * PART, G = 4 * PART, BYTES = G + 2 * GPART;
+};
+inline size_t ssm_block_bytes(int N) {
+  return N <= 32 ? SsmBlock<1>::BYTES : N <= 64 ? SsmBlock<2>::BYTES : N <= 128 ? SsmBlock<4>::BYTES : SsmBlock<8>::BYTES;
+}
+
+struct SsmScratch {
+  char* bc;       // [blocks][G] SsmBlock
+  float* states;  // [segments][H][P][N]: what a segment adds to the state after it
+  float* decay;   // [segments][H]: and what it leaves of the one before it
+  int blocks, segments;  // upper bounds of the call's chunks and segments
+  int per;               // chunks a segment
+  int pair, quads;       // two channels of a row, four states are aligned as one load
+};
+
+hipError_t ssm_prompt_f32(const SsmCall& c, const SsmScratch& w, hipStream_t st);
+hipError_t ssm_prompt_bf16(const SsmCall& c, const SsmScratch& w, hipStream_t st);
+hipError_t ssm_prompt_f16(const SsmCall& c, const SsmScratch& w, hipStream_t st);
+
 }  // namespace lcsm

@@ -1,0 +1,649 @@
+// Prompts of the state space mixer in chunks of 64 positions on the matrix
+// units; included by one source per element type.
+//
+// Within a chunk let l_t be the sum of the steps' log2-decays up to t, w_s =
+// step_s 2^(l_Q - l_s) and E_t = 2^(l_t - l_Q) (Q the last position).  The
+// recurrence unrolled over the chunk is, per head,
+//
+//   y_t  = E_t [ C (2^l_Q S)^T + tril(C B^T) (w o x) ]_t,
+//   S'   = 2^l_Q S + (w o x)^T B,
+//
+// three matrix products in which only w o x, S and the row factor E belong to
+// the head: B, C and tril(C B^T) are made once per chunk and group, by
+// k_ssm_bc, already as matrix operands, and staged in LDS for the heads of a
+// workgroup.  A wave has 32 channels of a head (lane: two neighbouring ones)
+// and keeps their states in registers as the products' accumulators; with the
+// K index of a product ordered as below, an accumulator of S is the right
+// operand of C S^T as it stands, and the lane that convolves x at a position
+// is the one that gets y there, so nothing of a head goes through LDS.
+//
+// E and w stay within 2^64 of each other while the chunk's decay does; where it
+// does not (steps that forget everything), the factor 2^(l_t - l_s) <= 1 is put
+// into the elements of tril(C B^T) one by one instead (`fast` false).
+//
+// Products are made of two bf16 parts a value (hi + lo, 2^-17 together), as hi
+// hi + hi lo + lo hi with fp32 sums: bf16 alone would cost three more digits
+// than the output's one rounding, and fp16 would not hold the range.
+//
+// A product with a value that is not finite reaches positions before it as 0 *
+// inf; where the state shows such a value, the affected channels' products are
+// made without it and their rows from it on set to NaN.
+#pragma once
+
+#include "lcsm_ssm_internal.h"
+
+namespace lcsm {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
+typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+
+// K slots of a 16x16x32 product: lane quarter q holds, in this order, 4q .. 4q+3
+// and 16 + 4q .. 16 + 4q+3 of the block's 32, which are the rows that it holds
+// of two 16x16 accumulators.
+__device__ __forceinline__ v4f mul3(v8bf ah, v8bf al, v8bf bh, v8bf bl, v4f c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bl, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al, bh, c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bh, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
+  v2bf h = {(bf16_t)a, (bf16_t)b};
+  hi = __builtin_bit_cast(unsigned, h);
+  const float ra = a - __builtin_bit_cast(float, hi << 16);
+  const float rb = b - __builtin_bit_cast(float, hi & 0xffff0000u);
+  v2bf l = {(bf16_t)ra, (bf16_t)rb};
+  lo = __builtin_bit_cast(unsigned, l);
+}
+// Eight values as an operand's two parts.
+__device__ __forceinline__ void split8(const float (&v)[8], v8bf& hi, v8bf& lo) {
+  v4u h, l;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    unsigned a, b;
+    split2(v[2 * k], v[2 * k + 1], a, b);
+    h[k] = a;
+    l[k] = b;
+  }
+  hi = __builtin_bit_cast(v8bf, h);
+  lo = __builtin_bit_cast(v8bf, l);
+}
+
+__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+// v / (1 + e^-v); the reciprocal is good to an ulp.
+__device__ __forceinline__ float silu_hw(float v) {
+  return v * __builtin_amdgcn_rcpf(1.f + exp2_hw(-1.44269504f * v));
+}
+
+// The piece [*k0, *k1) of `per` chunks (and its sequence, its number in it and
+// the sequence's chunks) that has number `want` when the pieces of all
+// sequences are counted one after another, every sequence having at least
+// `least`; false past the last one.  All lanes of a wave together.
+__device__ __forceinline__ bool ssm_piece(const SsmCall& c, int want, int per, int least, int& seq, int& num,
+                                          int& chunks) {
+  const int lane = (int)threadIdx.x & 63;
+  int base = 0;
+  for (int i0 = 0; i0 < c.n; i0 += 64) {
+    int mine = 0, ch = 0;
+    if (i0 + lane < c.n) {
+      int t0, t1;
+      ssm_rows(c, i0 + lane, t0, t1);
+      ch = (t1 - t0 + kSsmQ - 1) / kSsmQ;
+      mine = max((ch + per - 1) / per, least);
+    }
+    int sum = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+      const int v = __shfl_up(sum, m);
+      if (lane >= m) sum += v;
+    }
+    const int total = __shfl(sum, 63);
+    if (want < base + total) {
+      const unsigned long long past = __ballot(base + sum > want);
+      const int who = __ffsll(past) - 1;
+      seq = __builtin_amdgcn_readfirstlane(i0 + who);
+      num = __builtin_amdgcn_readfirstlane(want - base - __shfl(sum - mine, who));
+      chunks = __builtin_amdgcn_readfirstlane(__shfl(ch, who));
+      return true;
+    }
+    base += total;
+  }
+  return false;
+}
+
+// Element ch of row r of the sequence that begins at row t0, from the rows or
+// (r < t0) from the window of slot s.
+template <class E>
+__device__ __forceinline__ E ssm_row(const SsmCall& c, int r, int t0, int s, int ch) {
+  if (r >= t0) return static_cast<const E*>(c.xbc)[(size_t)r * c.xbc_stride + ch];
+  if (s < 0) return (E)0.f;
+  return static_cast<const E*>(c.window)[((size_t)s * (c.W - 1) + (r - t0 + c.W - 1)) * c.C + ch];
+}
+
+// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock).
+template <class E, int NT>
+__global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
+  constexpr int NP = 32 * NT, LD = NP + 4;
+  __shared__ __align__(16) float lb[kSsmQ * LD];
+  __shared__ __align__(16) float lc[kSsmQ * LD];
+  int seq, num, chunks;
+  if (!ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
+  if ((int)blockIdx.x >= w.blocks) return;
+  int t0, t1;
+  ssm_rows(c, seq, t0, t1);
+  const int s = ssm_slot(c.src, seq, c.slots), g = (int)blockIdx.y, r0 = t0 + num * kSsmQ;
+  const int tid = (int)threadIdx.x, rows = min(kSsmQ, t1 - r0);
+  // a thread convolves one channel along a quarter of the chunk's rows
+  constexpr int RUN = kSsmQ / 4;
+  for (int k = tid; k < 2 * NP * 4; k += 256) {
+    const int col = k % (2 * NP), run = k / (2 * NP) * RUN;
+    const int n = col % NP;
+    float* to = (col < NP ? lb : lc) + run * LD + n;
+    if (n >= c.N) {
+      for (int t = 0; t < RUN; ++t) to[t * LD] = 0.f;
+      continue;
+    }
+    const int ch = c.D + (col < NP ? 0 : c.G * c.N) + g * c.N + n;
+    float tap[4] = {0.f, 0.f, 0.f, 0.f}, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < c.W) tap[3 - j] = c.conv_w[(size_t)ch * c.W + c.W - 1 - j];
+    const float bias = c.conv_b[ch];
+#pragma unroll
+    for (int j = 1; j < 4; ++j)
+      if (j < c.W && run - j < rows) x[3 - j] = (float)ssm_row<E>(c, r0 + run - j, t0, s, ch);
+#pragma unroll
+    for (int t = 0; t < RUN; ++t) {
+      float v = 0.f;
+      if (run + t < rows) {
+        x[3] = (float)static_cast<const E*>(c.xbc)[(size_t)(r0 + run + t) * c.xbc_stride + ch];
+        v = bias;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (3 - j < c.W) v = fmaf(tap[j], x[j], v);
+        v = silu_hw(v);
+        x[0] = x[1];
+        x[1] = x[2];
+        x[2] = x[3];
+      }
+      to[t * LD] = v;
+    }
+  }
+  __syncthreads();
+  char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * SsmBlock<NT>::BYTES;
+  const int lane = tid & 63, wv = tid >> 6, q = lane >> 4, l = lane & 15;
+  auto put = [&](int at, int step, const float (&v)[8]) {
+    v8bf hi, lo;
+    split8(v, hi, lo);
+    reinterpret_cast<v8bf*>(out + at)[lane] = hi;
+    reinterpret_cast<v8bf*>(out + at + step)[lane] = lo;
+  };
+  for (int f = wv; f < 4 * NT; f += 4) {
+    const int tt = f / NT, cc = f % NT;
+    const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
+    const float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
+    put(SsmBlock<NT>::C + f * 1024, SsmBlock<NT>::PART, v);
+  }
+  for (int f = wv; f < 4 * NT; f += 4) {
+    const int a = f / 2, cc = f % 2;
+    const float* p = lb + (32 * cc + 4 * q) * LD + 16 * a + l;
+    const float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
+    put(SsmBlock<NT>::B + f * 1024, SsmBlock<NT>::PART, v);
+  }
+  // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
+  // are the lane's slots
+  for (int f = wv; f < 6; f += 4) {
+    const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
+    float v[8];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int st = 2 * cc + half;
+      v4f acc = {0.f, 0.f, 0.f, 0.f};
+      if (st <= tt) {
+        const float* pb = lb + (16 * st + l) * LD + q;
+        const float* pc = lc + (16 * tt + l) * LD + q;
+#pragma unroll 8
+        for (int k = 0; k < NP / 4; ++k)
+          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(pb[4 * k], pc[4 * k], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * half + i] = 16 * st + 4 * q + i <= 16 * tt + l ? acc[i] : 0.f;
+    }
+    put(SsmBlock<NT>::G + f * 1024, SsmBlock<NT>::GPART, v);
+  }
+}
+
+// Two neighbouring channels of a row as they come.
+template <class E>
+struct Pair {
+  unsigned v;
+  __device__ float lo() const {
+    const E e = __builtin_bit_cast(E, (unsigned short)v);
+    return (float)e;
+  }
+  __device__ float hi() const {
+    const E e = __builtin_bit_cast(E, (unsigned short)(v >> 16));
+    return (float)e;
+  }
+  __device__ void set(E a, E b) {
+    v = __builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+  }
+};
+template <>
+struct Pair<float> {
+  float a, b;
+  __device__ float lo() const { return a; }
+  __device__ float hi() const { return b; }
+  __device__ void set(float x, float y) {
+    a = x;
+    b = y;
+  }
+};
+
+// p[0], p[1] where there are `have` (0 .. 2) of them; `pair`: as one load.
+template <class E>
+__device__ __forceinline__ Pair<E> load_pair(const E* p, int have, bool pair) {
+  Pair<E> v;
+  if (pair) {
+    struct alignas(2 * sizeof(E)) Two {
+      E e[2];
+    };
+    v.set((E)0.f, (E)0.f);
+    if (have == 2) {
+      const Two t = *reinterpret_cast<const Two*>(p);
+      v.set(t.e[0], t.e[1]);
+    }
+  } else {
+    v.set(have > 0 ? p[0] : (E)0.f, have > 1 ? p[1] : (E)0.f);
+  }
+  return v;
+}
+
+// One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
+// state before it; else its own contribution to the state after it.
+template <class E, int NT, bool OUT>
+__global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
+  typedef SsmBlock<NT> Blk;
+  constexpr int NA = 2 * NT;
+  extern __shared__ __align__(16) char lds[];
+  const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), nw = (int)blockDim.x >> 6;
+  int seq, num, chunks;
+  if (!ssm_piece(c, (int)blockIdx.y, w.per, 1, seq, num, chunks)) return;
+  if ((int)blockIdx.y >= w.segments) return;
+  const bool last = (num + 1) * w.per >= chunks;
+  if (!OUT && last) return;
+  int t0, t1;
+  ssm_rows(c, seq, t0, t1);
+  const int src = ssm_slot(c.src, seq, c.slots), dst = ssm_slot(c.dst, seq, c.slots);
+  // the first block of this sequence, counted as k_ssm_bc does
+  int block0 = 0;
+  for (int i = lane; i < seq; i += 64) {
+    int a, b;
+    ssm_rows(c, i, a, b);
+    block0 += (b - a + kSsmQ - 1) / kSsmQ;
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) block0 += __shfl_xor(block0, m);
+  // (offsets that do not rise could count more blocks than there are)
+  const int k0 = num * w.per, k1 = min(min(k0 + w.per, chunks), w.blocks - block0);
+
+  // head and channels of this wave; a wave past the last one works on the last
+  // one's data and stores nothing
+  const int hg = c.H / c.G, parts = (c.P + 31) / 32, items = hg * parts;
+  const int wgs = (items + nw - 1) / nw;
+  const int g = (int)blockIdx.x / wgs;
+  const int item = ((int)blockIdx.x % wgs) * nw + wv;
+  const bool live = item < items;
+  const int it = live ? item : items - 1;
+  const int h = g * hg + it / parts, p = (it % parts) * 32 + 2 * l;
+  const int have = min(max(c.P - p, 0), 2);  // channels this lane has
+  const int ch = h * c.P + p;                // x, z, y
+  float* priv = reinterpret_cast<float*>(lds + Blk::BYTES) + wv * 4 * kSsmQ;
+  float *pw = priv, *pe = priv + kSsmQ, *plh = priv + 2 * kSsmQ, *pll = priv + 3 * kSsmQ;
+
+  float tap[2][4], bias[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int cc = min(ch + e, c.D - 1);
+    bias[e] = c.conv_b[cc];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tap[e][j] = 3 - j < c.W ? c.conv_w[(size_t)cc * c.W + c.W - 4 + j] : 0.f;
+  }
+  const float A = c.A[h], skip = c.skip[h], dtb = c.dt_bias[h];
+  const E* xp = static_cast<const E*>(c.xbc) + ch;
+  const E* zp = static_cast<const E*>(c.z) + ch;
+
+  v4f S[NA][2];  // n = 16 a + 4 q + i, channel p + e
+  auto state_at = [&](float* base, int a, int e) { return base + (size_t)(p + e) * c.N + 16 * a + 4 * q; };
+  auto get_state = [&](const float* base, int a, int e) {
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+    if (e >= have) return v;
+    const float* at = base + (size_t)(p + e) * c.N + 16 * a + 4 * q;
+    if (w.quads) {
+      if (16 * a + 4 * q < c.N) v = *reinterpret_cast<const v4f*>(at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (16 * a + 4 * q + i < c.N) v[i] = at[i];
+    }
+    return v;
+  };
+  auto put_state = [&](float* base) {
+    if (!live) return;
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (e >= have) continue;
+        float* at = state_at(base, a, e);
+        if (w.quads) {
+          if (16 * a + 4 * q < c.N) *reinterpret_cast<v4f*>(at) = S[a][e];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * a + 4 * q + i < c.N) at[i] = S[a][e][i];
+        }
+      }
+  };
+  const size_t per_head = (size_t)c.P * c.N;
+#pragma unroll
+  for (int a = 0; a < NA; ++a)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
+      if (OUT && src >= 0) S[a][e] = get_state(c.state + ((size_t)src * c.H + h) * per_head, a, e);
+    }
+  if (OUT) {
+    for (int k = 0; k < num; ++k) {
+      const size_t sg = (size_t)(blockIdx.y - num + k) * c.H + h;
+      const float f = w.decay[sg];
+#pragma unroll
+      for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const v4f v = get_state(w.states + sg * per_head, a, e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], f, v[i]);
+        }
+    }
+  }
+
+  double total = 0.0;  // log2 of the segment's decay
+  for (int k = k0; k < k1; ++k) {
+    const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
+    __syncthreads();  // the last chunk's operands have been read
+    {
+      const char* from = w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES;
+      const int first = OUT ? 0 : Blk::B, end = OUT ? Blk::BYTES : Blk::G;
+      for (int at = first + wv * 1024; at < end; at += nw * 1024)
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(from + at + lane * 16),
+            (__attribute__((address_space(3))) void*)(lds + at), 16, 0, 0);
+    }
+
+    // steps and decays, a position a lane
+    bool fast;
+    float dq;
+    {
+      float step = 0.f;
+      if (lane < rows)
+        step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + dtb);
+      double a = (double)(step * A) * 1.4426950408889634;
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) {
+        const double v = __shfl_up(a, m);
+        if (lane >= m) a += v;
+      }
+      const double aq = __shfl(a, 63);
+      total += aq;
+      const float lq = (float)aq;
+      dq = exp2_hw(lq);
+      fast = lq > -64.f && lq < 64.f;
+      pw[lane] = step * exp2_hw((float)(aq - a));
+      if (OUT) {
+        if (fast) {
+          pe[lane] = exp2_hw((float)(a - aq));
+        } else {
+          const float lh = (float)a;
+          pe[lane] = step;
+          plh[lane] = lh;
+          pll[lane] = (float)(a - (double)lh);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+
+    // x convolved: positions 16 m + 4 q + i, as slots of two blocks of 32
+    float u[4][4][2];
+    v8bf xh[2][2], xl[2][2];  // [block][channel]: w o x
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int tm = 16 * m + 4 * q;
+      Pair<E> raw[7];
+#pragma unroll
+      for (int j = 0; j < 7; ++j) {
+        const int r = r0 + tm - 3 + j;
+        if (j >= 3 || 3 - j < c.W) {
+          if (r >= t0 || r - t0 < -(c.W - 1)) {
+            raw[j] = load_pair<E>(xp + (size_t)max(min(r, t1 - 1), t0) * c.xbc_stride,
+                                  tm - 3 + j < rows && r >= t0 ? have : 0, w.pair);
+          } else {
+            raw[j].set(have > 0 ? ssm_row<E>(c, r, t0, src, ch) : (E)0.f,
+                       have > 1 ? ssm_row<E>(c, r, t0, src, ch + 1) : (E)0.f);
+          }
+        } else {
+          raw[j].set((E)0.f, (E)0.f);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a = bias[0], b = bias[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (3 - j < c.W) {
+            a = fmaf(tap[0][j], raw[i + j].lo(), a);
+            b = fmaf(tap[1][j], raw[i + j].hi(), b);
+          }
+        u[m][i][0] = tm + i < rows ? silu_hw(a) : 0.f;
+        u[m][i][1] = tm + i < rows ? silu_hw(b) : 0.f;
+      }
+    }
+    auto operands = [&](const float* by) {
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc) {
+        const v4f w0 = *reinterpret_cast<const v4f*>(by + 32 * cc + 4 * q);
+        const v4f w1 = *reinterpret_cast<const v4f*>(by + 32 * cc + 16 + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = u[2 * cc][i][e] * w0[i];
+            v[4 + i] = u[2 * cc + 1][i][e] * w1[i];
+          }
+          split8(v, xh[cc][e], xl[cc][e]);
+        }
+      }
+    };
+    operands(pw);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the chunk's operands are in LDS
+
+    auto frag = [&](int at) { return *reinterpret_cast<const v8bf*>(lds + at + lane * 16); };
+    v4f y[4][2];
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
+    const float before = fast ? dq : 1.f, after = fast ? 1.f : dq;
+#pragma unroll
+    for (int cc = 0; cc < NT; ++cc) {
+      if (OUT) {
+        v8bf sh[2], sl[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = S[2 * cc][e][i] *= before;
+            v[4 + i] = S[2 * cc + 1][e][i] *= before;
+          }
+          split8(v, sh[e], sl[e]);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          const v8bf ah = frag(Blk::C + (tt * NT + cc) * 1024), al = frag(Blk::C + Blk::PART + (tt * NT + cc) * 1024);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) y[tt][e] = mul3(ah, al, sh[e], sl[e], y[tt][e]);
+        }
+      }
+#pragma unroll
+      for (int a = 2 * cc; a < 2 * cc + 2; ++a) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) S[a][e] *= OUT ? after : dq;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const v8bf ah = frag(Blk::B + (a * 2 + b) * 1024), al = frag(Blk::B + Blk::PART + (a * 2 + b) * 1024);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) S[a][e] = mul3(ah, al, xh[b][e], xl[b][e], S[a][e]);
+        }
+      }
+    }
+    if (!OUT) continue;
+
+    if (!fast) {
+      // rows by 2^l_t, then the elements' own decays; operands without them
+      const float* by = pe;
+      operands(by);
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = 16 * tt + 4 * q + i;
+          const float f = exp2_hw(plh[t] + pll[t]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) y[tt][e][i] *= f;
+        }
+    }
+    // a value of w o x that is not finite shows in every state of its channel
+    int bad[2] = {kSsmQ, kSsmQ};
+    const bool odd = !(fabsf(S[0][0][0]) < INFINITY) || !(fabsf(S[0][1][0]) < INFINITY);
+    if (__ballot(odd)) {
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          v4u hi = __builtin_bit_cast(v4u, xh[cc][e]), lo = __builtin_bit_cast(v4u, xl[cc][e]);
+#pragma unroll
+          for (int j = 7; j >= 0; --j) {
+            const unsigned part = j & 1 ? 0xffff0000u : 0xffffu, top = part & 0x7f807f80u;
+            if ((hi[j / 2] & top) == top) {
+              hi[j / 2] &= ~part;
+              lo[j / 2] &= ~part;
+              bad[e] = min(bad[e], 32 * cc + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
+            }
+          }
+          xh[cc][e] = __builtin_bit_cast(v8bf, hi);
+          xl[cc][e] = __builtin_bit_cast(v8bf, lo);
+        }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        bad[e] = min(bad[e], __shfl_xor(bad[e], 16));
+        bad[e] = min(bad[e], __shfl_xor(bad[e], 32));
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < 6; ++f) {
+      const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
+      v8bf ah = frag(Blk::G + f * 1024), al = frag(Blk::G + Blk::GPART + f * 1024);
+      if (!fast) {
+        const int t = 16 * tt + l;
+        const float lt = plh[t], rt = pll[t];
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int s = 32 * cc + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
+          const float d = exp2_hw((lt - plh[s]) + (rt - pll[s]));
+          v[j] = s <= t ? ((float)ah[j] + (float)al[j]) * d : 0.f;
+        }
+        split8(v, ah, al);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) y[tt][e] = mul3(ah, al, xh[cc][e], xl[cc][e], y[tt][e]);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      v4f E4 = {1.f, 1.f, 1.f, 1.f};
+      if (fast) E4 = *reinterpret_cast<const v4f*>(pe + 16 * m + 4 * q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 16 * m + 4 * q + i;
+        if (t >= rows || have == 0 || !live) continue;
+        float v[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          v[e] = fmaf(skip, u[m][i][e], y[m][e][i] * E4[i]);
+          if (t >= bad[e]) v[e] = __builtin_nanf("");
+        }
+        if (c.z) {
+          const Pair<E> z = load_pair<E>(zp + (size_t)(r0 + t) * c.z_stride, have, w.pair);
+          v[0] *= silu_hw(z.lo());
+          v[1] *= silu_hw(z.hi());
+        }
+        E* to = static_cast<E*>(c.y) + (size_t)(r0 + t) * c.y_stride + ch;
+        if (w.pair) {
+          struct alignas(2 * sizeof(E)) Two {
+            E e[2];
+          };
+          *reinterpret_cast<Two*>(to) = Two{{(E)v[0], (E)v[1]}};
+        } else {
+          to[0] = (E)v[0];
+          if (have > 1) to[1] = (E)v[1];
+        }
+      }
+    }
+  }
+  if (!OUT) {
+    const size_t sg = (size_t)blockIdx.y * c.H + h;
+    put_state(w.states + sg * per_head);
+    if (live && lane == 0 && it % parts == 0) w.decay[sg] = (float)exp2(total);
+  } else if (last && dst >= 0) {
+    put_state(c.state + ((size_t)dst * c.H + h) * per_head);
+  }
+}
+
+template <class E, int NT>
+hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
+  const int items = c.H / c.G * ((c.P + 31) / 32);
+  const int nw = items < kSsmWaves ? items : kSsmWaves;
+  const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)), (unsigned)w.segments);
+  const size_t lds = SsmBlock<NT>::BYTES + (size_t)nw * 4 * kSsmQ * sizeof(float);
+  auto out = k_ssm_chunks<E, NT, true>;
+  auto sum = k_ssm_chunks<E, NT, false>;
+  hipError_t e = hipSuccess;
+  if (w.blocks) {
+    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)c.G), dim3(256), 0, st, c, w);
+    e = hipGetLastError();
+  }
+  for (const void* f : {reinterpret_cast<const void*>(out), reinterpret_cast<const void*>(sum)})
+    if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e == hipSuccess && w.segments > c.n) {
+    hipLaunchKernelGGL(sum, grid, dim3(64 * nw), lds, st, c, w);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(out, grid, dim3(64 * nw), lds, st, c, w);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t ssm_prompt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
+  if (c.N <= 32) return ssm_prompt_nt<E, 1>(c, w, st);
+  if (c.N <= 64) return ssm_prompt_nt<E, 2>(c, w, st);
+  if (c.N <= 128) return ssm_prompt_nt<E, 4>(c, w, st);
+  return ssm_prompt_nt<E, 8>(c, w, st);
+}
+
+}  // namespace lcsm
