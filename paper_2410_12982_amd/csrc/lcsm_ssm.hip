@@ -156,15 +156,15 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
 // are that many by themselves are not cut.
 constexpr int kSsmWorkgroups = 512;
 
-int head_groups(int H, int G, int P) {
-  const int items = H / G * ((P + 31) / 32), nw = items < kSsmWaves ? items : kSsmWaves;
+int head_groups(int H, int G, int P, int N) {
+  const int items = H / G * ((P + 31) / 32), nw = items < ssm_waves(N) ? items : ssm_waves(N);
   return G * ((items + nw - 1) / nw);
 }
 // Upper bound of the segments of a call that is cut: fewer than `want` pieces
 // of all chunks and one more for each of fewer than `want` sequences; `cuts`:
 // chunks and sequences of the largest call.
-size_t most_segments(int H, int G, int P, size_t cuts) {
-  const size_t most = 2 * (size_t)kSsmWorkgroups / head_groups(H, G, P) + 2;
+size_t most_segments(int H, int G, int P, int N, size_t cuts) {
+  const size_t most = 2 * (size_t)kSsmWorkgroups / head_groups(H, G, P, N) + 2;
   return most < cuts ? most : cuts;
 }
 
@@ -174,7 +174,7 @@ hipError_t launch_prompt(const SsmCall& c, int dtype, char* bc, float* states, f
   w.states = states;
   w.decay = decay;
   w.blocks = c.T / kSsmQ + c.n;  // a sequence's last chunk may be short
-  const int wgs = head_groups(c.H, c.G, c.P), want = kSsmWorkgroups / wgs;
+  const int wgs = head_groups(c.H, c.G, c.P, c.N), want = kSsmWorkgroups / wgs;
   w.per = want > c.n ? (w.blocks + want - 1) / want : w.blocks;
   w.segments = want > c.n ? w.blocks / w.per + c.n : c.n;
   const size_t e = dtype_size(dtype);
@@ -244,10 +244,11 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   take(&p->dt_bias, M * H * 4);
   if (s->max_tokens) {
     const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
-    const size_t segments = lcsm::most_segments(s->H, s->G, s->P, blocks + s->slots);
-    if ((double)blocks * s->G * lcsm::ssm_block_bytes(s->N) + (double)segments * D * s->N * 4 > 70368744177664.0)
+    const size_t each = lcsm::ssm_block_bytes(s->N, lcsm::dtype_size(s->dtype));
+    const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
+    if ((double)blocks * s->G * each + (double)segments * D * s->N * 4 > 70368744177664.0)
       return false;
-    take(&p->bc, blocks * s->G * lcsm::ssm_block_bytes(s->N));
+    take(&p->bc, blocks * s->G * each);
     take(&p->states, segments * (size_t)D * s->N * 4);
     take(&p->decay, segments * H * 4);
   }

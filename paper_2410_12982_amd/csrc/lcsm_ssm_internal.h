@@ -38,22 +38,36 @@ __device__ __forceinline__ void ssm_rows(const SsmCall& c, int i, int& t0, int& 
 
 // ---- prompts in chunks (lcsm_ssm_prompt.h)
 
-constexpr int kSsmQ = 64;     // positions of a chunk
-constexpr int kSsmWaves = 4;  // waves of a workgroup, 32 channels of a head each
+constexpr int kSsmQ = 64;  // positions of a chunk
+
+// bf16 parts of a value in products that end in fp32 (states, fp32 outputs), and
+// in those whose sum is rounded to 16 bits.
+constexpr int kSsmParts = 3;
+inline constexpr int ssm_out_parts(size_t elem) { return elem == 4 ? kSsmParts : 2; }
 
 // Operands of one chunk and group for NT blocks of 32 states, in bytes; a
 // fragment of 64 lanes is 1024.  C: [position / 16][state block], B: [state /
 // 16][position block], G = tril(C B^T): the six blocks of 16 x 32 positions
-// that are not above the diagonal; all low parts PART (GPART) after the high
-// ones.
-template <int NT>
+// that are not above the diagonal; every one part after part (PY of C and G, 3
+// of B).  C and B of NB state blocks at a time are what LDS holds (STAGE).
+template <int NT, int PY>
 struct SsmBlock {
-  static constexpr int PART = 4096 * NT, GPART = 6144;
-  static constexpr int C = 0, B = 2 * PART, G = 4 * PART, BYTES = G + 2 * GPART;
+  static constexpr int NB = NT < 4 ? NT : 4, STAGES = NT / NB;
+  static constexpr int PART = 4096 * NB, GPART = 6144;
+  static constexpr int STAGE = (PY + kSsmParts) * PART, G = STAGES * STAGE, GBYTES = PY * GPART;
+  static constexpr int BYTES = G + GBYTES, LDS = STAGE + GBYTES;
+  static constexpr int c_at(int tt, int cc) { return cc / NB * STAGE + (tt * NB + cc % NB) * 1024; }
+  static constexpr int b_at(int a, int b) { return a / (2 * NB) * STAGE + PY * PART + (a % (2 * NB) * 2 + b) * 1024; }
+  static constexpr int g_at(int f) { return G + f * 1024; }
 };
-inline size_t ssm_block_bytes(int N) {
-  return N <= 32 ? SsmBlock<1>::BYTES : N <= 64 ? SsmBlock<2>::BYTES : N <= 128 ? SsmBlock<4>::BYTES : SsmBlock<8>::BYTES;
+inline int ssm_blocks_of(int N) { return N <= 32 ? 1 : N <= 64 ? 2 : N <= 128 ? 4 : 8; }
+inline size_t ssm_block_bytes(int N, size_t elem) {
+  const int nt = ssm_blocks_of(N), py = ssm_out_parts(elem);
+  return (size_t)4096 * nt * (py + kSsmParts) + (size_t)py * 6144;
 }
+// Waves of a workgroup, 32 channels of a head each: they share the operands in
+// LDS, and have the registers of a compute unit to themselves.
+inline int ssm_waves(int N) { return N <= 128 ? 8 : 4; }
 
 struct SsmScratch {
   char* bc;       // [blocks][G] SsmBlock

@@ -21,14 +21,18 @@
 // does not (steps that forget everything), the factor 2^(l_t - l_s) <= 1 is put
 // into the elements of tril(C B^T) one by one instead (`fast` false).
 //
-// Products are made of two bf16 parts a value (hi + lo, 2^-17 together), as hi
-// hi + hi lo + lo hi with fp32 sums: bf16 alone would cost three more digits
-// than the output's one rounding, and fp16 would not hold the range.
+// Values go into the products as sums of bf16 parts, which hold fp32's range
+// (fp16 would not): three parts and the six products above 2^-24 for the states
+// and for fp32 outputs, whose sums are then as good as fp32's, two parts and
+// three products (2^-16) where the sum is rounded to 16 bits.  bf16 alone would
+// add an error as large as that rounding for every operand.
 //
 // A product with a value that is not finite reaches positions before it as 0 *
 // inf; where the state shows such a value, the affected channels' products are
 // made without it and their rows from it on set to NaN.
 #pragma once
+
+#include <type_traits>
 
 #include "lcsm_ssm_internal.h"
 
@@ -42,32 +46,35 @@ typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
 // K slots of a 16x16x32 product: lane quarter q holds, in this order, 4q .. 4q+3
 // and 16 + 4q .. 16 + 4q+3 of the block's 32, which are the rows that it holds
 // of two 16x16 accumulators.
-__device__ __forceinline__ v4f mul3(v8bf ah, v8bf al, v8bf bh, v8bf bl, v4f c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bl, c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al, bh, c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bh, c, 0, 0, 0);
+//
+// a b with both in parts, the small products first.
+template <int P>
+__device__ __forceinline__ v4f mul(const v8bf (&a)[P], const v8bf (&b)[P], v4f c) {
+#pragma unroll
+  for (int sum = P - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i <= sum; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[sum - i], c, 0, 0, 0);
+  return c;
 }
 
-__device__ __forceinline__ void split2(float a, float b, unsigned& hi, unsigned& lo) {
-  v2bf h = {(bf16_t)a, (bf16_t)b};
-  hi = __builtin_bit_cast(unsigned, h);
-  const float ra = a - __builtin_bit_cast(float, hi << 16);
-  const float rb = b - __builtin_bit_cast(float, hi & 0xffff0000u);
-  v2bf l = {(bf16_t)ra, (bf16_t)rb};
-  lo = __builtin_bit_cast(unsigned, l);
-}
-// Eight values as an operand's two parts.
-__device__ __forceinline__ void split8(const float (&v)[8], v8bf& hi, v8bf& lo) {
-  v4u h, l;
+// Eight values as an operand's parts: each the bf16 nearest to what the parts
+// before it leave.
+template <int P>
+__device__ __forceinline__ void split(float (&v)[8], v8bf (&to)[P]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    unsigned a, b;
-    split2(v[2 * k], v[2 * k + 1], a, b);
-    h[k] = a;
-    l[k] = b;
+  for (int p = 0; p < P; ++p) {
+    v4u w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const v2bf two = {(bf16_t)v[2 * k], (bf16_t)v[2 * k + 1]};
+      w[k] = __builtin_bit_cast(unsigned, two);
+      if (p + 1 < P) {
+        v[2 * k] -= __builtin_bit_cast(float, w[k] << 16);
+        v[2 * k + 1] -= __builtin_bit_cast(float, w[k] & 0xffff0000u);
+      }
+    }
+    to[p] = __builtin_bit_cast(v8bf, w);
   }
-  hi = __builtin_bit_cast(v8bf, h);
-  lo = __builtin_bit_cast(v8bf, l);
 }
 
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -124,7 +131,8 @@ __device__ __forceinline__ E ssm_row(const SsmCall& c, int r, int t0, int s, int
 // B, C and tril(C B^T) of one chunk and group as operands (SsmBlock).
 template <class E, int NT>
 __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
-  constexpr int NP = 32 * NT, LD = NP + 4;
+  constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
+  typedef SsmBlock<NT, PY> Blk;
   __shared__ __align__(16) float lb[kSsmQ * LD];
   __shared__ __align__(16) float lc[kSsmQ * LD];
   int seq, num, chunks;
@@ -171,25 +179,27 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
     }
   }
   __syncthreads();
-  char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * SsmBlock<NT>::BYTES;
+  char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * Blk::BYTES;
   const int lane = tid & 63, wv = tid >> 6, q = lane >> 4, l = lane & 15;
-  auto put = [&](int at, int step, const float (&v)[8]) {
-    v8bf hi, lo;
-    split8(v, hi, lo);
-    reinterpret_cast<v8bf*>(out + at)[lane] = hi;
-    reinterpret_cast<v8bf*>(out + at + step)[lane] = lo;
+  auto put = [&](int at, int step, float (&v)[8], auto parts) {
+    v8bf w[decltype(parts)::value];
+    split(v, w);
+#pragma unroll
+    for (int k = 0; k < decltype(parts)::value; ++k) reinterpret_cast<v8bf*>(out + at + k * step)[lane] = w[k];
   };
+  const std::integral_constant<int, PY> py;
+  const std::integral_constant<int, kSsmParts> ps;
   for (int f = wv; f < 4 * NT; f += 4) {
     const int tt = f / NT, cc = f % NT;
     const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
-    const float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
-    put(SsmBlock<NT>::C + f * 1024, SsmBlock<NT>::PART, v);
+    float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
+    put(Blk::c_at(tt, cc), Blk::PART, v, py);
   }
   for (int f = wv; f < 4 * NT; f += 4) {
-    const int a = f / 2, cc = f % 2;
-    const float* p = lb + (32 * cc + 4 * q) * LD + 16 * a + l;
-    const float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
-    put(SsmBlock<NT>::B + f * 1024, SsmBlock<NT>::PART, v);
+    const int a = f / 2, b = f % 2;
+    const float* p = lb + (32 * b + 4 * q) * LD + 16 * a + l;
+    float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
+    put(Blk::b_at(a, b), Blk::PART, v, ps);
   }
   // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
   // are the lane's slots
@@ -210,7 +220,7 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * half + i] = 16 * st + 4 * q + i <= 16 * tt + l ? acc[i] : 0.f;
     }
-    put(SsmBlock<NT>::G + f * 1024, SsmBlock<NT>::GPART, v);
+    put(Blk::g_at(f), Blk::GPART, v, py);
   }
 }
 
@@ -263,9 +273,10 @@ __device__ __forceinline__ Pair<E> load_pair(const E* p, int have, bool pair) {
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
 template <class E, int NT, bool OUT>
-__global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
-  typedef SsmBlock<NT> Blk;
-  constexpr int NA = 2 * NT;
+__global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, SsmScratch w) {
+  constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
+  typedef SsmBlock<NT, PY> Blk;
+  constexpr int NA = 2 * NT, NB = Blk::NB;
   extern __shared__ __align__(16) char lds[];
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), nw = (int)blockDim.x >> 6;
@@ -300,7 +311,7 @@ __global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   const int h = g * hg + it / parts, p = (it % parts) * 32 + 2 * l;
   const int have = min(max(c.P - p, 0), 2);  // channels this lane has
   const int ch = h * c.P + p;                // x, z, y
-  float* priv = reinterpret_cast<float*>(lds + Blk::BYTES) + wv * 4 * kSsmQ;
+  float* priv = reinterpret_cast<float*>(lds + Blk::LDS) + wv * 4 * kSsmQ;
   float *pw = priv, *pe = priv + kSsmQ, *plh = priv + 2 * kSsmQ, *pll = priv + 3 * kSsmQ;
 
   float tap[2][4], bias[2];
@@ -373,15 +384,19 @@ __global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   double total = 0.0;  // log2 of the segment's decay
   for (int k = k0; k < k1; ++k) {
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
+    const char* from = w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES;
+    auto fetch = [&](int at, int to, int bytes) {
+      for (int i = wv * 1024; i < bytes; i += nw * 1024)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + at + i + lane * 16),
+                                         (__attribute__((address_space(3))) void*)(lds + to + i), 16, 0, 0);
+    };
+    auto fetch_stage = [&](int stage) {
+      const int skip = OUT ? 0 : PY * Blk::PART;
+      fetch(stage * Blk::STAGE + skip, skip, Blk::STAGE - skip);
+      if (OUT && stage == Blk::STAGES - 1) fetch(Blk::G, Blk::STAGE, Blk::GBYTES);
+    };
     __syncthreads();  // the last chunk's operands have been read
-    {
-      const char* from = w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES;
-      const int first = OUT ? 0 : Blk::B, end = OUT ? Blk::BYTES : Blk::G;
-      for (int at = first + wv * 1024; at < end; at += nw * 1024)
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void*)(from + at + lane * 16),
-            (__attribute__((address_space(3))) void*)(lds + at), 16, 0, 0);
-    }
+    fetch_stage(0);
 
     // steps and decays, a position a lane
     bool fast;
@@ -417,7 +432,6 @@ __global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
 
     // x convolved: positions 16 m + 4 q + i, as slots of two blocks of 32
     float u[4][4][2];
-    v8bf xh[2][2], xl[2][2];  // [block][channel]: w o x
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const int tm = 16 * m + 4 * q;
@@ -450,128 +464,153 @@ __global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
         u[m][i][1] = tm + i < rows ? silu_hw(b) : 0.f;
       }
     }
-    auto operands = [&](const float* by) {
+    // u by a factor for every position, as the right operand of position block b
+    auto operand = [&](const float* by, int b, int e, auto& to) {
+      const v4f w0 = *reinterpret_cast<const v4f*>(by + 32 * b + 4 * q);
+      const v4f w1 = *reinterpret_cast<const v4f*>(by + 32 * b + 16 + 4 * q);
+      float v[8];
 #pragma unroll
-      for (int cc = 0; cc < 2; ++cc) {
-        const v4f w0 = *reinterpret_cast<const v4f*>(by + 32 * cc + 4 * q);
-        const v4f w1 = *reinterpret_cast<const v4f*>(by + 32 * cc + 16 + 4 * q);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = u[2 * cc][i][e] * w0[i];
-            v[4 + i] = u[2 * cc + 1][i][e] * w1[i];
-          }
-          split8(v, xh[cc][e], xl[cc][e]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        v[i] = u[2 * b][i][e] * w0[i];
+        v[4 + i] = u[2 * b + 1][i][e] * w1[i];
       }
+      split(v, to);
     };
-    operands(pw);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // the chunk's operands are in LDS
-
-    auto frag = [&](int at) { return *reinterpret_cast<const v8bf*>(lds + at + lane * 16); };
+    auto frag = [&](int at, int step, auto& to) {
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof(to) / sizeof(to[0])); ++k)
+        to[k] = *reinterpret_cast<const v8bf*>(lds + at + k * step + lane * 16);
+    };
     v4f y[4][2];
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
+    int bad[2] = {kSsmQ, kSsmQ};
     const float before = fast ? dq : 1.f, after = fast ? 1.f : dq;
 #pragma unroll
-    for (int cc = 0; cc < NT; ++cc) {
+    for (int stage = 0; stage < Blk::STAGES; ++stage) {
+      if (stage > 0) {
+        __syncthreads();  // the stage before has been read
+        fetch_stage(stage);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();  // the operands are in LDS
       if (OUT) {
-        v8bf sh[2], sl[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float v[8];
+        for (int cc = stage * NB; cc < (stage + 1) * NB; ++cc) {
+          v8bf sp[2][PY];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = S[2 * cc][e][i] *= before;
-            v[4 + i] = S[2 * cc + 1][e][i] *= before;
+          for (int e = 0; e < 2; ++e) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              v[i] = S[2 * cc][e][i] *= before;
+              v[4 + i] = S[2 * cc + 1][e][i] *= before;
+            }
+            split(v, sp[e]);
           }
-          split8(v, sh[e], sl[e]);
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt) {
+            v8bf cp[PY];
+            frag(Blk::c_at(tt, cc) - stage * Blk::STAGE, Blk::PART, cp);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) y[tt][e] = mul(cp, sp[e], y[tt][e]);
+          }
         }
+        if (!fast && stage == Blk::STAGES - 1) {
+          // rows by 2^l_t; the products below have the elements' own decays
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          const v8bf ah = frag(Blk::C + (tt * NT + cc) * 1024), al = frag(Blk::C + Blk::PART + (tt * NT + cc) * 1024);
+          for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) y[tt][e] = mul3(ah, al, sh[e], sl[e], y[tt][e]);
+            for (int i = 0; i < 4; ++i) {
+              const int t = 16 * tt + 4 * q + i;
+              const float f = exp2_hw(plh[t] + pll[t]);
+#pragma unroll
+              for (int e = 0; e < 2; ++e) y[tt][e][i] *= f;
+            }
         }
       }
 #pragma unroll
-      for (int a = 2 * cc; a < 2 * cc + 2; ++a) {
+      for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
 #pragma unroll
         for (int e = 0; e < 2; ++e) S[a][e] *= OUT ? after : dq;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const v8bf ah = frag(Blk::B + (a * 2 + b) * 1024), al = frag(Blk::B + Blk::PART + (a * 2 + b) * 1024);
+      for (int b = 0; b < 2; ++b) {
+        v8bf xp[2][PS];  // w o x
 #pragma unroll
-          for (int e = 0; e < 2; ++e) S[a][e] = mul3(ah, al, xh[b][e], xl[b][e], S[a][e]);
+        for (int e = 0; e < 2; ++e) operand(pw, b, e, xp[e]);
+#pragma unroll
+        for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a) {
+          v8bf bp[PS];
+          frag(Blk::b_at(a, b) - stage * Blk::STAGE, Blk::PART, bp);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) S[a][e] = mul(bp, xp[e], S[a][e]);
+        }
+        if (!OUT || stage != Blk::STAGES - 1) continue;
+        v8bf yp[2][PY];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (fast) {
+#pragma unroll
+            for (int k = 0; k < PY; ++k) yp[e][k] = xp[e][k];
+          } else {
+            operand(pe, b, e, yp[e]);
+          }
+        }
+        // a value of w o x that is not finite shows in every state of its channel
+        const bool odd = !(fabsf(S[0][0][0]) < INFINITY) || !(fabsf(S[0][1][0]) < INFINITY);
+        if (__ballot(odd)) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            v4u part[PY];
+#pragma unroll
+            for (int k = 0; k < PY; ++k) part[k] = __builtin_bit_cast(v4u, yp[e][k]);
+#pragma unroll
+            for (int j = 7; j >= 0; --j) {
+              const unsigned half = j & 1 ? 0xffff0000u : 0xffffu, top = half & 0x7f807f80u;
+              if ((part[0][j / 2] & top) != top) continue;
+#pragma unroll
+              for (int k = 0; k < PY; ++k) part[k][j / 2] &= ~half;
+              bad[e] = min(bad[e], 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
+            }
+#pragma unroll
+            for (int k = 0; k < PY; ++k) yp[e][k] = __builtin_bit_cast(v8bf, part[k]);
+          }
+        }
+#pragma unroll
+        for (int f = 0; f < 6; ++f) {
+          const int tt = f < 2 ? f : 2 + (f - 2) / 2;
+          if ((f < 2 ? 0 : (f - 2) % 2) != b) continue;
+          v8bf gp[PY];
+          frag(Blk::STAGE + f * 1024, Blk::GPART, gp);
+          if (!fast) {
+            const int t = 16 * tt + l;
+            const float lt = plh[t], rt = pll[t];
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int s = 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
+              const float d = exp2_hw((lt - plh[s]) + (rt - pll[s]));
+              float sum = (float)gp[PY - 1][j];
+#pragma unroll
+              for (int k = PY - 2; k >= 0; --k) sum += (float)gp[k][j];
+              v[j] = s <= t ? sum * d : 0.f;
+            }
+            split(v, gp);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) y[tt][e] = mul(gp, yp[e], y[tt][e]);
         }
       }
     }
     if (!OUT) continue;
-
-    if (!fast) {
-      // rows by 2^l_t, then the elements' own decays; operands without them
-      const float* by = pe;
-      operands(by);
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = 16 * tt + 4 * q + i;
-          const float f = exp2_hw(plh[t] + pll[t]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) y[tt][e][i] *= f;
-        }
-    }
-    // a value of w o x that is not finite shows in every state of its channel
-    int bad[2] = {kSsmQ, kSsmQ};
-    const bool odd = !(fabsf(S[0][0][0]) < INFINITY) || !(fabsf(S[0][1][0]) < INFINITY);
-    if (__ballot(odd)) {
-#pragma unroll
-      for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          v4u hi = __builtin_bit_cast(v4u, xh[cc][e]), lo = __builtin_bit_cast(v4u, xl[cc][e]);
-#pragma unroll
-          for (int j = 7; j >= 0; --j) {
-            const unsigned part = j & 1 ? 0xffff0000u : 0xffffu, top = part & 0x7f807f80u;
-            if ((hi[j / 2] & top) == top) {
-              hi[j / 2] &= ~part;
-              lo[j / 2] &= ~part;
-              bad[e] = min(bad[e], 32 * cc + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
-            }
-          }
-          xh[cc][e] = __builtin_bit_cast(v8bf, hi);
-          xl[cc][e] = __builtin_bit_cast(v8bf, lo);
-        }
+    if (__ballot(bad[0] < kSsmQ || bad[1] < kSsmQ)) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         bad[e] = min(bad[e], __shfl_xor(bad[e], 16));
         bad[e] = min(bad[e], __shfl_xor(bad[e], 32));
       }
-    }
-#pragma unroll
-    for (int f = 0; f < 6; ++f) {
-      const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
-      v8bf ah = frag(Blk::G + f * 1024), al = frag(Blk::G + Blk::GPART + f * 1024);
-      if (!fast) {
-        const int t = 16 * tt + l;
-        const float lt = plh[t], rt = pll[t];
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int s = 32 * cc + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
-          const float d = exp2_hw((lt - plh[s]) + (rt - pll[s]));
-          v[j] = s <= t ? ((float)ah[j] + (float)al[j]) * d : 0.f;
-        }
-        split8(v, ah, al);
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) y[tt][e] = mul3(ah, al, xh[cc][e], xl[cc][e], y[tt][e]);
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -617,9 +656,9 @@ __global__ __launch_bounds__(256) void k_ssm_chunks(SsmCall c, SsmScratch w) {
 template <class E, int NT>
 hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
   const int items = c.H / c.G * ((c.P + 31) / 32);
-  const int nw = items < kSsmWaves ? items : kSsmWaves;
+  const int nw = items < ssm_waves(c.N) ? items : ssm_waves(c.N);
   const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)), (unsigned)w.segments);
-  const size_t lds = SsmBlock<NT>::BYTES + (size_t)nw * 4 * kSsmQ * sizeof(float);
+  const size_t lds = SsmBlock<NT, ssm_out_parts(sizeof(E))>::LDS + (size_t)nw * 4 * kSsmQ * sizeof(float);
   auto out = k_ssm_chunks<E, NT, true>;
   auto sum = k_ssm_chunks<E, NT, false>;
   hipError_t e = hipSuccess;
