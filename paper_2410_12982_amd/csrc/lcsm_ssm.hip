@@ -168,11 +168,7 @@ size_t most_segments(int H, int G, int P, int N, size_t cuts) {
   return most < cuts ? most : cuts;
 }
 
-hipError_t launch_prompt(const SsmCall& c, int dtype, char* bc, float* states, float* decay, hipStream_t st) {
-  SsmScratch w{};
-  w.bc = bc;
-  w.states = states;
-  w.decay = decay;
+hipError_t launch_prompt(const SsmCall& c, int dtype, SsmScratch w, hipStream_t st) {
   w.blocks = c.T / kSsmQ + c.n;  // a sequence's last chunk may be short
   const int wgs = head_groups(c.H, c.G, c.P, c.N), want = kSsmWorkgroups / wgs;
   w.per = want > c.n ? (w.blocks + want - 1) / want : w.blocks;
@@ -203,8 +199,8 @@ struct lcsm_ssm {
   char* mem;
   void* owned;
   float *state, *conv_w, *conv_b, *A, *skip, *dt_bias;
-  char *window, *bc;
-  float *states, *decay;
+  char* window;
+  lcsm::SsmScratch scratch;
   size_t zero_floats;  // states and windows, from `state` on
   bool faulted;
   char msg[256];
@@ -215,7 +211,7 @@ namespace {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
-  size_t state, window, conv_w, conv_b, A, skip, dt_bias, bc, states, decay, total;
+  size_t state, window, conv_w, conv_b, A, skip, dt_bias, bc, scal, lq, states, decay, total;
 };
 
 bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
@@ -246,9 +242,11 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
     const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
     const size_t each = lcsm::ssm_block_bytes(s->N, lcsm::dtype_size(s->dtype));
     const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
-    if ((double)blocks * s->G * each + (double)segments * D * s->N * 4 > 70368744177664.0)
+    if ((double)blocks * (s->G * (double)each + H * 2048.0) + (double)segments * D * s->N * 4 > 70368744177664.0)
       return false;
     take(&p->bc, blocks * s->G * each);
+    take(&p->scal, blocks * H * 4 * lcsm::kSsmQ * 4);
+    take(&p->lq, blocks * H * 8);
     take(&p->states, segments * (size_t)D * s->N * 4);
     take(&p->decay, segments * H * 4);
   }
@@ -276,6 +274,8 @@ int ssm_call(lcsm_ssm* c, int layer, int T, int n, const lcsm_ssm_io* io, lcsm::
     if (io->xbc_stride < (size_t)c->C || io->dt_stride < (size_t)c->s.H || io->y_stride < (size_t)c->D ||
         (io->z && io->z_stride < (size_t)c->D))
       return ssm_fail(c, LCSM_EINVAL, "a row stride is shorter than the row");
+    for (size_t stride : {io->xbc_stride, io->dt_stride, io->y_stride, io->z ? io->z_stride : 0})
+      if (stride > lcsm::kSsmMaxStride) return ssm_fail(c, LCSM_EINVAL, "a row stride is above 2^25 elements");
   }
   if (c->faulted) return LCSM_ESTATE;
   const size_t m = (size_t)layer, C = (size_t)c->C, H = (size_t)c->s.H;
@@ -333,9 +333,11 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
   c->skip = (float*)(c->mem + p.skip);
   c->dt_bias = (float*)(c->mem + p.dt_bias);
   if (shape->max_tokens) {
-    c->bc = c->mem + p.bc;
-    c->states = (float*)(c->mem + p.states);
-    c->decay = (float*)(c->mem + p.decay);
+    c->scratch.bc = c->mem + p.bc;
+    c->scratch.scal = (float*)(c->mem + p.scal);
+    c->scratch.lq = (double*)(c->mem + p.lq);
+    c->scratch.states = (float*)(c->mem + p.states);
+    c->scratch.decay = (float*)(c->mem + p.decay);
   }
   const size_t MC = (size_t)shape->M * c->C, MH = (size_t)shape->M * shape->H;
   const struct {
@@ -382,7 +384,7 @@ int lcsm_ssm_prompt_layer(lcsm_ssm* ctx, int layer, int T, int n, const int* off
   int r = ssm_call(ctx, layer, T, n, io, &k);
   if (r || !n) return r;
   k.offsets = offsets;
-  hipError_t e = lcsm::launch_prompt(k, ctx->s.dtype, ctx->bc, ctx->states, ctx->decay, ctx->stream);
+  hipError_t e = lcsm::launch_prompt(k, ctx->s.dtype, ctx->scratch, ctx->stream);
   return e == hipSuccess ? LCSM_OK : ssm_fail(ctx, LCSM_EDEVICE, "prompt launch", e);
 }
 

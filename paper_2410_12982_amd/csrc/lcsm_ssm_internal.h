@@ -39,6 +39,7 @@ __device__ __forceinline__ void ssm_rows(const SsmCall& c, int i, int& t0, int& 
 // ---- prompts in chunks (lcsm_ssm_prompt.h)
 
 constexpr int kSsmQ = 64;  // positions of a chunk
+constexpr size_t kSsmMaxStride = (size_t)1 << 25;  // elements between rows: 25 rows of fp32 stay below 2^32 bytes
 
 // bf16 parts of a value in products that end in fp32 (states, fp32 outputs), and
 // in those whose sum is rounded to 16 bits.
@@ -71,6 +72,8 @@ inline int ssm_waves(int N) { return N <= 128 ? 8 : 4; }
 
 struct SsmScratch {
   char* bc;       // [blocks][G] SsmBlock
+  float* scal;    // [blocks][H][4][64]: what a chunk's positions have of a head
+  double* lq;     // [blocks][H]: log2 of a chunk's decay
   float* states;  // [segments][H][P][N]: what a segment adds to the state after it
   float* decay;   // [segments][H]: and what it leaves of the one before it
   int blocks, segments;  // upper bounds of the call's chunks and segments

@@ -128,7 +128,38 @@ __device__ __forceinline__ E ssm_row(const SsmCall& c, int r, int t0, int s, int
   return static_cast<const E*>(c.window)[((size_t)s * (c.W - 1) + (r - t0 + c.W - 1)) * c.C + ch];
 }
 
-// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock).
+// What a chunk's positions have of a head, a position a lane: w, then E where
+// the chunk is `fast`, else step and l in two parts.
+__device__ __forceinline__ bool ssm_fast(double lq) { return lq > -64.0 && lq < 64.0; }
+
+template <class E>
+__device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h) {
+  const int lane = (int)threadIdx.x & 63;
+  float step = 0.f;
+  if (lane < rows)
+    step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + c.dt_bias[h]);
+  // fp64: l reaches thousands where steps are long, and its differences count
+  double l = (double)(step * c.A[h]) * 1.4426950408889634;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const double v = __shfl_up(l, m);
+    if (lane >= m) l += v;
+  }
+  const double lq = __shfl(l, 63);
+  const size_t at = (size_t)block * c.H + h;
+  float* to = w.scal + at * 4 * kSsmQ + lane;
+  to[0] = step * exp2_hw((float)(lq - l));
+  const float hi = (float)l;
+  to[kSsmQ] = ssm_fast(lq) ? exp2_hw((float)(l - lq)) : step;
+  to[2 * kSsmQ] = hi;
+  to[3 * kSsmQ] = (float)(l - (double)hi);
+  if (lane == 0) w.lq[at] = lq;
+}
+
+// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); the
+// workgroups past the groups take the decays of kSsmDecayHeads heads each.
+constexpr int kSsmDecayHeads = 16;
+
 template <class E, int NT>
 __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
@@ -142,6 +173,11 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   ssm_rows(c, seq, t0, t1);
   const int s = ssm_slot(c.src, seq, c.slots), g = (int)blockIdx.y, r0 = t0 + num * kSsmQ;
   const int tid = (int)threadIdx.x, rows = min(kSsmQ, t1 - r0);
+  if (g >= c.G) {
+    const int h0 = (g - c.G) * kSsmDecayHeads, h1 = min(h0 + kSsmDecayHeads, c.H);
+    for (int h = h0 + tid / 64; h < h1; h += 4) ssm_decays<E>(c, w, (int)blockIdx.x, r0, rows, h);
+    return;
+  }
   // a thread convolves one channel along a quarter of the chunk's rows
   constexpr int RUN = kSsmQ / 4;
   for (int k = tid; k < 2 * NP * 4; k += 256) {
@@ -224,55 +260,80 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   }
 }
 
-// Two neighbouring channels of a row as they come.
+// Two neighbouring channels as they come.
 template <class E>
-struct Pair {
+struct Two {
   unsigned v;
-  __device__ float lo() const {
-    const E e = __builtin_bit_cast(E, (unsigned short)v);
-    return (float)e;
-  }
-  __device__ float hi() const {
-    const E e = __builtin_bit_cast(E, (unsigned short)(v >> 16));
-    return (float)e;
-  }
-  __device__ void set(E a, E b) {
-    v = __builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+  __device__ float lo() const { return (float)__builtin_bit_cast(E, (unsigned short)v); }
+  __device__ float hi() const { return (float)__builtin_bit_cast(E, (unsigned short)(v >> 16)); }
+  __device__ void set(float a, float b) {
+    v = __builtin_bit_cast(unsigned short, (E)a) | (unsigned)__builtin_bit_cast(unsigned short, (E)b) << 16;
   }
 };
 template <>
-struct Pair<float> {
-  float a, b;
-  __device__ float lo() const { return a; }
-  __device__ float hi() const { return b; }
+struct Two<float> {
+  unsigned a, b;
+  __device__ float lo() const { return __builtin_bit_cast(float, a); }
+  __device__ float hi() const { return __builtin_bit_cast(float, b); }
   __device__ void set(float x, float y) {
-    a = x;
-    b = y;
+    a = __builtin_bit_cast(unsigned, x);
+    b = __builtin_bit_cast(unsigned, y);
   }
 };
 
-// p[0], p[1] where there are `have` (0 .. 2) of them; `pair`: as one load.
+// Rows as a buffer of whole rows from a base row on: what lies past its end
+// reads as zero and is not stored.  `rows` of them, `width` elements in the
+// last; kSsmMaxStride keeps offsets of 25 rows below 2^32.
 template <class E>
-__device__ __forceinline__ Pair<E> load_pair(const E* p, int have, bool pair) {
-  Pair<E> v;
-  if (pair) {
-    struct alignas(2 * sizeof(E)) Two {
-      E e[2];
-    };
-    v.set((E)0.f, (E)0.f);
-    if (have == 2) {
-      const Two t = *reinterpret_cast<const Two*>(p);
-      v.set(t.e[0], t.e[1]);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size_t row, size_t stride, int rows,
+                                                             int width) {
+  const unsigned bytes = rows > 0 ? (unsigned)((rows - 1) * stride + width) * (unsigned)sizeof(E) : 0u;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(static_cast<const E*>(p) + row * stride), 0, (int)bytes,
+                                           0x00027000);
+}
+template <class E, bool PAIR>
+__device__ __forceinline__ Two<E> load_two(__amdgpu_buffer_rsrc_t r, unsigned at) {
+  Two<E> t;
+  if constexpr (sizeof(E) == 4) {
+    if constexpr (PAIR) {
+      const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
+      t.a = v[0];
+      t.b = v[1];
+    } else {
+      t.a = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+      t.b = __builtin_amdgcn_raw_buffer_load_b32(r, at + 4, 0, 0);
     }
+  } else if constexpr (PAIR) {
+    t.v = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
   } else {
-    v.set(have > 0 ? p[0] : (E)0.f, have > 1 ? p[1] : (E)0.f);
+    const unsigned a = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+    const unsigned b = __builtin_amdgcn_raw_buffer_load_b16(r, at + 2, 0, 0);
+    t.v = a | b << 16;
   }
-  return v;
+  return t;
+}
+// `second`: where the second channel goes by itself.
+template <class E, bool PAIR>
+__device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, unsigned at, unsigned second) {
+  if constexpr (sizeof(E) == 4) {
+    if constexpr (PAIR) {
+      typedef unsigned v2u __attribute__((ext_vector_type(2)));
+      __builtin_amdgcn_raw_buffer_store_b64((v2u){t.a, t.b}, r, at, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b32(t.a, r, at, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(t.b, r, second, 0, 0);
+    }
+  } else if constexpr (PAIR) {
+    __builtin_amdgcn_raw_buffer_store_b32(t.v, r, at, 0, 0);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)t.v, r, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(t.v >> 16), r, second, 0, 0);
+  }
 }
 
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
-template <class E, int NT, bool OUT>
+template <class E, int NT, bool OUT, bool PAIR>
 __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
   typedef SsmBlock<NT, PY> Blk;
@@ -322,9 +383,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
     for (int j = 0; j < 4; ++j) tap[e][j] = 3 - j < c.W ? c.conv_w[(size_t)cc * c.W + c.W - 4 + j] : 0.f;
   }
-  const float A = c.A[h], skip = c.skip[h], dtb = c.dt_bias[h];
-  const E* xp = static_cast<const E*>(c.xbc) + ch;
-  const E* zp = static_cast<const E*>(c.z) + ch;
+  const float skip = c.skip[h];
 
   v4f S[NA][2];  // n = 16 a + 4 q + i, channel p + e
   auto state_at = [&](float* base, int a, int e) { return base + (size_t)(p + e) * c.N + 16 * a + 4 * q; };
@@ -381,88 +440,90 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     }
   }
 
+  constexpr unsigned ES = sizeof(E), kNowhere = 0xC0000000u;  // past every row_buffer
+  const unsigned xs = (unsigned)c.xbc_stride * ES, xq = 4 * q * xs + (unsigned)ch * ES;
+  const unsigned zs = (unsigned)c.z_stride * ES, zq = 4 * q * zs + (unsigned)ch * ES;
+  const unsigned ys = (unsigned)c.y_stride * ES, yq = live && have > 0 ? 4 * q * ys + (unsigned)ch * ES : kNowhere;
+  const unsigned yq2 = live && have > 1 ? yq + ES : kNowhere;
+  // rows 16 m + 4 q - 3 .. + 3 of chunk k, zeros before the sequence and past it
+  Two<E> raw[4][7];
+  auto load_rows = [&](int k) {
+    const int r0 = t0 + k * kSsmQ;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int up = k == 0 && m == 0 ? 0 : 3;  // rows between the base and row 16 m
+      const int base = r0 + 16 * m - up;
+      const auto r = row_buffer<E>(c.xbc, base, c.xbc_stride, min(t1 - base, 22), c.C);
+#pragma unroll
+      for (int j = 0; j < 7; ++j) raw[m][j] = load_two<E, PAIR>(r, xq + (unsigned)(j - 3 + up) * xs);
+    }
+  };
+  constexpr bool AHEAD = sizeof(E) == 2;  // the next chunk's rows are loaded under this one's products
+  if (AHEAD && k0 < k1) load_rows(k0);
+
   double total = 0.0;  // log2 of the segment's decay
   for (int k = k0; k < k1; ++k) {
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
-    const char* from = w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES;
-    auto fetch = [&](int at, int to, int bytes) {
-      for (int i = wv * 1024; i < bytes; i += nw * 1024)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + at + i + lane * 16),
-                                         (__attribute__((address_space(3))) void*)(lds + to + i), 16, 0, 0);
+    const size_t block = (size_t)(block0 + k);
+    const char* from = w.bc + (block * c.G + g) * Blk::BYTES;
+    auto fetch = [&](const void* src, int to) {
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + lane * 16),
+          (__attribute__((address_space(3))) void*)(lds + to), 16, 0, 0);
+    };
+    auto fetch_part = [&](int at, int to, int bytes) {
+      for (int i = wv * 1024; i < bytes; i += nw * 1024) fetch(from + at + i, to + i);
     };
     auto fetch_stage = [&](int stage) {
       const int skip = OUT ? 0 : PY * Blk::PART;
-      fetch(stage * Blk::STAGE + skip, skip, Blk::STAGE - skip);
-      if (OUT && stage == Blk::STAGES - 1) fetch(Blk::G, Blk::STAGE, Blk::GBYTES);
+      fetch_part(stage * Blk::STAGE + skip, skip, Blk::STAGE - skip);
+      if (OUT && stage == Blk::STAGES - 1) fetch_part(Blk::G, Blk::STAGE, Blk::GBYTES);
     };
+    if (!AHEAD) load_rows(k);
     __syncthreads();  // the last chunk's operands have been read
+    fetch(w.scal + (block * c.H + h) * 4 * kSsmQ, Blk::LDS + wv * 4 * kSsmQ * (int)sizeof(float));
     fetch_stage(0);
+    const double lq = w.lq[block * c.H + h];
+    total += lq;
+    const bool fast = ssm_fast(lq);
+    const float dq = exp2_hw((float)lq);
 
-    // steps and decays, a position a lane
-    bool fast;
-    float dq;
-    {
-      float step = 0.f;
-      if (lane < rows)
-        step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + dtb);
-      double a = (double)(step * A) * 1.4426950408889634;
+    // x convolved: positions 16 m + 4 q + i, zeros past the sequence
+    if (k == 0 && src >= 0 && q == 0) {
 #pragma unroll
-      for (int m = 1; m < 64; m *= 2) {
-        const double v = __shfl_up(a, m);
-        if (lane >= m) a += v;
-      }
-      const double aq = __shfl(a, 63);
-      total += aq;
-      const float lq = (float)aq;
-      dq = exp2_hw(lq);
-      fast = lq > -64.f && lq < 64.f;
-      pw[lane] = step * exp2_hw((float)(aq - a));
-      if (OUT) {
-        if (fast) {
-          pe[lane] = exp2_hw((float)(a - aq));
-        } else {
-          const float lh = (float)a;
-          pe[lane] = step;
-          plh[lane] = lh;
-          pll[lane] = (float)(a - (double)lh);
+      for (int j = 0; j < 3; ++j)
+        if (3 - j < c.W) {
+          const E* at = static_cast<const E*>(c.window) + ((size_t)src * (c.W - 1) + (j - 3 + c.W - 1)) * c.C + ch;
+          raw[0][j].set(have > 0 ? (float)at[0] : 0.f, have > 1 ? (float)at[1] : 0.f);
         }
-      }
-      __builtin_amdgcn_wave_barrier();
     }
-
-    // x convolved: positions 16 m + 4 q + i, as slots of two blocks of 32
     float u[4][4][2];
+    auto convolve = [&](auto full) {
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int tm = 16 * m + 4 * q;
-      Pair<E> raw[7];
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-      for (int j = 0; j < 7; ++j) {
-        const int r = r0 + tm - 3 + j;
-        if (j >= 3 || 3 - j < c.W) {
-          if (r >= t0 || r - t0 < -(c.W - 1)) {
-            raw[j] = load_pair<E>(xp + (size_t)max(min(r, t1 - 1), t0) * c.xbc_stride,
-                                  tm - 3 + j < rows && r >= t0 ? have : 0, w.pair);
-          } else {
-            raw[j].set(have > 0 ? ssm_row<E>(c, r, t0, src, ch) : (E)0.f,
-                       have > 1 ? ssm_row<E>(c, r, t0, src, ch + 1) : (E)0.f);
-          }
-        } else {
-          raw[j].set((E)0.f, (E)0.f);
+        for (int i = 0; i < 4; ++i) {
+          float a = bias[0], b = bias[1];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (decltype(full)::value || 3 - j < c.W) {
+              a = fmaf(tap[0][j], raw[m][i + j].lo(), a);
+              b = fmaf(tap[1][j], raw[m][i + j].hi(), b);
+            }
+          u[m][i][0] = silu_hw(a);
+          u[m][i][1] = silu_hw(b);
         }
-      }
+    };
+    if (c.W == 4)
+      convolve(std::true_type{});
+    else
+      convolve(std::false_type{});
+    if (rows < kSsmQ) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a = bias[0], b = bias[1];
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (3 - j < c.W) {
-            a = fmaf(tap[0][j], raw[i + j].lo(), a);
-            b = fmaf(tap[1][j], raw[i + j].hi(), b);
-          }
-        u[m][i][0] = tm + i < rows ? silu_hw(a) : 0.f;
-        u[m][i][1] = tm + i < rows ? silu_hw(b) : 0.f;
-      }
+        for (int i = 0; i < 4; ++i)
+          if (16 * m + 4 * q + i >= rows) u[m][i][0] = u[m][i][1] = 0.f;
     }
     // u by a factor for every position, as the right operand of position block b
     auto operand = [&](const float* by, int b, int e, auto& to) {
@@ -487,7 +548,6 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
       for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
     int bad[2] = {kSsmQ, kSsmQ};
-    const float before = fast ? dq : 1.f, after = fast ? 1.f : dq;
 #pragma unroll
     for (int stage = 0; stage < Blk::STAGES; ++stage) {
       if (stage > 0) {
@@ -496,7 +556,14 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();  // the operands are in LDS
+      if (AHEAD && stage == 0 && k + 1 < k1) load_rows(k + 1);
       if (OUT) {
+        if (fast) {
+#pragma unroll
+          for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) S[a][e] *= dq;
+        }
 #pragma unroll
         for (int cc = stage * NB; cc < (stage + 1) * NB; ++cc) {
           v8bf sp[2][PY];
@@ -505,8 +572,8 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             float v[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              v[i] = S[2 * cc][e][i] *= before;
-              v[4 + i] = S[2 * cc + 1][e][i] *= before;
+              v[i] = S[2 * cc][e][i];
+              v[4 + i] = S[2 * cc + 1][e][i];
             }
             split(v, sp[e]);
           }
@@ -531,10 +598,12 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             }
         }
       }
+      if (!OUT || !fast) {
 #pragma unroll
-      for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
+        for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) S[a][e] *= OUT ? after : dq;
+          for (int e = 0; e < 2; ++e) S[a][e] *= dq;
+      }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         v8bf xp[2][PS];  // w o x
@@ -610,37 +679,41 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int e = 0; e < 2; ++e) {
         bad[e] = min(bad[e], __shfl_xor(bad[e], 16));
         bad[e] = min(bad[e], __shfl_xor(bad[e], 32));
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * m + 4 * q + i >= bad[e]) y[m][e][i] = __builtin_nanf("");
+      }
+    }
+    if (fast) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const v4f f = *reinterpret_cast<const v4f*>(pe + 16 * m + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) y[m][e] *= f;
       }
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      v4f E4 = {1.f, 1.f, 1.f, 1.f};
-      if (fast) E4 = *reinterpret_cast<const v4f*>(pe + 16 * m + 4 * q);
+      const int left = min(rows - 16 * m, 16);
+      const auto rz = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, c.z ? left : 0, c.D);
+      const auto ry = row_buffer<E>(c.y, r0 + 16 * m, c.y_stride, left, c.D);
+      Two<E> z[4];
+      if (c.z) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = load_two<E, PAIR>(rz, zq + i * zs);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int t = 16 * m + 4 * q + i;
-        if (t >= rows || have == 0 || !live) continue;
-        float v[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          v[e] = fmaf(skip, u[m][i][e], y[m][e][i] * E4[i]);
-          if (t >= bad[e]) v[e] = __builtin_nanf("");
-        }
+        float v0 = fmaf(skip, u[m][i][0], y[m][0][i]), v1 = fmaf(skip, u[m][i][1], y[m][1][i]);
         if (c.z) {
-          const Pair<E> z = load_pair<E>(zp + (size_t)(r0 + t) * c.z_stride, have, w.pair);
-          v[0] *= silu_hw(z.lo());
-          v[1] *= silu_hw(z.hi());
+          v0 *= silu_hw(z[i].lo());
+          v1 *= silu_hw(z[i].hi());
         }
-        E* to = static_cast<E*>(c.y) + (size_t)(r0 + t) * c.y_stride + ch;
-        if (w.pair) {
-          struct alignas(2 * sizeof(E)) Two {
-            E e[2];
-          };
-          *reinterpret_cast<Two*>(to) = Two{{(E)v[0], (E)v[1]}};
-        } else {
-          to[0] = (E)v[0];
-          if (have > 1) to[1] = (E)v[1];
-        }
+        Two<E> out;
+        out.set(v0, v1);
+        store_two<E, PAIR>(out, ry, yq + i * ys, yq2 + i * ys);
       }
     }
   }
@@ -659,11 +732,11 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   const int nw = items < ssm_waves(c.N) ? items : ssm_waves(c.N);
   const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)), (unsigned)w.segments);
   const size_t lds = SsmBlock<NT, ssm_out_parts(sizeof(E))>::LDS + (size_t)nw * 4 * kSsmQ * sizeof(float);
-  auto out = k_ssm_chunks<E, NT, true>;
-  auto sum = k_ssm_chunks<E, NT, false>;
+  auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
+  auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
   hipError_t e = hipSuccess;
   if (w.blocks) {
-    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)c.G), dim3(256), 0, st, c, w);
+    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + (c.H + kSsmDecayHeads - 1) / kSsmDecayHeads)), dim3(256), 0, st, c, w);
     e = hipGetLastError();
   }
   for (const void* f : {reinterpret_cast<const void*>(out), reinterpret_cast<const void*>(sum)})
