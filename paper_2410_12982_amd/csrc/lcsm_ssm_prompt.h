@@ -281,6 +281,15 @@ struct Two<float> {
   }
 };
 
+// A buffer that is the same for all lanes (which the compiler does not always
+// see, and then loops over the lanes' values at every access).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_buffer(const void* p, unsigned bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)at), hi = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0,
+                                           __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
+}
+
 // Rows as a buffer of whole rows from a base row on: what lies past its end
 // reads as zero and is not stored.  `rows` of them, `width` elements in the
 // last; kSsmMaxStride keeps offsets of 25 rows below 2^32.
@@ -288,8 +297,7 @@ template <class E>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size_t row, size_t stride, int rows,
                                                              int width) {
   const unsigned bytes = rows > 0 ? (unsigned)((rows - 1) * stride + width) * (unsigned)sizeof(E) : 0u;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(static_cast<const E*>(p) + row * stride), 0, (int)bytes,
-                                           0x00027000);
+  return uniform_buffer(static_cast<const E*>(p) + row * stride, bytes);
 }
 template <class E, bool PAIR>
 __device__ __forceinline__ Two<E> load_two(__amdgpu_buffer_rsrc_t r, unsigned at) {
@@ -348,7 +356,10 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   if (!OUT && last) return;
   int t0, t1;
   ssm_rows(c, seq, t0, t1);
-  const int src = ssm_slot(c.src, seq, c.slots), dst = ssm_slot(c.dst, seq, c.slots);
+  t0 = __builtin_amdgcn_readfirstlane(t0);
+  t1 = __builtin_amdgcn_readfirstlane(t1);
+  const int src = __builtin_amdgcn_readfirstlane(ssm_slot(c.src, seq, c.slots));
+  const int dst = __builtin_amdgcn_readfirstlane(ssm_slot(c.dst, seq, c.slots));
   // the first block of this sequence, counted as k_ssm_bc does
   int block0 = 0;
   for (int i = lane; i < seq; i += 64) {
@@ -358,6 +369,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) block0 += __shfl_xor(block0, m);
+  block0 = __builtin_amdgcn_readfirstlane(block0);
   // (offsets that do not rise could count more blocks than there are)
   const int k0 = num * w.per, k1 = min(min(k0 + w.per, chunks), w.blocks - block0);
 
@@ -385,35 +397,39 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   }
   const float skip = c.skip[h];
 
+  constexpr unsigned kNowhere = 0xC0000000u;  // past every buffer here
   v4f S[NA][2];  // n = 16 a + 4 q + i, channel p + e
-  auto state_at = [&](float* base, int a, int e) { return base + (size_t)(p + e) * c.N + 16 * a + 4 * q; };
-  auto get_state = [&](const float* base, int a, int e) {
-    v4f v = {0.f, 0.f, 0.f, 0.f};
-    if (e >= have) return v;
-    const float* at = base + (size_t)(p + e) * c.N + 16 * a + 4 * q;
-    if (w.quads) {
-      if (16 * a + 4 * q < c.N) v = *reinterpret_cast<const v4f*>(at);
-    } else {
+  // a head's states as a buffer; quads: four states are aligned as one
+  const unsigned sq = ((unsigned)p * c.N + 4 * q) * 4;
+  auto state_buffer = [&](const float* head) {
+    return uniform_buffer(head, (unsigned)c.P * c.N * 4);
+  };
+  auto state_at = [&](int a, int e, int i) {
+    return e < have && 16 * a + 4 * q + i < c.N ? sq + (unsigned)(e * c.N + 16 * a + i) * 4 : kNowhere;
+  };
+  auto get_state = [&](__amdgpu_buffer_rsrc_t r, int a, int e) {
+    if (w.quads) return __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, state_at(a, e, 0), 0, 0));
+    v4f v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (16 * a + 4 * q + i < c.N) v[i] = at[i];
-    }
+    for (int i = 0; i < 4; ++i)
+      v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, state_at(a, e, i), 0, 0));
     return v;
   };
-  auto put_state = [&](float* base) {
+  auto put_state = [&](float* head) {
     if (!live) return;
+    const auto r = state_buffer(head);
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        if (e >= have) continue;
-        float* at = state_at(base, a, e);
         if (w.quads) {
-          if (16 * a + 4 * q < c.N) *reinterpret_cast<v4f*>(at) = S[a][e];
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, S[a][e]), r, state_at(a, e, 0), 0, 0);
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (16 * a + 4 * q + i < c.N) at[i] = S[a][e][i];
+          for (int i = 0; i < 4; ++i) {
+            const float v = S[a][e][i];  // (a bit cast of the element itself takes the first one)
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), r, state_at(a, e, i), 0, 0);
+          }
         }
       }
   };
@@ -421,26 +437,43 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
   for (int a = 0; a < NA; ++a)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
-      if (OUT && src >= 0) S[a][e] = get_state(c.state + ((size_t)src * c.H + h) * per_head, a, e);
+    for (int e = 0; e < 2; ++e) S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
+  // Of a sequence in several segments the last one may be done before another has
+  // begun, and dst may be src: the state before it is kept where the last
+  // segment's contribution would be, which nobody needs.
+  const int segments = (chunks + w.per - 1) / w.per;
+  float* kept = w.states + ((size_t)min((int)blockIdx.y - num + segments - 1, w.segments - 1) * c.H + h) * per_head;
+  if (src >= 0 && (OUT || num == 0)) {
+    const auto r = state_buffer(OUT && segments > 1 ? kept : c.state + ((size_t)src * c.H + h) * per_head);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) S[a][e] = get_state(r, a, e);
+    if (!OUT) {
+      put_state(kept);
+#pragma unroll
+      for (int a = 0; a < NA; ++a)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
     }
+  }
   if (OUT) {
     for (int k = 0; k < num; ++k) {
       const size_t sg = (size_t)(blockIdx.y - num + k) * c.H + h;
       const float f = w.decay[sg];
+      const auto r = state_buffer(w.states + sg * per_head);
 #pragma unroll
       for (int a = 0; a < NA; ++a)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const v4f v = get_state(w.states + sg * per_head, a, e);
+          const v4f v = get_state(r, a, e);
 #pragma unroll
           for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], f, v[i]);
         }
     }
   }
 
-  constexpr unsigned ES = sizeof(E), kNowhere = 0xC0000000u;  // past every row_buffer
+  constexpr unsigned ES = sizeof(E);
   const unsigned xs = (unsigned)c.xbc_stride * ES, xq = 4 * q * xs + (unsigned)ch * ES;
   const unsigned zs = (unsigned)c.z_stride * ES, zq = 4 * q * zs + (unsigned)ch * ES;
   const unsigned ys = (unsigned)c.y_stride * ES, yq = live && have > 0 ? 4 * q * ys + (unsigned)ch * ES : kNowhere;
@@ -498,26 +531,25 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         }
     }
     float u[4][4][2];
-    auto convolve = [&](auto full) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[m][i][0] = bias[0], u[m][i][1] = bias[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (3 - j >= c.W) continue;  // a tap that is not there multiplies nothing, were it inf
 #pragma unroll
       for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float a = bias[0], b = bias[1];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (decltype(full)::value || 3 - j < c.W) {
-              a = fmaf(tap[0][j], raw[m][i + j].lo(), a);
-              b = fmaf(tap[1][j], raw[m][i + j].hi(), b);
-            }
-          u[m][i][0] = silu_hw(a);
-          u[m][i][1] = silu_hw(b);
+          u[m][i][0] = fmaf(tap[0][j], raw[m][i + j].lo(), u[m][i][0]);
+          u[m][i][1] = fmaf(tap[1][j], raw[m][i + j].hi(), u[m][i][1]);
         }
-    };
-    if (c.W == 4)
-      convolve(std::true_type{});
-    else
-      convolve(std::false_type{});
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[m][i][0] = silu_hw(u[m][i][0]), u[m][i][1] = silu_hw(u[m][i][1]);
     if (rows < kSsmQ) {
 #pragma unroll
       for (int m = 0; m < 4; ++m)
@@ -695,25 +727,34 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       }
     }
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int left = min(rows - 16 * m, 16);
-      const auto rz = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, c.z ? left : 0, c.D);
-      const auto ry = row_buffer<E>(c.y, r0 + 16 * m, c.y_stride, left, c.D);
-      Two<E> z[4];
-      if (c.z) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = load_two<E, PAIR>(rz, zq + i * zs);
-      }
+    for (int m = 0; m < 4; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float v0 = fmaf(skip, u[m][i][0], y[m][0][i]), v1 = fmaf(skip, u[m][i][1], y[m][1][i]);
-        if (c.z) {
-          v0 *= silu_hw(z[i].lo());
-          v1 *= silu_hw(z[i].hi());
+        y[m][0][i] = fmaf(skip, u[m][i][0], y[m][0][i]);
+        y[m][1][i] = fmaf(skip, u[m][i][1], y[m][1][i]);
+      }
+    if (c.z) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const auto r = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, min(rows - 16 * m, 16), c.D);
+        Two<E> z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = load_two<E, PAIR>(r, zq + i * zs);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[m][0][i] *= silu_hw(z[i].lo());
+          y[m][1][i] *= silu_hw(z[i].hi());
         }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const auto r = row_buffer<E>(c.y, r0 + 16 * m, c.y_stride, min(rows - 16 * m, 16), c.D);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         Two<E> out;
-        out.set(v0, v1);
-        store_two<E, PAIR>(out, ry, yq + i * ys, yq2 + i * ys);
+        out.set(y[m][0][i], y[m][1][i]);
+        store_two<E, PAIR>(out, r, yq + i * ys, yq2 + i * ys);
       }
     }
   }

@@ -172,6 +172,17 @@ def test_a_prompt_in_pieces_is_the_prompt():
         close(s[k], lay.state[0, 0], SUMS)
 
 
+@pytest.mark.parametrize("shape", [(1, 64, 64, 1, 4), (8, 64, 128, 1, 4), (40, 64, 16, 1, 4), (3, 20, 9, 3, 3)], ids=str)
+def test_long_prompts_continued_in_place(shape):
+    """Sequences long enough to be cut, each read from and written to its own
+    slot: whoever finishes first must not change what the others begin from."""
+    lay = Layer(*shape, slots=3, max_tokens=5000, seed=15, decay=1.1)
+    for lens in ([2000, 1, 300], [3000, 700, 0], [640, 64, 4100]):
+        offs = [0, lens[0], lens[0] + lens[1], sum(lens)]
+        x, xr = lay.inputs(offs[-1], gate=False)
+        lay.check(lay.ctx.prompt(0, x[0], x[1], offsets=ints(offs)), lay.want(xr, offs), str(lens))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_rows_of_one_wide_projection(dtype):
     """xbc, z and dt as slices of the rows of one projection (strides, starts
