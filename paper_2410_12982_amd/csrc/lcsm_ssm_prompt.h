@@ -339,6 +339,10 @@ __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, un
   }
 }
 
+// All waves past their LDS accesses; loads and stores of global memory stay on
+// their way, which __syncthreads would wait for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
 template <class E, int NT, bool OUT, bool PAIR>
@@ -438,39 +442,20 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   for (int a = 0; a < NA; ++a)
 #pragma unroll
     for (int e = 0; e < 2; ++e) S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
-  // Of a sequence in several segments the last one may be done before another has
-  // begun, and dst may be src: the state before it is kept where the last
-  // segment's contribution would be, which nobody needs.
-  const int segments = (chunks + w.per - 1) / w.per;
-  float* kept = w.states + ((size_t)min((int)blockIdx.y - num + segments - 1, w.segments - 1) * c.H + h) * per_head;
-  if (src >= 0 && (OUT || num == 0)) {
-    const auto r = state_buffer(OUT && segments > 1 ? kept : c.state + ((size_t)src * c.H + h) * per_head);
+  // A sequence in one segment begins from its slot.  Of one in several the last
+  // may be done, and dst may be src, before another has begun: k_ssm_join has put
+  // the state before each segment where the segment's contribution was.
+  const float* from_state = nullptr;
+  if (OUT && chunks > w.per)
+    from_state = w.states + ((size_t)blockIdx.y * c.H + h) * per_head;
+  else if (OUT && src >= 0)
+    from_state = c.state + ((size_t)src * c.H + h) * per_head;
+  if (from_state) {
+    const auto r = state_buffer(from_state);
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
       for (int e = 0; e < 2; ++e) S[a][e] = get_state(r, a, e);
-    if (!OUT) {
-      put_state(kept);
-#pragma unroll
-      for (int a = 0; a < NA; ++a)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) S[a][e] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-  }
-  if (OUT) {
-    for (int k = 0; k < num; ++k) {
-      const size_t sg = (size_t)(blockIdx.y - num + k) * c.H + h;
-      const float f = w.decay[sg];
-      const auto r = state_buffer(w.states + sg * per_head);
-#pragma unroll
-      for (int a = 0; a < NA; ++a)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const v4f v = get_state(r, a, e);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], f, v[i]);
-        }
-    }
   }
 
   constexpr unsigned ES = sizeof(E);
@@ -491,8 +476,6 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int j = 0; j < 7; ++j) raw[m][j] = load_two<E, PAIR>(r, xq + (unsigned)(j - 3 + up) * xs);
     }
   };
-  constexpr bool AHEAD = sizeof(E) == 2;  // the next chunk's rows are loaded under this one's products
-  if (AHEAD && k0 < k1) load_rows(k0);
 
   double total = 0.0;  // log2 of the segment's decay
   for (int k = k0; k < k1; ++k) {
@@ -512,8 +495,18 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       fetch_part(stage * Blk::STAGE + skip, skip, Blk::STAGE - skip);
       if (OUT && stage == Blk::STAGES - 1) fetch_part(Blk::G, Blk::STAGE, Blk::GBYTES);
     };
-    if (!AHEAD) load_rows(k);
-    __syncthreads();  // the last chunk's operands have been read
+    // rows first: they arrive while the operands are fetched, z by the end
+    load_rows(k);
+    Two<E> z[4][4];
+    if (OUT && c.z) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const auto r = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, min(rows - 16 * m, 16), c.D);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, zq + i * zs);
+      }
+    }
+    lds_barrier();  // the last chunk's operands have been read
     fetch(w.scal + (block * c.H + h) * 4 * kSsmQ, Blk::LDS + wv * 4 * kSsmQ * (int)sizeof(float));
     fetch_stage(0);
     const double lq = w.lq[block * c.H + h];
@@ -583,12 +576,11 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
     for (int stage = 0; stage < Blk::STAGES; ++stage) {
       if (stage > 0) {
-        __syncthreads();  // the stage before has been read
+        lds_barrier();  // the stage before has been read
         fetch_stage(stage);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();  // the operands are in LDS
-      if (AHEAD && stage == 0 && k + 1 < k1) load_rows(k + 1);
+      lds_barrier();  // the operands are in LDS
       if (OUT) {
         if (fast) {
 #pragma unroll
@@ -735,17 +727,12 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       }
     if (c.z) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const auto r = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, min(rows - 16 * m, 16), c.D);
-        Two<E> z[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = load_two<E, PAIR>(r, zq + i * zs);
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[m][0][i] *= silu_hw(z[i].lo());
-          y[m][1][i] *= silu_hw(z[i].hi());
+          y[m][0][i] *= silu_hw(z[m][i].lo());
+          y[m][1][i] *= silu_hw(z[m][i].hi());
         }
-      }
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -767,6 +754,54 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   }
 }
 
+// The states before the segments of a cut sequence, in place of the segments'
+// contributions: a thread per state of a head (grid: states, heads, sequences).
+constexpr int kSsmJoin = 8;  // contributions on their way
+
+inline __device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScratch& w) {
+  const int seq = (int)blockIdx.z, h = (int)blockIdx.y;
+  // the segments before this sequence's
+  int base = 0;
+  for (int i = (int)threadIdx.x & 63; i < seq; i += 64) {
+    int a, b;
+    ssm_rows(c, i, a, b);
+    base += max(((b - a + kSsmQ - 1) / kSsmQ + w.per - 1) / w.per, 1);
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) base += __shfl_xor(base, m);
+  base = __builtin_amdgcn_readfirstlane(base);
+  int t0, t1;
+  ssm_rows(c, seq, t0, t1);
+  const int segments = min(((t1 - t0 + kSsmQ - 1) / kSsmQ + w.per - 1) / w.per, w.segments - base);
+  if (segments < 2) return;
+  const int each = c.P * c.N, at = (int)blockIdx.x * 256 + (int)threadIdx.x;
+  if (at >= each) return;
+  const int src = ssm_slot(c.src, seq, c.slots);
+  float s = src >= 0 ? c.state[((size_t)src * c.H + h) * each + at] : 0.f;
+  const size_t step = (size_t)c.H * each;
+  float* p = w.states + ((size_t)base * c.H + h) * each + at;
+  const float* f = w.decay + (size_t)base * c.H + h;
+  for (int k = 0; k < segments; k += kSsmJoin) {
+    float v[kSsmJoin], d[kSsmJoin];
+#pragma unroll
+    for (int j = 0; j < kSsmJoin; ++j) {
+      const bool in = k + j < segments - 1;
+      v[j] = in ? p[(k + j) * step] : 0.f;
+      d[j] = in ? f[(size_t)(k + j) * c.H] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kSsmJoin; ++j) {
+      if (k + j >= segments) break;
+      p[(k + j) * step] = s;
+      s = fmaf(s, d[j], v[j]);
+    }
+  }
+}
+template <class E>  // one for each source that has this header
+__global__ __launch_bounds__(256) void k_ssm_join(SsmCall c, SsmScratch w) {
+  ssm_join(c, w);
+}
+
 template <class E, int NT>
 hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
   const int items = c.H / c.G * ((c.P + 31) / 32);
@@ -784,6 +819,8 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
     if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e == hipSuccess && w.segments > c.n) {
     hipLaunchKernelGGL(sum, grid, dim3(64 * nw), lds, st, c, w);
+    hipLaunchKernelGGL(k_ssm_join<E>, dim3((unsigned)((c.P * c.N + 255) / 256), (unsigned)c.H, (unsigned)c.n), dim3(256), 0,
+                       st, c, w);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
