@@ -56,10 +56,25 @@ struct SsmBlock {
   static constexpr int NB = NT < 4 ? NT : 4, STAGES = NT / NB;
   static constexpr int PART = 4096 * NB, GPART = 6144;
   static constexpr int STAGE = (PY + kSsmParts) * PART, G = STAGES * STAGE, GBYTES = PY * GPART;
-  static constexpr int BYTES = G + GBYTES, LDS = STAGE + GBYTES;
+  static constexpr int BYTES = G + GBYTES;
   static constexpr int c_at(int tt, int cc) { return cc / NB * STAGE + (tt * NB + cc % NB) * 1024; }
   static constexpr int b_at(int a, int b) { return a / (2 * NB) * STAGE + PY * PART + (a % (2 * NB) * 2 + b) * 1024; }
   static constexpr int g_at(int f) { return G + f * 1024; }
+};
+
+// What a workgroup of `waves` keeps of a block in LDS: C and G (not where only
+// the states are wanted), then B, then what each wave's positions have of its
+// head.  AHEAD: the first of these (B where it is the only one) and the last
+// exist twice, so that the next chunk's are fetched while this one's are used.
+constexpr int kSsmLds = 163840;
+template <int NT, int PY, bool OUT>
+struct SsmLds {
+  typedef SsmBlock<NT, PY> Blk;
+  static constexpr int CG = OUT ? PY * Blk::PART + Blk::GBYTES : 0, BB = kSsmParts * Blk::PART;
+  static constexpr int SCAL = 4 * kSsmQ * (int)sizeof(float);
+  static constexpr bool AHEAD = Blk::STAGES == 1 && (OUT ? 2 * CG + BB : 2 * BB) + 16 * SCAL <= kSsmLds;
+  static constexpr int B = (AHEAD ? 2 : 1) * CG, B2 = AHEAD && !OUT ? BB : 0, WAVES = B + B2 + BB;
+  static constexpr int bytes(int waves) { return WAVES + (AHEAD ? 2 : 1) * waves * SCAL; }
 };
 inline int ssm_blocks_of(int N) { return N <= 32 ? 1 : N <= 64 ? 2 : N <= 128 ? 4 : 8; }
 inline size_t ssm_block_bytes(int N, size_t elem) {

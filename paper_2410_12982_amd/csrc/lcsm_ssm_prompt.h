@@ -47,14 +47,15 @@ typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
 // and 16 + 4q .. 16 + 4q+3 of the block's 32, which are the rows that it holds
 // of two 16x16 accumulators.
 //
-// a b with both in parts, the small products first.
-template <int P>
-__device__ __forceinline__ v4f mul(const v8bf (&a)[P], const v8bf (&b)[P], v4f c) {
+// c[e] += a b[e] with both in parts, the small products first.
+template <int P, int Q>
+__device__ __forceinline__ void mul(const v8bf (&a)[P], const v8bf (&b)[2][Q], v4f (&c)[2]) {
 #pragma unroll
   for (int sum = P - 1; sum >= 0; --sum)
 #pragma unroll
-    for (int i = 0; i <= sum; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[sum - i], c, 0, 0, 0);
-  return c;
+    for (int i = 0; i <= sum; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) c[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[e][sum - i], c[e], 0, 0, 0);
 }
 
 // Eight values as an operand's parts: each the bf16 nearest to what the parts
@@ -349,13 +350,19 @@ template <class E, int NT, bool OUT, bool PAIR>
 __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
   typedef SsmBlock<NT, PY> Blk;
-  constexpr int NA = 2 * NT, NB = Blk::NB;
+  typedef SsmLds<NT, PY, OUT> Lds;
+  constexpr int NA = 2 * NT, NB = Blk::NB, STAGES = Blk::STAGES;
   extern __shared__ __align__(16) char lds[];
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), nw = (int)blockDim.x >> 6;
+  // workgroups of one segment share its operands: every eighth one, as an XCD
+  // (and its L2) gets them
+  const int hg = c.H / c.G, parts = (c.P + 31) / 32, items = hg * parts;
+  const int wgs = (items + nw - 1) / nw, wgx = c.G * wgs;
+  const int wg = (int)blockIdx.x / 8 % wgx, segment = (int)blockIdx.x / (8 * wgx) * 8 + (int)blockIdx.x % 8;
+  if (segment >= w.segments) return;
   int seq, num, chunks;
-  if (!ssm_piece(c, (int)blockIdx.y, w.per, 1, seq, num, chunks)) return;
-  if ((int)blockIdx.y >= w.segments) return;
+  if (!ssm_piece(c, segment, w.per, 1, seq, num, chunks)) return;
   const bool last = (num + 1) * w.per >= chunks;
   if (!OUT && last) return;
   int t0, t1;
@@ -379,18 +386,12 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 
   // head and channels of this wave; a wave past the last one works on the last
   // one's data and stores nothing
-  const int hg = c.H / c.G, parts = (c.P + 31) / 32, items = hg * parts;
-  const int wgs = (items + nw - 1) / nw;
-  const int g = (int)blockIdx.x / wgs;
-  const int item = ((int)blockIdx.x % wgs) * nw + wv;
+  const int g = wg / wgs, item = wg % wgs * nw + wv;
   const bool live = item < items;
   const int it = live ? item : items - 1;
   const int h = g * hg + it / parts, p = (it % parts) * 32 + 2 * l;
   const int have = min(max(c.P - p, 0), 2);  // channels this lane has
   const int ch = h * c.P + p;                // x, z, y
-  float* priv = reinterpret_cast<float*>(lds + Blk::LDS) + wv * 4 * kSsmQ;
-  float *pw = priv, *pe = priv + kSsmQ, *plh = priv + 2 * kSsmQ, *pll = priv + 3 * kSsmQ;
-
   float tap[2][4], bias[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   // the state before each segment where the segment's contribution was.
   const float* from_state = nullptr;
   if (OUT && chunks > w.per)
-    from_state = w.states + ((size_t)blockIdx.y * c.H + h) * per_head;
+    from_state = w.states + ((size_t)segment * c.H + h) * per_head;
   else if (OUT && src >= 0)
     from_state = c.state + ((size_t)src * c.H + h) * per_head;
   if (from_state) {
@@ -477,24 +478,38 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     }
   };
 
+  auto fetch = [&](const void* src, int to) {
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + lane * 16),
+        (__attribute__((address_space(3))) void*)(lds + to), 16, 0, 0);
+  };
+  auto fetch_part = [&](const char* from, int to, int bytes) {
+    for (int i = wv * 1024; i < bytes; i += nw * 1024) fetch(from + i, to + i);
+  };
+  auto operands_of = [&](int k) { return w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES; };
+  auto scal_at = [&](int k) { return Lds::WAVES + ((Lds::AHEAD ? (k & 1) * nw : 0) + wv) * Lds::SCAL; };
+  auto fetch_scal = [&](int k) { fetch(w.scal + ((size_t)(block0 + k) * c.H + h) * 4 * kSsmQ, scal_at(k)); };
+  auto fetch_cg = [&](int k, int stage) {
+    const int to = Lds::AHEAD ? (k & 1) * Lds::CG : 0;
+    fetch_part(operands_of(k) + stage * Blk::STAGE, to, PY * Blk::PART);
+    if (stage == STAGES - 1) fetch_part(operands_of(k) + Blk::G, to + PY * Blk::PART, Blk::GBYTES);
+  };
+  auto fetch_b = [&](int k, int stage) {
+    fetch_part(operands_of(k) + stage * Blk::STAGE + PY * Blk::PART, Lds::B + (k & 1) * Lds::B2, Lds::BB);
+  };
+  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+  if (Lds::AHEAD && k0 < k1) {
+    if (OUT)
+      fetch_cg(k0, 0);
+    else
+      fetch_b(k0, 0);
+    fetch_scal(k0);
+    arrived();
+  }
+
   double total = 0.0;  // log2 of the segment's decay
   for (int k = k0; k < k1; ++k) {
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
-    const size_t block = (size_t)(block0 + k);
-    const char* from = w.bc + (block * c.G + g) * Blk::BYTES;
-    auto fetch = [&](const void* src, int to) {
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + lane * 16),
-          (__attribute__((address_space(3))) void*)(lds + to), 16, 0, 0);
-    };
-    auto fetch_part = [&](int at, int to, int bytes) {
-      for (int i = wv * 1024; i < bytes; i += nw * 1024) fetch(from + at + i, to + i);
-    };
-    auto fetch_stage = [&](int stage) {
-      const int skip = OUT ? 0 : PY * Blk::PART;
-      fetch_part(stage * Blk::STAGE + skip, skip, Blk::STAGE - skip);
-      if (OUT && stage == Blk::STAGES - 1) fetch_part(Blk::G, Blk::STAGE, Blk::GBYTES);
-    };
     // rows first: they arrive while the operands are fetched, z by the end
     load_rows(k);
     Two<E> z[4][4];
@@ -506,13 +521,27 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, zq + i * zs);
       }
     }
-    lds_barrier();  // the last chunk's operands have been read
-    fetch(w.scal + (block * c.H + h) * 4 * kSsmQ, Blk::LDS + wv * 4 * kSsmQ * (int)sizeof(float));
-    fetch_stage(0);
-    const double lq = w.lq[block * c.H + h];
+    lds_barrier();  // the last chunk's operands have been read (and this one's first ones are there)
+    if (!Lds::AHEAD) {
+      fetch_scal(k);
+      if (OUT) fetch_cg(k, 0);
+      fetch_b(k, 0);
+    } else {
+      if (OUT) fetch_b(k, 0);
+      if (k + 1 < k1) {
+        if (OUT)
+          fetch_cg(k + 1, 0);
+        else
+          fetch_b(k + 1, 0);
+        fetch_scal(k + 1);
+      }
+    }
+    const double lq = w.lq[(size_t)(block0 + k) * c.H + h];
     total += lq;
     const bool fast = ssm_fast(lq);
     const float dq = exp2_hw((float)lq);
+    const float* pw = reinterpret_cast<const float*>(lds + scal_at(k));
+    const float *pe = pw + kSsmQ, *plh = pw + 2 * kSsmQ, *pll = pw + 3 * kSsmQ;
 
     // x convolved: positions 16 m + 4 q + i, zeros past the sequence
     if (k == 0 && src >= 0 && q == 0) {
@@ -567,6 +596,8 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int k = 0; k < (int)(sizeof(to) / sizeof(to[0])); ++k)
         to[k] = *reinterpret_cast<const v8bf*>(lds + at + k * step + lane * 16);
     };
+    const int lds_c = OUT && Lds::AHEAD ? (k & 1) * Lds::CG : 0, lds_g = lds_c + PY * Blk::PART;
+    const int lds_b = Lds::B + (k & 1) * Lds::B2;
     v4f y[4][2];
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
@@ -574,13 +605,17 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
     int bad[2] = {kSsmQ, kSsmQ};
 #pragma unroll
-    for (int stage = 0; stage < Blk::STAGES; ++stage) {
+    for (int stage = 0; stage < STAGES; ++stage) {
+      constexpr int NF = 4 * NB;  // fragments of C, and of B for a block of positions twice as many states / 16
       if (stage > 0) {
         lds_barrier();  // the stage before has been read
-        fetch_stage(stage);
+        if (OUT) fetch_cg(k, stage);
+        fetch_b(k, stage);
       }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      lds_barrier();  // the operands are in LDS
+      if (!Lds::AHEAD) {
+        arrived();
+        lds_barrier();  // the operands are in LDS
+      }
       if (OUT) {
         if (fast) {
 #pragma unroll
@@ -588,28 +623,29 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
             for (int e = 0; e < 2; ++e) S[a][e] *= dq;
         }
+        // fragments are read one ahead of their products
+        v8bf cp[2][PY], sp[2][PY];
+        frag(lds_c, Blk::PART, cp[0]);
 #pragma unroll
-        for (int cc = stage * NB; cc < (stage + 1) * NB; ++cc) {
-          v8bf sp[2][PY];
+        for (int f = 0; f < NF; ++f) {
+          const int cc = stage * NB + f / 4, tt = f % 4;
+          if (f + 1 < NF) frag(lds_c + ((f + 1) % 4 * NB + (f + 1) / 4) * 1024, Blk::PART, cp[(f + 1) & 1]);
+          if (tt == 0) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v[8];
+            for (int e = 0; e < 2; ++e) {
+              float v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              v[i] = S[2 * cc][e][i];
-              v[4 + i] = S[2 * cc + 1][e][i];
+              for (int i = 0; i < 4; ++i) {
+                v[i] = S[2 * cc][e][i];
+                v[4 + i] = S[2 * cc + 1][e][i];
+              }
+              split(v, sp[e]);
             }
-            split(v, sp[e]);
           }
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt) {
-            v8bf cp[PY];
-            frag(Blk::c_at(tt, cc) - stage * Blk::STAGE, Blk::PART, cp);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) y[tt][e] = mul(cp, sp[e], y[tt][e]);
-          }
+          __builtin_amdgcn_sched_barrier(0);
+          mul(cp[f & 1], sp, y[tt]);
         }
-        if (!fast && stage == Blk::STAGES - 1) {
+        if (!fast && stage == STAGES - 1) {
           // rows by 2^l_t; the products below have the elements' own decays
 #pragma unroll
           for (int tt = 0; tt < 4; ++tt)
@@ -621,6 +657,10 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
               for (int e = 0; e < 2; ++e) y[tt][e][i] *= f;
             }
         }
+        if (Lds::AHEAD) {
+          arrived();
+          lds_barrier();  // B is in LDS
+        }
       }
       if (!OUT || !fast) {
 #pragma unroll
@@ -630,17 +670,17 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        v8bf xp[2][PS];  // w o x
+        v8bf xp[2][PS], bp[2][PS];  // w o x; B
+        frag(lds_b + b * 1024, Blk::PART, bp[0]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) operand(pw, b, e, xp[e]);
 #pragma unroll
-        for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a) {
-          v8bf bp[PS];
-          frag(Blk::b_at(a, b) - stage * Blk::STAGE, Blk::PART, bp);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) S[a][e] = mul(bp, xp[e], S[a][e]);
+        for (int f = 0; f < 2 * NB; ++f) {
+          if (f + 1 < 2 * NB) frag(lds_b + (2 * f + 2 + b) * 1024, Blk::PART, bp[(f + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+          mul(bp[f & 1], xp, S[2 * stage * NB + f]);
         }
-        if (!OUT || stage != Blk::STAGES - 1) continue;
+        if (!OUT || stage != STAGES - 1) continue;
         v8bf yp[2][PY];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -671,12 +711,13 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             for (int k = 0; k < PY; ++k) yp[e][k] = __builtin_bit_cast(v8bf, part[k]);
           }
         }
+        // the blocks of G that have positions of b as columns: 0, 1, 2, 4 or 3, 5
+        v8bf gp[2][PY];
+        auto g_at = [&](int tt) { return lds_g + (tt < 2 ? tt : 2 * tt - 2 + b) * 1024; };
+        frag(g_at(2 * b), Blk::GPART, gp[0]);
 #pragma unroll
-        for (int f = 0; f < 6; ++f) {
-          const int tt = f < 2 ? f : 2 + (f - 2) / 2;
-          if ((f < 2 ? 0 : (f - 2) % 2) != b) continue;
-          v8bf gp[PY];
-          frag(Blk::STAGE + f * 1024, Blk::GPART, gp);
+        for (int tt = 2 * b; tt < 4; ++tt) {
+          if (tt < 3) frag(g_at(tt + 1), Blk::GPART, gp[(tt + 1) & 1]);
           if (!fast) {
             const int t = 16 * tt + l;
             const float lt = plh[t], rt = pll[t];
@@ -685,18 +726,18 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             for (int j = 0; j < 8; ++j) {
               const int s = 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
               const float d = exp2_hw((lt - plh[s]) + (rt - pll[s]));
-              float sum = (float)gp[PY - 1][j];
+              float sum = (float)gp[tt & 1][PY - 1][j];
 #pragma unroll
-              for (int k = PY - 2; k >= 0; --k) sum += (float)gp[k][j];
+              for (int k = PY - 2; k >= 0; --k) sum += (float)gp[tt & 1][k][j];
               v[j] = s <= t ? sum * d : 0.f;
             }
-            split(v, gp);
+            split(v, gp[tt & 1]);
           }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) y[tt][e] = mul(gp, yp[e], y[tt][e]);
+          mul(gp[tt & 1], yp, y[tt]);
         }
       }
     }
+    if (Lds::AHEAD) arrived();  // the next chunk's operands, before the stores
     if (!OUT) continue;
     if (__ballot(bad[0] < kSsmQ || bad[1] < kSsmQ)) {
 #pragma unroll
@@ -746,7 +787,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     }
   }
   if (!OUT) {
-    const size_t sg = (size_t)blockIdx.y * c.H + h;
+    const size_t sg = (size_t)segment * c.H + h;
     put_state(w.states + sg * per_head);
     if (live && lane == 0 && it % parts == 0) w.decay[sg] = (float)exp2(total);
   } else if (last && dst >= 0) {
@@ -806,8 +847,9 @@ template <class E, int NT>
 hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
   const int items = c.H / c.G * ((c.P + 31) / 32);
   const int nw = items < ssm_waves(c.N) ? items : ssm_waves(c.N);
-  const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)), (unsigned)w.segments);
-  const size_t lds = SsmBlock<NT, ssm_out_parts(sizeof(E))>::LDS + (size_t)nw * 4 * kSsmQ * sizeof(float);
+  const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)) * (((unsigned)w.segments + 7) / 8 * 8));
+  constexpr int PY = ssm_out_parts(sizeof(E));
+  const int lds_out = SsmLds<NT, PY, true>::bytes(nw), lds_sum = SsmLds<NT, PY, false>::bytes(nw);
   auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
   hipError_t e = hipSuccess;
@@ -815,16 +857,19 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
     hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + (c.H + kSsmDecayHeads - 1) / kSsmDecayHeads)), dim3(256), 0, st, c, w);
     e = hipGetLastError();
   }
-  for (const void* f : {reinterpret_cast<const void*>(out), reinterpret_cast<const void*>(sum)})
-    if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  auto allow = [&](const void* f, int bytes) {
+    if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  allow(reinterpret_cast<const void*>(out), lds_out);
+  if (w.segments > c.n) allow(reinterpret_cast<const void*>(sum), lds_sum);
   if (e == hipSuccess && w.segments > c.n) {
-    hipLaunchKernelGGL(sum, grid, dim3(64 * nw), lds, st, c, w);
+    hipLaunchKernelGGL(sum, grid, dim3(64 * nw), lds_sum, st, c, w);
     hipLaunchKernelGGL(k_ssm_join<E>, dim3((unsigned)((c.P * c.N + 255) / 256), (unsigned)c.H, (unsigned)c.n), dim3(256), 0,
                        st, c, w);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(out, grid, dim3(64 * nw), lds, st, c, w);
+  hipLaunchKernelGGL(out, grid, dim3(64 * nw), lds_out, st, c, w);
   return hipGetLastError();
 }
 
