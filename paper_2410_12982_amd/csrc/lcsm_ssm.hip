@@ -151,10 +151,10 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
   return hipGetLastError();
 }
 
-// How a prompt call is cut: segments of `per` chunks so that about
-// kSsmWorkgroups workgroups of the widest kind are on their way; sequences that
-// are that many by themselves are not cut.
-constexpr int kSsmWorkgroups = 512;
+// How a prompt call is cut: segments of `per` chunks so that about one
+// workgroup per compute unit is on its way, which is what LDS holds; sequences
+// that are that many by themselves are not cut.
+constexpr int kSsmWorkgroups = 256;
 
 int head_groups(int H, int G, int P, int N) {
   const int items = H / G * ((P + 31) / 32), nw = items < ssm_waves(N) ? items : ssm_waves(N);
@@ -246,7 +246,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
       return false;
     take(&p->bc, blocks * s->G * each);
     take(&p->scal, blocks * H * 4 * lcsm::kSsmQ * 4);
-    take(&p->lq, blocks * H * 8);
+    take(&p->lq, blocks * H * 16);
     take(&p->states, segments * (size_t)D * s->N * 4);
     take(&p->decay, segments * H * 4);
   }

@@ -53,7 +53,7 @@ inline constexpr int ssm_out_parts(size_t elem) { return elem == 4 ? kSsmParts :
 // of B).  C and B of NB state blocks at a time are what LDS holds (STAGE).
 template <int NT, int PY>
 struct SsmBlock {
-  static constexpr int NB = NT < 4 ? NT : 4, STAGES = NT / NB;
+  static constexpr int NB = NT < 2 ? NT : 2, STAGES = NT / NB;
   static constexpr int PART = 4096 * NB, GPART = 6144;
   static constexpr int STAGE = (PY + kSsmParts) * PART, G = STAGES * STAGE, GBYTES = PY * GPART;
   static constexpr int BYTES = G + GBYTES;
@@ -62,20 +62,18 @@ struct SsmBlock {
   static constexpr int g_at(int f) { return G + f * 1024; }
 };
 
-// What a workgroup of `waves` keeps of a block in LDS: C and G (not where only
-// the states are wanted), then B, then what each wave's positions have of its
-// head.  AHEAD: the first of these (B where it is the only one) and the last
-// exist twice, so that the next chunk's are fetched while this one's are used.
-constexpr int kSsmLds = 163840;
+// What a workgroup of `waves` keeps in LDS: two stages (C and B; B alone where
+// only the states are wanted), so that the next one is fetched while one is
+// used, G of the chunk, and twice what each wave's positions have of its head.
 template <int NT, int PY, bool OUT>
 struct SsmLds {
   typedef SsmBlock<NT, PY> Blk;
-  static constexpr int CG = OUT ? PY * Blk::PART + Blk::GBYTES : 0, BB = kSsmParts * Blk::PART;
+  static constexpr int C = OUT ? PY * Blk::PART : 0, STAGE = C + kSsmParts * Blk::PART;
+  static constexpr int G = 2 * STAGE, WAVES = G + (OUT ? Blk::GBYTES : 0);
   static constexpr int SCAL = 4 * kSsmQ * (int)sizeof(float);
-  static constexpr bool AHEAD = Blk::STAGES == 1 && (OUT ? 2 * CG + BB : 2 * BB) + 16 * SCAL <= kSsmLds;
-  static constexpr int B = (AHEAD ? 2 : 1) * CG, B2 = AHEAD && !OUT ? BB : 0, WAVES = B + B2 + BB;
-  static constexpr int bytes(int waves) { return WAVES + (AHEAD ? 2 : 1) * waves * SCAL; }
+  static constexpr int bytes(int waves) { return WAVES + 2 * waves * SCAL; }
 };
+
 inline int ssm_blocks_of(int N) { return N <= 32 ? 1 : N <= 64 ? 2 : N <= 128 ? 4 : 8; }
 inline size_t ssm_block_bytes(int N, size_t elem) {
   const int nt = ssm_blocks_of(N), py = ssm_out_parts(elem);
@@ -88,7 +86,7 @@ inline int ssm_waves(int N) { return N <= 128 ? 8 : 4; }
 struct SsmScratch {
   char* bc;       // [blocks][G] SsmBlock
   float* scal;    // [blocks][H][4][64]: what a chunk's positions have of a head
-  double* lq;     // [blocks][H]: log2 of a chunk's decay
+  double* lq;     // [blocks][H][2]: log2 of the decays of a chunk's halves
   float* states;  // [segments][H][P][N]: what a segment adds to the state after it
   float* decay;   // [segments][H]: and what it leaves of the one before it
   int blocks, segments;  // upper bounds of the call's chunks and segments

@@ -1,12 +1,15 @@
 // Prompts of the state space mixer in chunks of 64 positions on the matrix
 // units; included by one source per element type.
 //
-// Within a chunk let l_t be the sum of the steps' log2-decays up to t, w_s =
-// step_s 2^(l_Q - l_s) and E_t = 2^(l_t - l_Q) (Q the last position).  The
-// recurrence unrolled over the chunk is, per head,
+// Within a chunk let l_t be the sum of the steps' log2-decays up to t, e the last
+// position of t's half (32 positions) of the chunk, w_t = step_t 2^(l_e - l_t)
+// and E_t = 2^(l_t - l_e).  The recurrence unrolled over a half is, per head,
 //
-//   y_t  = E_t [ C (2^l_Q S)^T + tril(C B^T) (w o x) ]_t,
-//   S'   = 2^l_Q S + (w o x)^T B,
+//   y_t  = E_t [ C (2^l_e S)^T + tril(C B^T) (w o x) ]_t,
+//   S'   = 2^l_e S + (w o x)^T B,
+//
+// and over the chunk the same with the first half's share of the second one's
+// rows, and of S, multiplied by the second one's decay in between:
 //
 // three matrix products in which only w o x, S and the row factor E belong to
 // the head: B, C and tril(C B^T) are made once per chunk and group, by
@@ -17,8 +20,8 @@
 // operand of C S^T as it stands, and the lane that convolves x at a position
 // is the one that gets y there, so nothing of a head goes through LDS.
 //
-// E and w stay within 2^64 of each other while the chunk's decay does; where it
-// does not (steps that forget everything), the factor 2^(l_t - l_s) <= 1 is put
+// E and w stay within 2^64 of each other while the halves' decays do; where they
+// do not (steps that forget everything), the factor 2^(l_t - l_s) <= 1 is put
 // into the elements of tril(C B^T) one by one instead (`fast` false).
 //
 // Values go into the products as sums of bf16 parts, which hold fp32's range
@@ -131,7 +134,7 @@ __device__ __forceinline__ E ssm_row(const SsmCall& c, int r, int t0, int s, int
 
 // What a chunk's positions have of a head, a position a lane: w, then E where
 // the chunk is `fast`, else step and l in two parts.
-__device__ __forceinline__ bool ssm_fast(double lq) { return lq > -64.0 && lq < 64.0; }
+__device__ __forceinline__ bool ssm_fast(double l0, double l1) { return fabs(l0) < 64.0 && fabs(l1) < 64.0; }
 
 template <class E>
 __device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h) {
@@ -146,15 +149,15 @@ __device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w
     const double v = __shfl_up(l, m);
     if (lane >= m) l += v;
   }
-  const double lq = __shfl(l, 63);
+  const double l0 = __shfl(l, 31), lq = __shfl(l, 63), le = lane < 32 ? l0 : lq;
   const size_t at = (size_t)block * c.H + h;
   float* to = w.scal + at * 4 * kSsmQ + lane;
-  to[0] = step * exp2_hw((float)(lq - l));
+  to[0] = step * exp2_hw((float)(le - l));
   const float hi = (float)l;
-  to[kSsmQ] = ssm_fast(lq) ? exp2_hw((float)(l - lq)) : step;
+  to[kSsmQ] = ssm_fast(l0, lq - l0) ? exp2_hw((float)(l - le)) : step;
   to[2 * kSsmQ] = hi;
   to[3 * kSsmQ] = (float)(l - (double)hi);
-  if (lane == 0) w.lq[at] = lq;
+  if (lane < 2) w.lq[2 * at + lane] = lane ? lq - l0 : l0;
 }
 
 // B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); the
@@ -340,6 +343,13 @@ __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, un
   }
 }
 
+// v, with what is made of it made here: sums of it and of what is the same in
+// every turn of a loop are not kept in registers from one turn to the next.
+__device__ __forceinline__ unsigned here(unsigned v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // All waves past their LDS accesses; loads and stores of global memory stay on
 // their way, which __syncthreads would wait for.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -468,80 +478,63 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   Two<E> raw[4][7];
   auto load_rows = [&](int k) {
     const int r0 = t0 + k * kSsmQ;
+    const unsigned from = here(xq);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const int up = k == 0 && m == 0 ? 0 : 3;  // rows between the base and row 16 m
       const int base = r0 + 16 * m - up;
       const auto r = row_buffer<E>(c.xbc, base, c.xbc_stride, min(t1 - base, 22), c.C);
 #pragma unroll
-      for (int j = 0; j < 7; ++j) raw[m][j] = load_two<E, PAIR>(r, xq + (unsigned)(j - 3 + up) * xs);
+      for (int j = 0; j < 7; ++j) raw[m][j] = load_two<E, PAIR>(r, from + (unsigned)(j - 3 + up) * xs);
     }
   };
 
-  auto fetch = [&](const void* src, int to) {
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(static_cast<const char*>(src) + lane * 16),
-        (__attribute__((address_space(3))) void*)(lds + to), 16, 0, 0);
+  // the next chunk's rows are loaded under this one's products, where there are
+  // registers for them
+  constexpr bool AHEAD = sizeof(E) == 2 && (!OUT || NT < 4);
+  // 1024 bytes at `at` of a buffer into LDS, 16 a lane
+  auto fetch = [&](__amdgpu_buffer_rsrc_t r, int at, int to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + to), 16, lane * 16, at, 0, 0);
   };
-  auto fetch_part = [&](const char* from, int to, int bytes) {
-    for (int i = wv * 1024; i < bytes; i += nw * 1024) fetch(from + i, to + i);
+  auto fetch_part = [&](__amdgpu_buffer_rsrc_t r, int at, int to, int bytes) {
+    for (int i = wv * 1024; i < bytes; i += nw * 1024) fetch(r, at + i, to + i);
   };
-  auto operands_of = [&](int k) { return w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES; };
-  auto scal_at = [&](int k) { return Lds::WAVES + ((Lds::AHEAD ? (k & 1) * nw : 0) + wv) * Lds::SCAL; };
-  auto fetch_scal = [&](int k) { fetch(w.scal + ((size_t)(block0 + k) * c.H + h) * 4 * kSsmQ, scal_at(k)); };
-  auto fetch_cg = [&](int k, int stage) {
-    const int to = Lds::AHEAD ? (k & 1) * Lds::CG : 0;
-    fetch_part(operands_of(k) + stage * Blk::STAGE, to, PY * Blk::PART);
-    if (stage == STAGES - 1) fetch_part(operands_of(k) + Blk::G, to + PY * Blk::PART, Blk::GBYTES);
+  auto operands_of = [&](int k) {
+    return uniform_buffer(w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES, Blk::BYTES);
   };
-  auto fetch_b = [&](int k, int stage) {
-    fetch_part(operands_of(k) + stage * Blk::STAGE + PY * Blk::PART, Lds::B + (k & 1) * Lds::B2, Lds::BB);
+  auto stage_at = [&](int k, int stage) { return (k * STAGES + stage) % 2 * Lds::STAGE; };
+  auto scal_at = [&](int k) { return Lds::WAVES + (k % 2 * nw + wv) * Lds::SCAL; };
+  // stage `stage` of chunk k; with the first one what the positions have, with
+  // the last one G
+  auto fetch_stage = [&](int k, int stage) {
+    fetch_part(operands_of(k), stage * Blk::STAGE + (OUT ? 0 : PY * Blk::PART), stage_at(k, stage), Lds::STAGE);
+    if (stage == 0) fetch(uniform_buffer(w.scal + ((size_t)(block0 + k) * c.H + h) * 4 * kSsmQ, Lds::SCAL), 0, scal_at(k));
   };
   auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
-  if (Lds::AHEAD && k0 < k1) {
-    if (OUT)
-      fetch_cg(k0, 0);
-    else
-      fetch_b(k0, 0);
-    fetch_scal(k0);
+  if (k0 < k1) {
+    if (AHEAD) load_rows(k0);
+    fetch_stage(k0, 0);
     arrived();
   }
 
   double total = 0.0;  // log2 of the segment's decay
   for (int k = k0; k < k1; ++k) {
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
-    // rows first: they arrive while the operands are fetched, z by the end
-    load_rows(k);
-    Two<E> z[4][4];
-    if (OUT && c.z) {
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const auto r = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, min(rows - 16 * m, 16), c.D);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, zq + i * zs);
-      }
-    }
-    lds_barrier();  // the last chunk's operands have been read (and this one's first ones are there)
-    if (!Lds::AHEAD) {
-      fetch_scal(k);
-      if (OUT) fetch_cg(k, 0);
-      fetch_b(k, 0);
-    } else {
-      if (OUT) fetch_b(k, 0);
-      if (k + 1 < k1) {
-        if (OUT)
-          fetch_cg(k + 1, 0);
-        else
-          fetch_b(k + 1, 0);
-        fetch_scal(k + 1);
-      }
-    }
-    const double lq = w.lq[(size_t)(block0 + k) * c.H + h];
-    total += lq;
-    const bool fast = ssm_fast(lq);
-    const float dq = exp2_hw((float)lq);
+    if (!AHEAD) load_rows(k);
+    lds_barrier();  // the stage before has been read, this one is there
+    if (STAGES > 1)
+      fetch_stage(k, 1);
+    else if (k + 1 < k1)
+      fetch_stage(k + 1, 0);
+    if (OUT) fetch_part(operands_of(k), Blk::G, Lds::G, Blk::GBYTES);
+    const double* lq = w.lq + 2 * ((size_t)(block0 + k) * c.H + h);
+    const double l0 = lq[0], l1 = lq[1];
+    total += l0 + l1;
+    const bool fast = ssm_fast(l0, l1);
+    const float dq0 = exp2_hw((float)l0), dq1 = exp2_hw((float)l1);
     const float* pw = reinterpret_cast<const float*>(lds + scal_at(k));
     const float *pe = pw + kSsmQ, *plh = pw + 2 * kSsmQ, *pll = pw + 3 * kSsmQ;
+    Two<E> z[4][4];
 
     // x convolved: positions 16 m + 4 q + i, zeros past the sequence
     if (k == 0 && src >= 0 && q == 0) {
@@ -596,8 +589,6 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int k = 0; k < (int)(sizeof(to) / sizeof(to[0])); ++k)
         to[k] = *reinterpret_cast<const v8bf*>(lds + at + k * step + lane * 16);
     };
-    const int lds_c = OUT && Lds::AHEAD ? (k & 1) * Lds::CG : 0, lds_g = lds_c + PY * Blk::PART;
-    const int lds_b = Lds::B + (k & 1) * Lds::B2;
     v4f y[4][2];
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
@@ -606,22 +597,39 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     int bad[2] = {kSsmQ, kSsmQ};
 #pragma unroll
     for (int stage = 0; stage < STAGES; ++stage) {
-      constexpr int NF = 4 * NB;  // fragments of C, and of B for a block of positions twice as many states / 16
+      constexpr int NF = 4 * NB;  // fragments of C
+      const int a0 = 2 * stage * NB, a1 = a0 + 2 * NB, lds_c = stage_at(k, stage), lds_b = lds_c + Lds::C;
+      const bool final = stage == STAGES - 1;
       if (stage > 0) {
-        lds_barrier();  // the stage before has been read
-        if (OUT) fetch_cg(k, stage);
-        fetch_b(k, stage);
-      }
-      if (!Lds::AHEAD) {
         arrived();
-        lds_barrier();  // the operands are in LDS
+        lds_barrier();  // the stage before has been read, this one is there
+        if (!final)
+          fetch_stage(k, stage + 1);
+        else if (k + 1 < k1)
+          fetch_stage(k + 1, 0);
+      } else if (OUT && STAGES == 1) {
+        arrived();
+        lds_barrier();  // G is there
+      }
+      if (final) {
+        // under the products: this chunk's gates, the next one's rows
+        if (OUT && c.z) {
+          const unsigned from = here(zq);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const auto r = row_buffer<E>(c.z, r0 + 16 * m, c.z_stride, min(rows - 16 * m, 16), c.D);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, from + i * zs);
+          }
+        }
+        if (AHEAD) load_rows(k + 1);  // (past the segment's end too: nothing then depends on them)
       }
       if (OUT) {
         if (fast) {
 #pragma unroll
-          for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
+          for (int a = a0; a < a1; ++a)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) S[a][e] *= dq;
+            for (int e = 0; e < 2; ++e) S[a][e] *= dq0;
         }
         // fragments are read one ahead of their products
         v8bf cp[2][PY], sp[2][PY];
@@ -645,7 +653,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
           __builtin_amdgcn_sched_barrier(0);
           mul(cp[f & 1], sp, y[tt]);
         }
-        if (!fast && stage == STAGES - 1) {
+        if (!fast && final) {
           // rows by 2^l_t; the products below have the elements' own decays
 #pragma unroll
           for (int tt = 0; tt < 4; ++tt)
@@ -657,16 +665,12 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
               for (int e = 0; e < 2; ++e) y[tt][e][i] *= f;
             }
         }
-        if (Lds::AHEAD) {
-          arrived();
-          lds_barrier();  // B is in LDS
-        }
       }
       if (!OUT || !fast) {
 #pragma unroll
-        for (int a = 2 * stage * NB; a < 2 * (stage + 1) * NB; ++a)
+        for (int a = a0; a < a1; ++a)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) S[a][e] *= dq;
+          for (int e = 0; e < 2; ++e) S[a][e] *= dq0;
       }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -674,13 +678,25 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         frag(lds_b + b * 1024, Blk::PART, bp[0]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) operand(pw, b, e, xp[e]);
+        if (b) {
+#pragma unroll
+          for (int a = a0; a < a1; ++a)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) S[a][e] *= dq1;
+        }
 #pragma unroll
         for (int f = 0; f < 2 * NB; ++f) {
           if (f + 1 < 2 * NB) frag(lds_b + (2 * f + 2 + b) * 1024, Blk::PART, bp[(f + 1) & 1]);
           __builtin_amdgcn_sched_barrier(0);
-          mul(bp[f & 1], xp, S[2 * stage * NB + f]);
+          mul(bp[f & 1], xp, S[a0 + f]);
         }
-        if (!OUT || stage != STAGES - 1) continue;
+        if (!OUT || !final) continue;
+        if (b && fast) {
+#pragma unroll
+          for (int tt = 2; tt < 4; ++tt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) y[tt][e] *= dq1;
+        }
         v8bf yp[2][PY];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -713,7 +729,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         }
         // the blocks of G that have positions of b as columns: 0, 1, 2, 4 or 3, 5
         v8bf gp[2][PY];
-        auto g_at = [&](int tt) { return lds_g + (tt < 2 ? tt : 2 * tt - 2 + b) * 1024; };
+        auto g_at = [&](int tt) { return Lds::G + (tt < 2 ? tt : 2 * tt - 2 + b) * 1024; };
         frag(g_at(2 * b), Blk::GPART, gp[0]);
 #pragma unroll
         for (int tt = 2 * b; tt < 4; ++tt) {
@@ -737,7 +753,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         }
       }
     }
-    if (Lds::AHEAD) arrived();  // the next chunk's operands, before the stores
+    arrived();  // the next chunk's first stage, before the stores are on their way
     if (!OUT) continue;
     if (__ballot(bad[0] < kSsmQ || bad[1] < kSsmQ)) {
 #pragma unroll
@@ -775,6 +791,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
           y[m][1][i] *= silu_hw(z[m][i].hi());
         }
     }
+    const unsigned to = here(yq), to2 = here(yq2);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const auto r = row_buffer<E>(c.y, r0 + 16 * m, c.y_stride, min(rows - 16 * m, 16), c.D);
@@ -782,7 +799,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int i = 0; i < 4; ++i) {
         Two<E> out;
         out.set(y[m][0][i], y[m][1][i]);
-        store_two<E, PAIR>(out, r, yq + i * ys, yq2 + i * ys);
+        store_two<E, PAIR>(out, r, to + i * ys, to2 + i * ys);
       }
     }
   }
