@@ -26,7 +26,10 @@ auto with_dtype(int t, F&& f) {
   }
 }
 
-__device__ __forceinline__ float silu(float v) { return v / (1.0f + __expf(-v)); }
+__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+// The reciprocal is good to an ulp.
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + exp2_hw(-1.44269504f * v)); }
+__device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
 __device__ __forceinline__ float softplus(float v) { return v > 20.0f ? v : log1pf(__expf(v)); }
 
 }  // namespace lcsm

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         float f = 1.f;
-        if (c.act != LCSM_ACT_NONE) f = 1.f / (1.f + __expf(-u[e]));
+        if (c.act != LCSM_ACT_NONE) f = sigmoid(u[e]);
         if (c.act == LCSM_ACT_SILU) f *= u[e];
         v[k * VEC + e] = t[e] * f;
       }

@@ -14,98 +14,232 @@ namespace {
 
 constexpr int kSsmMaxN = 256;
 constexpr int kSsmMaxW = 4;
-constexpr int kScanRows = 16;  // channels of a head a workgroup takes
-
-// The short convolution of channel ch at row t of a sequence that begins at
-// row t0: taps before t0 from the window of slot s (s < 0: zeros).
-template <class E>
-__device__ __forceinline__ float ssm_conv(const SsmCall& c, int ch, int t, int t0, int s) {
-  const E* x = static_cast<const E*>(c.xbc);
-  const E* w = static_cast<const E*>(c.window);
-  float a = c.conv_b[ch];
-  for (int k = 0; k < c.W; ++k) {
-    const int tt = t - c.W + 1 + k;
-    float v = 0.f;
-    if (tt >= t0)
-      v = (float)x[(size_t)tt * c.xbc_stride + ch];
-    else if (s >= 0)
-      v = (float)w[((size_t)s * (c.W - 1) + (tt - t0 + c.W - 1)) * c.C + ch];
-    a = fmaf(c.conv_w[(size_t)ch * c.W + k], v, a);
-  }
-  return silu(a);
-}
-
-// The recurrence as it is written, one workgroup per sequence, head and
-// kScanRows channels.  L lanes hold the states of a channel, four of every 4 L
-// of them each.
-template <class E, int L>
+// The recurrence as it is written, for single tokens and short prompts.  A
+// workgroup takes ROWS channels of a head of one sequence and keeps their states
+// in registers (L lanes a channel, four states each); TB positions at a time it
+// convolves their x and its group's B and C into LDS, side by side, and then
+// goes through them one by one.  What a position costs is then a dozen FMAs a
+// lane: the sums over the states' lanes are taken for eight positions at once,
+// halving the lanes' shares of them instead of repeating the sum in all.
+//
+// The window of x is read and written by the workgroup that has its channels;
+// that of B and C is read by all heads of the group, and written by whichever
+// of them is the last to have read it (a count in `tickets`, back at zero
+// afterwards), so that a sequence can be continued in its own slot by this one
+// launch.
+template <class E, int L, int R, int TB>
 __global__ __launch_bounds__(256) void k_ssm_scan(SsmCall c) {
-  constexpr int RPP = 256 / L;  // channels side by side
-  constexpr int R = kScanRows > RPP ? kScanRows / RPP : 1;
-  __shared__ float su[2][kScanRows + 2 * kSsmMaxN];
-  const int i = (int)blockIdx.x, h = (int)blockIdx.y, p0 = (int)blockIdx.z * kScanRows;
+  constexpr int RPP = 256 / L, ROWS = R * RPP, NP = 4 * L, NC = ROWS + 2 * NP;
+  __shared__ __align__(16) float su[TB][NC];  // x, B, C
+  __shared__ float sy[TB][ROWS];
+  __shared__ float sstep[TB], sdecay[TB];
+  __shared__ int slast;
+  const int i = (int)blockIdx.z, h = (int)blockIdx.y, p0 = (int)blockIdx.x * ROWS;
   const int tid = (int)threadIdx.x, n0 = tid % L * 4, r0 = tid / L;
-  const int g = h / (c.H / c.G);
+  const int g = h / (c.H / c.G), W1 = c.W - 1;
   int t0, t1;
   ssm_rows(c, i, t0, t1);
   const int s = ssm_slot(c.src, i, c.slots), d = ssm_slot(c.dst, i, c.slots);
+  const size_t head = (size_t)c.P * c.N;
+  const bool quads = c.N % 4 == 0;
+  // a single token's gate is on its way from the start
+  E zt = (E)0.f;
+  if (TB == 1 && c.z && tid < ROWS && p0 + tid < c.P)
+    zt = static_cast<const E*>(c.z)[(size_t)i * c.z_stride + h * c.P + p0 + tid];
   float S[R][4];
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R; ++r) {
+    const int p = p0 + r0 + r * RPP;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int p = p0 + r0 + r * RPP;
-      const bool in = r0 + r * RPP < kScanRows && p < c.P && n0 + e < c.N;
-      S[r][e] = in && s >= 0 ? c.state[(((size_t)s * c.H + h) * c.P + p) * c.N + n0 + e] : 0.f;
-    }
-  for (int t = t0; t < t1; ++t) {
-    float* u = su[t & 1];
-    for (int k = tid; k < kScanRows + 2 * c.N; k += 256) {
-      int ch;
-      bool in = true;
-      if (k < kScanRows) {
-        in = p0 + k < c.P;
-        ch = h * c.P + p0 + k;
-      } else {
-        const int j = k - kScanRows;
-        ch = c.D + (j < c.N ? g * c.N + j : c.G * c.N + g * c.N + j - c.N);
-      }
-      u[k] = in ? ssm_conv<E>(c, ch, t, t0, s) : 0.f;
-    }
-    const float step = softplus((float)static_cast<const E*>(c.dt)[(size_t)t * c.dt_stride + h] +
-                                c.dt_bias[h]);
-    const float decay = __expf(step * c.A[h]);
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int q = r0 + r * RPP, p = p0 + q;
-      const float x = q < kScanRows ? u[q] : 0.f;
-      float y = 0.f;
+    for (int e = 0; e < 4; ++e) S[r][e] = 0.f;
+    if (s < 0 || p >= c.P || n0 >= c.N) continue;
+    const float* at = c.state + ((size_t)s * c.H + h) * head + (size_t)p * c.N + n0;
+    if (quads) {
+      const float4 v = *reinterpret_cast<const float4*>(at);
+      S[r][0] = v.x, S[r][1] = v.y, S[r][2] = v.z, S[r][3] = v.w;
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (n0 + e < c.N) {
-          S[r][e] = fmaf(S[r][e], decay, step * x * u[kScanRows + n0 + e]);
-          y = fmaf(S[r][e], u[kScanRows + c.N + n0 + e], y);
-        }
-#pragma unroll
-      for (int m = 1; m < L; m *= 2) y += __shfl_xor(y, m);
-      if (tid % L == 0 && q < kScanRows && p < c.P) {
-        const int ch = h * c.P + p;
-        y = fmaf(c.skip[h], x, y);
-        if (c.z) y *= silu((float)static_cast<const E*>(c.z)[(size_t)t * c.z_stride + ch]);
-        static_cast<E*>(c.y)[(size_t)t * c.y_stride + ch] = (E)y;
+        if (n0 + e < c.N) S[r][e] = at[e];
+    }
+  }
+  // channel of a row that column k of su is, -1: none
+  auto channel = [&](int k) {
+    if (k < ROWS) return p0 + k < c.P ? h * c.P + p0 + k : -1;
+    const int j = (k - ROWS) % NP;
+    return j < c.N ? c.D + (k < ROWS + NP ? 0 : c.G * c.N) + g * c.N + j : -1;
+  };
+  const E* x = static_cast<const E*>(c.xbc);
+  E* win = static_cast<E*>(c.window);
+  // rows before t0 from the window of slot s
+  auto raw = [&](int t, int ch) {
+    if (t >= t0) return x[(size_t)t * c.xbc_stride + ch];
+    return s >= 0 ? win[((size_t)s * W1 + (t - t0 + W1)) * c.C + ch] : (E)0.f;
+  };
+  const float skip = c.skip[h];
+  int ticket = 0;
+
+  for (int b = t0; b < t1; b += TB) {
+    const int nt = min(TB, t1 - b);
+    if (TB > 1 && b > t0) __syncthreads();  // the positions before have been read
+    for (int k = tid; k < NC; k += 256) {
+      const int ch = channel(k);
+      if (ch < 0) {
+        for (int t = 0; t < nt; ++t) su[t][k] = 0.f;
+        continue;
       }
+      float tap[4], v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tap[j] = 3 - j < c.W ? c.conv_w[(size_t)ch * c.W + c.W - 4 + j] : 0.f;
+      const float bias = c.conv_b[ch];
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (3 - j < c.W) v[j] = (float)raw(b - 3 + j, ch);
+#pragma unroll 8
+      for (int t = 0; t < nt; ++t) {
+        v[3] = (float)x[(size_t)(b + t) * c.xbc_stride + ch];
+        float a = bias;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (3 - j < c.W) a = fmaf(tap[j], v[j], a);
+        su[t][k] = silu(a);
+        v[0] = v[1], v[1] = v[2], v[2] = v[3];
+      }
+    }
+    if (tid < nt) {
+      const float step =
+          softplus((float)static_cast<const E*>(c.dt)[(size_t)(b + tid) * c.dt_stride + h] + c.dt_bias[h]);
+      sstep[tid] = step;
+      sdecay[tid] = __expf(step * c.A[h]);
+    }
+    __syncthreads();
+    if constexpr (TB == 1) {
+      const float step = sstep[0], decay = sdecay[0];
+      const float4 B = *reinterpret_cast<const float4*>(&su[0][ROWS + n0]);
+      const float4 C = *reinterpret_cast<const float4*>(&su[0][ROWS + NP + n0]);
+      float y[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float dx = step * su[0][r0 + r * RPP];
+        S[r][0] = fmaf(S[r][0], decay, dx * B.x);
+        S[r][1] = fmaf(S[r][1], decay, dx * B.y);
+        S[r][2] = fmaf(S[r][2], decay, dx * B.z);
+        S[r][3] = fmaf(S[r][3], decay, dx * B.w);
+        y[r] = fmaf(C.x, S[r][0], fmaf(C.y, S[r][1], fmaf(C.z, S[r][2], C.w * S[r][3])));
+      }
+#pragma unroll
+      for (int m = L / 2; m >= 1; m /= 2)
+#pragma unroll
+        for (int r = 0; r < R; ++r) y[r] += __shfl_xor(y[r], m);
+      if (tid % L == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sy[0][r0 + r * RPP] = y[r];
+    } else {
+      constexpr int U = 8;
+      for (int u0 = 0; u0 < nt; u0 += U) {
+        float y[R][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          // positions past the last one leave the states as they are
+          const bool in = u0 + u < nt;
+          const int t = in ? u0 + u : nt - 1;
+          const float step = sstep[t], decay = sdecay[t];
+          const float4 B = *reinterpret_cast<const float4*>(&su[t][ROWS + n0]);
+          const float4 C = *reinterpret_cast<const float4*>(&su[t][ROWS + NP + n0]);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float dx = step * su[t][r0 + r * RPP];
+            if (in) {
+              S[r][0] = fmaf(S[r][0], decay, dx * B.x);
+              S[r][1] = fmaf(S[r][1], decay, dx * B.y);
+              S[r][2] = fmaf(S[r][2], decay, dx * B.z);
+              S[r][3] = fmaf(S[r][3], decay, dx * B.w);
+            }
+            y[r][u] = fmaf(C.x, S[r][0], fmaf(C.y, S[r][1], fmaf(C.z, S[r][2], C.w * S[r][3])));
+          }
+        }
+        // lanes that differ in bit 0, 1, 2 share the eight sums among them
+        const int lane = tid % L;
+        constexpr int HALVE = L >= 8 ? 3 : 2;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+          for (int k = 0; k < HALVE; ++k) {
+            const int m = 1 << k, half = U >> (k + 1);
+            const bool up = lane & m;
+#pragma unroll
+            for (int j = 0; j < half; ++j) {
+              const float mine = up ? y[r][j + half] : y[r][j], theirs = up ? y[r][j] : y[r][j + half];
+              y[r][j] = mine + __shfl_xor(theirs, m);
+            }
+          }
+#pragma unroll
+          for (int m = 1 << HALVE; m < L; m *= 2)
+#pragma unroll
+            for (int j = 0; j < (U >> HALVE); ++j) y[r][j] += __shfl_xor(y[r][j], m);
+          if ((lane >> HALVE) == 0) {
+            int u = 0;
+#pragma unroll
+            for (int k = 0; k < HALVE; ++k) u += lane & (1 << k) ? U >> (k + 1) : 0;
+#pragma unroll
+            for (int j = 0; j < (U >> HALVE); ++j)
+              if (u0 + u + j < nt) sy[u0 + u + j][r0 + r * RPP] = y[r][j];
+          }
+        }
+      }
+    }
+    // All of this workgroup's reads of the window lie before the barrier above, their
+    // values used; relaxed, since nothing else is handed over (a release would
+    // write the whole L2 back), and looked at only at the end.
+    if (b == t0 && tid == 0 && W1 > 0 && d >= 0)
+      ticket = __hip_atomic_fetch_add(c.tickets + (size_t)i * c.G + g, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    for (int k = tid; k < nt * ROWS; k += 256) {
+      const int t = TB > 1 ? k / ROWS : 0, r = k % ROWS;
+      if (p0 + r >= c.P) continue;
+      const int ch = h * c.P + p0 + r;
+      float y = fmaf(skip, su[t][r], sy[t][r]);
+      if (c.z) y *= silu((float)(TB == 1 ? zt : static_cast<const E*>(c.z)[(size_t)(b + t) * c.z_stride + ch]));
+      static_cast<E*>(c.y)[(size_t)(b + t) * c.y_stride + ch] = (E)y;
     }
   }
   if (d < 0) return;
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R; ++r) {
+    const int p = p0 + r0 + r * RPP;
+    if (p >= c.P || n0 >= c.N) continue;
+    float* at = c.state + ((size_t)d * c.H + h) * head + (size_t)p * c.N + n0;
+    if (quads) {
+      *reinterpret_cast<float4*>(at) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int p = p0 + r0 + r * RPP;
-      if (r0 + r * RPP < kScanRows && p < c.P && n0 + e < c.N)
-        c.state[(((size_t)d * c.H + h) * c.P + p) * c.N + n0 + e] = S[r][e];
+      for (int e = 0; e < 4; ++e)
+        if (n0 + e < c.N) at[e] = S[r][e];
     }
+  }
+  // the window: x's by this workgroup, B's and C's by the last of the group; a
+  // sequence without tokens has read nothing, and copies its own
+  if (W1 == 0) return;
+  const bool none = t0 == t1;
+  if (none && s == d) return;
+  if (tid == 0) {
+    slast = none ? h % (c.H / c.G) == 0 && blockIdx.x == 0 : ticket == c.H / c.G * (int)gridDim.x - 1;
+    if (slast && !none)
+      __hip_atomic_store(c.tickets + (size_t)i * c.G + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  const bool shared = slast;
+  for (int k = tid; k < NC; k += 256) {
+    const int ch = channel(k);
+    if (ch < 0 || (k >= ROWS && !shared)) continue;
+    E v[3];
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (j < W1) v[j] = raw(t1 - W1 + j, ch);
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (j < W1) win[((size_t)d * W1 + j) * c.C + ch] = v[j];
+  }
 }
 
 // The windows after a call: a thread per sequence and channel.
@@ -135,21 +269,36 @@ __global__ __launch_bounds__(256) void k_ssm_window(SsmCall c) {
     if (k < c.W - 1) w[((size_t)d * (c.W - 1) + k) * c.C + ch] = v[k];
 }
 
-template <class E>
-hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
-  const dim3 grid((unsigned)c.n, (unsigned)c.H, (unsigned)((c.P + kScanRows - 1) / kScanRows));
-  if (c.N > 128)
-    hipLaunchKernelGGL((k_ssm_scan<E, 64>), grid, dim3(256), 0, st, c);
-  else if (c.N > 64)
-    hipLaunchKernelGGL((k_ssm_scan<E, 32>), grid, dim3(256), 0, st, c);
-  else
-    hipLaunchKernelGGL((k_ssm_scan<E, 16>), grid, dim3(256), 0, st, c);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || c.W == 1) return e;
-  hipLaunchKernelGGL(k_ssm_window<E>, dim3((unsigned)((c.C + 255) / 256), (unsigned)c.n), dim3(256),
-                     0, st, c);
+template <class E, int L, int R, int TB>
+hipError_t launch_scan_of(const SsmCall& c, hipStream_t st) {
+  constexpr int ROWS = R * 256 / L;
+  hipLaunchKernelGGL((k_ssm_scan<E, L, R, TB>), dim3((unsigned)((c.P + ROWS - 1) / ROWS), (unsigned)c.H, (unsigned)c.n),
+                     dim3(256), 0, st, c);
   return hipGetLastError();
 }
+constexpr int kScanBlock = 32;  // positions of a prompt in LDS
+
+// 16 channels a workgroup while that is what fills the card, 64 where there are
+// heads and sequences enough: B and C are then convolved for four times as many.
+template <class E, int L, int R, int R4>
+hipError_t launch_scan_rows(const SsmCall& c, hipStream_t st) {
+  if (!c.step) return launch_scan_of<E, L, R, kScanBlock>(c, st);
+  if ((long long)c.n * c.H * ((c.P + 63) / 64) >= 1024) return launch_scan_of<E, L, R4, 1>(c, st);
+  return launch_scan_of<E, L, R, 1>(c, st);
+}
+template <class E>
+hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
+  if (c.N <= 16) return launch_scan_rows<E, 4, 1, 1>(c, st);
+  if (c.N <= 32) return launch_scan_rows<E, 8, 1, 2>(c, st);
+  if (c.N <= 64) return launch_scan_rows<E, 16, 1, 4>(c, st);
+  if (c.N <= 128) return launch_scan_rows<E, 32, 2, 8>(c, st);
+  return launch_scan_rows<E, 64, 4, 16>(c, st);
+}
+
+// Up to so many tokens a prompt call goes through k_ssm_scan.  One prompt of 32
+// heads x 64 x 128 takes 19 us for 29 tokens, 60 for 128, 114 for 256 with it,
+// and in chunks 41 for 29, 89 for 513 to 1024.
+constexpr int kSsmScanTokens = 192;
 
 // How a prompt call is cut: segments of `per` chunks so that about one
 // workgroup per compute unit is on its way, which is what LDS holds; sequences
@@ -200,8 +349,9 @@ struct lcsm_ssm {
   void* owned;
   float *state, *conv_w, *conv_b, *A, *skip, *dt_bias;
   char* window;
+  int* tickets;
   lcsm::SsmScratch scratch;
-  size_t zero_floats;  // states and windows, from `state` on
+  size_t zero_floats;  // states, windows and tickets, from `state` on
   bool faulted;
   char msg[256];
 };
@@ -211,7 +361,7 @@ namespace {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
-  size_t state, window, conv_w, conv_b, A, skip, dt_bias, bc, scal, lq, states, decay, total;
+  size_t state, window, tickets, conv_w, conv_b, A, skip, dt_bias, bc, scal, lq, states, decay, total;
 };
 
 bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
@@ -233,6 +383,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   };
   take(&p->state, MS * (size_t)D * s->N * 4);
   take(&p->window, MS * (s->W - 1) * c * lcsm::dtype_size(s->dtype));
+  take(&p->tickets, (size_t)s->slots * s->G * 4);
   take(&p->conv_w, M * c * s->W * 4);
   take(&p->conv_b, M * c * 4);
   take(&p->A, M * H * 4);
@@ -284,7 +435,7 @@ int ssm_call(lcsm_ssm* c, int layer, int T, int n, const lcsm_ssm_io* io, lcsm::
                      io->xbc_stride, io->dt_stride, io->z_stride, io->y_stride,
                      c->conv_w + m * C * c->s.W, c->conv_b + m * C, c->A + m * H, c->skip + m * H,
                      c->dt_bias + m * H, c->state + m * c->s.slots * (size_t)c->D * c->s.N,
-                     c->window + m * c->s.slots * (c->s.W - 1) * C * lcsm::dtype_size(c->s.dtype)};
+                     c->window + m * c->s.slots * (c->s.W - 1) * C * lcsm::dtype_size(c->s.dtype), c->tickets};
   return LCSM_OK;
 }
 
@@ -326,6 +477,7 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
   }
   c->state = (float*)(c->mem + p.state);
   c->window = c->mem + p.window;
+  c->tickets = (int*)(c->mem + p.tickets);
   c->zero_floats = (p.conv_w - p.state) / 4;
   c->conv_w = (float*)(c->mem + p.conv_w);
   c->conv_b = (float*)(c->mem + p.conv_b);
@@ -384,7 +536,11 @@ int lcsm_ssm_prompt_layer(lcsm_ssm* ctx, int layer, int T, int n, const int* off
   int r = ssm_call(ctx, layer, T, n, io, &k);
   if (r || !n) return r;
   k.offsets = offsets;
-  hipError_t e = lcsm::launch_prompt(k, ctx->s.dtype, ctx->scratch, ctx->stream);
+  hipError_t e;
+  if (T <= lcsm::kSsmScanTokens)
+    e = lcsm::with_dtype(ctx->s.dtype, [&](auto v) { return lcsm::launch_scan<decltype(v)>(k, ctx->stream); });
+  else
+    e = lcsm::launch_prompt(k, ctx->s.dtype, ctx->scratch, ctx->stream);
   return e == hipSuccess ? LCSM_OK : ssm_fail(ctx, LCSM_EDEVICE, "prompt launch", e);
 }
 

@@ -19,6 +19,7 @@ struct SsmCall {
   const float *conv_w, *conv_b, *A, *skip, *dt_bias;  // of the layer
   float* state;                                       // [slots][H][P][N]
   void* window;                                       // [slots][W-1][C]
+  int* tickets;                                       // [slots][G], zero between calls
 };
 
 __device__ __forceinline__ int ssm_slot(const int* list, int i, int slots) {

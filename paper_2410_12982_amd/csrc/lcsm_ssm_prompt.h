@@ -81,12 +81,6 @@ __device__ __forceinline__ void split(float (&v)[8], v8bf (&to)[P]) {
   }
 }
 
-__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
-// v / (1 + e^-v); the reciprocal is good to an ulp.
-__device__ __forceinline__ float silu_hw(float v) {
-  return v * __builtin_amdgcn_rcpf(1.f + exp2_hw(-1.44269504f * v));
-}
-
 // The piece [*k0, *k1) of `per` chunks (and its sequence, its number in it and
 // the sequence's chunks) that has number `want` when the pieces of all
 // sequences are counted one after another, every sequence having at least
@@ -210,7 +204,7 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (3 - j < c.W) v = fmaf(tap[j], x[j], v);
-        v = silu_hw(v);
+        v = silu(v);
         x[0] = x[1];
         x[1] = x[2];
         x[2] = x[3];
@@ -564,7 +558,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) u[m][i][0] = silu_hw(u[m][i][0]), u[m][i][1] = silu_hw(u[m][i][1]);
+      for (int i = 0; i < 4; ++i) u[m][i][0] = silu(u[m][i][0]), u[m][i][1] = silu(u[m][i][1]);
     if (rows < kSsmQ) {
 #pragma unroll
       for (int m = 0; m < 4; ++m)
@@ -787,8 +781,8 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[m][0][i] *= silu_hw(z[m][i].lo());
-          y[m][1][i] *= silu_hw(z[m][i].hi());
+          y[m][0][i] *= silu(z[m][i].lo());
+          y[m][1][i] *= silu(z[m][i].hi());
         }
     }
     const unsigned to = here(yq), to2 = here(yq2);
