@@ -73,41 +73,22 @@ __device__ __forceinline__ typename Mat<E>::V weights(unsigned w) {
   return __builtin_bit_cast(typename T::V, r);
 }
 
-// Inputs k .. k+7 of a row, zeros past K and for rows that there are not.
-template <class E>
-__device__ __forceinline__ void load_x(const E* row, int k, int K, bool vec, bool live, E (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (E)0.f;
-  if (!live) return;
-  if (vec && k + 8 <= K) {
-    struct alignas(16) Pack {
-      E e[8];
-    };
-    const Pack p = *reinterpret_cast<const Pack*>(row + k);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p.e[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k + i < K) v[i] = row[k + i];
-  }
-}
-
-template <class E>
-__device__ __forceinline__ void operand(const E (&v)[8], typename Mat<E>::V (&a)[Mat<E>::PARTS]) {
+template <class E, int XV>
+__device__ __forceinline__ void operand(const v4u (&x)[XV], typename Mat<E>::V (&a)[Mat<E>::PARTS]) {
   if constexpr (std::is_same<E, float>::value) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const bf16_t hi = (bf16_t)v[i];
-      const float r1 = v[i] - (float)hi;
+      const unsigned w = x[i / 4][i % 4];
+      const float v = __builtin_bit_cast(float, w);
+      const bf16_t hi = (bf16_t)v;
+      const float r1 = v - (float)hi;
       const bf16_t mid = (bf16_t)r1;
       a[0][i] = hi;
       a[1][i] = mid;
       a[2][i] = (bf16_t)(r1 - (float)mid);
     }
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[0][i] = v[i];
+    a[0] = __builtin_bit_cast(typename Mat<E>::V, x[0]);
   }
 }
 
@@ -117,73 +98,135 @@ __device__ __forceinline__ float scale_at(const void* p, int dtype, size_t i) {
   return static_cast<const float*>(p)[i];
 }
 
+// What a wave loads of a tile ahead of its products: codes, scales and zeros, and
+// for up to 16 rows x as it comes (more rows would not leave the registers).
+template <class E, int SPG, int RT, int NT>
+struct Tile {
+  static constexpr int GS = 4 / SPG;                 // scales a tile and output
+  static constexpr int XV = sizeof(E) == 4 ? 2 : 1;  // 16-byte loads for eight inputs
+  static constexpr int XA = RT == 1 ? 4 : 1;
+  v4u w[NT], x[XA][RT][XV];
+  float s[NT][GS], z[NT][GS];
+};
+
 // A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
 // every so many'th tile along K, their sums meet in LDS and are added in a
 // fixed order.  SPG: 32-input products a scale (4: a scale for the whole tile).
+// The next tile's loads are on their way while one is multiplied.
 template <class E, int SPG, int RT, int NT>
-__global__ __launch_bounds__(kMaxWaves * 64) void k_q4(Q4Call c, bool vec) {
+__global__ __launch_bounds__(RT == 1 ? kMaxWaves * 64 : kMaxWaves * 32) void k_q4(Q4Call c, bool vec) {
   typedef Mat<E> T;
+  typedef Tile<E, SPG, RT, NT> Tl;
+  constexpr int GS = Tl::GS;
   extern __shared__ float part[];  // [waves][NT][RT][16 rows][16 outputs]
-  const int lane = (int)threadIdx.x & 63, wv = (int)threadIdx.x >> 6, nw = (int)blockDim.x >> 6;
+  const int lane = (int)threadIdx.x & 63, nw = (int)blockDim.x >> 6;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int q = lane >> 4, col = lane & 15;
   const int nt0 = (int)blockIdx.x * NT, r0 = (int)blockIdx.y * 16 * RT;
   const int nts = (c.N + kTileN - 1) / kTileN;
   const unsigned one = std::is_same<E, f16_t>::value ? 0x3C003C00u : 0x3F803F80u;
   const typename T::V ones = __builtin_bit_cast(typename T::V, (v4u){one, one, one, one});
+  const v4f none = {0.f, 0.f, 0.f, 0.f};
   v4f y[NT][RT];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int r = 0; r < RT; ++r) y[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
-  const v4f none = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < RT; ++r) y[t][r] = none;
+  // rows past the last one are the last one again: an output row has its x row
+  // only, and these are not stored
+  const E* row[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+    row[r] = static_cast<const E*>(c.x) + (size_t)min(r0 + 16 * r + col, c.rows - 1) * c.x_stride + 8 * q;
 
-  for (int kb = wv; kb < c.kb; kb += nw) {
-    v4u w[NT];
+  // inputs 32 j + 8 q ..+7 of tile kb, zeros past K
+  auto load_x = [&](int kb, int j, v4u (&to)[RT][Tl::XV]) {
+    const int k0 = kb * kTileK + 32 * j;
+    if (vec && (kb + 1) * kTileK <= c.K) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int v = 0; v < Tl::XV; ++v) to[r][v] = reinterpret_cast<const v4u*>(row[r] + k0)[v];
+    } else {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        struct {
+          E e[8];
+        } p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.e[i] = k0 + i + 8 * q < c.K ? row[r][k0 + i] : (E)0.f;
+        struct Words {
+          v4u v[Tl::XV];
+        };
+        const Words w = __builtin_bit_cast(Words, p);
+#pragma unroll
+        for (int v = 0; v < Tl::XV; ++v) to[r][v] = w.v[v];
+      }
+    }
+  };
+  auto load = [&](int kb, Tl& to) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int nt = min(nt0 + t, nts - 1);
-      w[t] = static_cast<const v4u*>(c.codes)[((size_t)nt * c.kb + kb) * 64 + lane];
+      const size_t nt = (size_t)min(nt0 + t, nts - 1);
+      to.w[t] = static_cast<const v4u*>(c.codes)[(nt * c.kb + kb) * 64 + lane];
+#pragma unroll
+      for (int g = 0; g < GS; ++g) {
+        const int at = SPG == 4 ? kb * kTileK / c.group : min(kb * GS + g, c.ng - 1);
+        const size_t i = (nt * c.ng + at) * kTileN + col;
+        to.s[t][g] = scale_at(c.scales, c.scale_dtype, i);
+        to.z[t][g] = c.zeros ? -16.f - (float)c.zeros[i] : -24.f;
+      }
     }
+    if (RT == 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_x(kb, j, to.x[RT == 1 ? j : 0]);
+    }
+  };
+  auto multiply = [&](int kb, Tl& tl) {
     v4f acc[NT][RT], sum[RT];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       typename T::V a[RT][T::PARTS];
+      if (RT > 1) load_x(kb, j, tl.x[0]);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const int row = r0 + 16 * r + col;
-        E v[8];
-        load_x<E>(static_cast<const E*>(c.x) + (size_t)row * c.x_stride, kb * kTileK + 32 * j + 8 * q,
-                  c.K, vec, row < c.rows, v);
-        operand<E>(v, a[r]);
-      }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
+        operand<E>(tl.x[RT == 1 ? j : 0][r], a[r]);
         if (j % SPG == 0) sum[r] = none;
 #pragma unroll
         for (int p = 0; p < T::PARTS; ++p) sum[r] = T::mul(a[r][p], ones, sum[r]);
       }
-      const int g = SPG == 4 ? kb * kTileK / c.group : kb * (4 / SPG) + j / SPG;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const typename T::V b = weights<E>(w[t][j]);
+        const typename T::V b = weights<E>(tl.w[t][j]);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           if (j % SPG == 0) acc[t][r] = none;
 #pragma unroll
           for (int p = 0; p < T::PARTS; ++p) acc[t][r] = T::mul(a[r][p], b, acc[t][r]);
         }
-        if (j % SPG == SPG - 1 && g < c.ng) {
-          const size_t at = ((size_t)min(nt0 + t, nts - 1) * c.ng + g) * kTileN + col;
-          const float s = scale_at(c.scales, c.scale_dtype, at);
-          const float z = c.zeros ? 16.f + (float)c.zeros[at] : 24.f;
+      }
+      if (j % SPG == SPG - 1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              y[t][r][e] = fmaf(s, fmaf(-z, sum[r][e], acc[t][r][e]), y[t][r][e]);
-        }
+              y[t][r][e] = fmaf(tl.s[t][j / SPG], fmaf(tl.z[t][j / SPG], sum[r][e], acc[t][r][e]), y[t][r][e]);
       }
     }
+  };
+  Tl a, b;
+  int kb = wv;
+  if (kb < c.kb) load(kb, a);
+  while (kb < c.kb) {
+    if (kb + nw < c.kb) load(kb + nw, b);
+    multiply(kb, a);
+    kb += nw;
+    if (kb >= c.kb) break;
+    if (kb + nw < c.kb) load(kb + nw, a);
+    multiply(kb, b);
+    kb += nw;
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -196,11 +239,11 @@ __global__ __launch_bounds__(kMaxWaves * 64) void k_q4(Q4Call c, bool vec) {
   constexpr int OUT = NT * RT * 256;
   for (int o = (int)threadIdx.x; o < OUT; o += (int)blockDim.x) {
     const int t = o / (RT * 256), r = o / 16 % (RT * 16), n = (nt0 + t) * kTileN + o % 16;
-    const int row = r0 + r;
-    if (n >= c.N || row >= c.rows) continue;
+    const int at = r0 + r;
+    if (n >= c.N || at >= c.rows) continue;
     float v = c.bias ? c.bias[n] : 0.f;
     for (int w = 0; w < nw; ++w) v += part[w * OUT + o];
-    static_cast<E*>(c.y)[(size_t)row * c.y_stride + n] = (E)v;
+    static_cast<E*>(c.y)[(size_t)at * c.y_stride + n] = (E)v;
   }
 }
 
@@ -270,7 +313,7 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w
 template <class E, int SPG, int RT, int NT>
 hipError_t launch(const Q4Call& c, hipStream_t st) {
   const bool vec = ((uintptr_t)c.x & 15) == 0 && c.x_stride * sizeof(E) % 16 == 0;
-  const int waves = c.kb < 8 ? c.kb : 8;
+  const int most = RT == 1 ? kMaxWaves : kMaxWaves / 2, waves = c.kb < most ? c.kb : most;
   const dim3 grid((unsigned)(((c.N + 15) / 16 + NT - 1) / NT), (unsigned)((c.rows + 16 * RT - 1) / (16 * RT)));
   hipLaunchKernelGGL((k_q4<E, SPG, RT, NT>), grid, dim3(64 * waves), (size_t)waves * NT * RT * 1024, st, c, vec);
   return hipGetLastError();
