@@ -45,12 +45,14 @@ template <class E>
 struct Mat {  // fp16
   typedef v8h V;
   static constexpr int PARTS = 1, ROT = 29;
+  static constexpr float OFF = -16.f;  // (minus) what an operand has above its code
   static constexpr unsigned BASE = 0x4C004C00u, MASK = 0x03C003C0u;  // codes at bits 6 and 22
   static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 struct MatBf {
   typedef v8bf V;
   static constexpr int PARTS = 1, ROT = 0;
+  static constexpr float OFF = -16.f;
   static constexpr unsigned BASE = 0x41804180u, MASK = 0x00780078u;  // codes at bits 3 and 19
   static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
@@ -59,6 +61,7 @@ struct Mat<bf16_t> : MatBf {};
 template <>
 struct Mat<float> : MatBf {
   static constexpr int PARTS = 3;
+  static constexpr float OFF = 8.f;
 };
 
 template <class E>
@@ -69,6 +72,17 @@ __device__ __forceinline__ typename Mat<E>::V weights(unsigned w) {
   for (int t = 0; t < 4; ++t) {
     const unsigned k = __builtin_rotateright32(w, (4 * t + T::ROT) % 32);
     r[t] = (k & T::MASK) | T::BASE;
+  }
+  if constexpr (std::is_same<E, float>::value) {
+    // code - 8 instead, exact as well: sums that are to be good to fp32 must not
+    // lose bits to 24 sums of x that come off again
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+      const v2bf two = {(bf16_t)(__builtin_bit_cast(float, r[t] << 16) - 24.f),
+                        (bf16_t)(__builtin_bit_cast(float, r[t] & 0xffff0000u) - 24.f)};
+      r[t] = __builtin_bit_cast(unsigned, two);
+    }
   }
   return __builtin_bit_cast(typename T::V, r);
 }
@@ -109,12 +123,18 @@ struct Tile {
   float s[NT][GS], z[NT][GS];
 };
 
+// Waves of a workgroup at most: 16 where 128 registers are enough, else 8.
+template <class E, int SPG>
+constexpr int q4_waves(int RT, int NT) {
+  return RT == 1 && (NT == 1 || (sizeof(E) == 2 && (NT == 2 || SPG == 4))) ? kMaxWaves : kMaxWaves / 2;
+}
+
 // A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
 // every so many'th tile along K, their sums meet in LDS and are added in a
 // fixed order.  SPG: 32-input products a scale (4: a scale for the whole tile).
 // The next tile's loads are on their way while one is multiplied.
 template <class E, int SPG, int RT, int NT>
-__global__ __launch_bounds__(RT == 1 ? kMaxWaves * 64 : kMaxWaves * 32) void k_q4(Q4Call c, bool vec) {
+__global__ __launch_bounds__((q4_waves<E, SPG>(RT, NT)) * 64) void k_q4(Q4Call c, bool vec) {
   typedef Mat<E> T;
   typedef Tile<E, SPG, RT, NT> Tl;
   constexpr int GS = Tl::GS;
@@ -174,7 +194,7 @@ __global__ __launch_bounds__(RT == 1 ? kMaxWaves * 64 : kMaxWaves * 32) void k_q
         const int at = SPG == 4 ? kb * kTileK / c.group : min(kb * GS + g, c.ng - 1);
         const size_t i = (nt * c.ng + at) * kTileN + col;
         to.s[t][g] = scale_at(c.scales, c.scale_dtype, i);
-        to.z[t][g] = c.zeros ? -16.f - (float)c.zeros[i] : -24.f;
+        to.z[t][g] = Mat<E>::OFF - (c.zeros ? (float)c.zeros[i] : 8.f);
       }
     }
     if (RT == 1) {
@@ -311,19 +331,53 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w
 }
 
 template <class E, int SPG, int RT, int NT>
-hipError_t launch(const Q4Call& c, hipStream_t st) {
+hipError_t launch(const Q4Call& c, int most, hipStream_t st) {
   const bool vec = ((uintptr_t)c.x & 15) == 0 && c.x_stride * sizeof(E) % 16 == 0;
-  const int most = RT == 1 ? kMaxWaves : kMaxWaves / 2, waves = c.kb < most ? c.kb : most;
+  constexpr int MOST = q4_waves<E, SPG>(RT, NT);
+  if (most > MOST) most = MOST;
+  const int waves = c.kb < most ? c.kb : most;
+  const size_t lds = (size_t)waves * NT * RT * 1024;
   const dim3 grid((unsigned)(((c.N + 15) / 16 + NT - 1) / NT), (unsigned)((c.rows + 16 * RT - 1) / (16 * RT)));
-  hipLaunchKernelGGL((k_q4<E, SPG, RT, NT>), grid, dim3(64 * waves), (size_t)waves * NT * RT * 1024, st, c, vec);
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q4<E, SPG, RT, NT>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_q4<E, SPG, RT, NT>), grid, dim3(64 * waves), lds, st, c, vec);
   return hipGetLastError();
 }
 
+// The largest pieces that still are workgroups enough: a piece of NT tiles reads
+// x once for all of them, one of RT tiles of rows unpacks the codes once.  bf16,
+// groups of 128, us (workgroups' pieces as RT NT / waves):
+//   16 rows, 8512 x 2048: 14/16 6.2, 12/8 7.3, 11/8 8.4;  2048 x 4096: 11/16 6.5,
+//   12/16 7.2, 14/16 10.5;  16384 x 8192: 12/8 23.3, 14/16 25.8, 11/8 34.3
+//   (one row 17.1, 23.1, 20.2: long rows are read by fewer waves)
+//   32 rows, 8512 x 2048: 24/8 8.8, 12/8 10.0;  4096 x 1024: 12/8 3.8, 11/16 4.5,
+//   24/8 above 5;  2048 x 4096: 11/16 6.7, 12/16 7.3
+//   64 rows, 8512 x 2048: 44/8 13.6, 22/8 16.0;  4096 x 1024: 14/16 4.9, 22/8 5.1;
+//   2048 x 4096: 12/16 7.5, 11/16 11.7, 14/16 11.5
 template <class E, int SPG>
 hipError_t launch_rows(const Q4Call& c, hipStream_t st) {
-  if (c.rows <= 16) return launch<E, SPG, 1, 1>(c, st);
-  if (c.rows <= 32) return launch<E, SPG, 2, 1>(c, st);
-  return launch<E, SPG, 4, 1>(c, st);
+  const long long tiles = (c.N + 15) / 16, rows = (c.rows + 15) / 16;
+  auto groups = [&](int rt, int nt) { return (tiles + nt - 1) / nt * ((rows + rt - 1) / rt); };
+  if (rows > 2) {
+    // (scales for every 32 or 64 inputs, or fp32 rows in three parts, leave no
+    // registers for pieces as large)
+    constexpr int RT = sizeof(E) == 4 ? 2 : 4, NT = SPG == 4 && sizeof(E) == 2 ? 4 : 2;
+    if (groups(4, 4) >= 128) return launch<E, SPG, RT, NT>(c, 8, st);
+    if (groups(1, 4) >= 256) return launch<E, SPG, 1, 4>(c, 16, st);
+    return launch<E, SPG, 1, 2>(c, 16, st);
+  }
+  if (rows == 2) {
+    constexpr int NT = SPG == 4 && sizeof(E) == 2 ? 4 : 2;
+    if (groups(2, 4) >= 128) return launch<E, SPG, 2, NT>(c, 8, st);
+    if (groups(1, 2) >= 256) return launch<E, SPG, 1, 2>(c, 8, st);
+    return launch<E, SPG, 1, 1>(c, 16, st);
+  }
+  if (tiles < 512) return launch<E, SPG, 1, 1>(c, 16, st);
+  if (c.kb <= 16) return launch<E, SPG, 1, 4>(c, 16, st);
+  return launch<E, SPG, 1, 2>(c, 8, st);
 }
 
 template <class E>
