@@ -117,147 +117,6 @@ __device__ __forceinline__ bool ssm_piece(const SsmCall& c, int want, int per, i
   return false;
 }
 
-// Element ch of row r of the sequence that begins at row t0, from the rows or
-// (r < t0) from the window of slot s.
-template <class E>
-__device__ __forceinline__ E ssm_row(const SsmCall& c, int r, int t0, int s, int ch) {
-  if (r >= t0) return static_cast<const E*>(c.xbc)[(size_t)r * c.xbc_stride + ch];
-  if (s < 0) return (E)0.f;
-  return static_cast<const E*>(c.window)[((size_t)s * (c.W - 1) + (r - t0 + c.W - 1)) * c.C + ch];
-}
-
-// What a chunk's positions have of a head, a position a lane: w, then E where
-// the chunk is `fast`, else step and l in two parts.
-__device__ __forceinline__ bool ssm_fast(double l0, double l1) { return fabs(l0) < 64.0 && fabs(l1) < 64.0; }
-
-template <class E>
-__device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h) {
-  const int lane = (int)threadIdx.x & 63;
-  float step = 0.f;
-  if (lane < rows)
-    step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + c.dt_bias[h]);
-  // fp64: l reaches thousands where steps are long, and its differences count
-  double l = (double)(step * c.A[h]) * 1.4426950408889634;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const double v = __shfl_up(l, m);
-    if (lane >= m) l += v;
-  }
-  const double l0 = __shfl(l, 31), lq = __shfl(l, 63), le = lane < 32 ? l0 : lq;
-  const size_t at = (size_t)block * c.H + h;
-  float* to = w.scal + at * 4 * kSsmQ + lane;
-  to[0] = step * exp2_hw((float)(le - l));
-  const float hi = (float)l;
-  to[kSsmQ] = ssm_fast(l0, lq - l0) ? exp2_hw((float)(l - le)) : step;
-  to[2 * kSsmQ] = hi;
-  to[3 * kSsmQ] = (float)(l - (double)hi);
-  if (lane < 2) w.lq[2 * at + lane] = lane ? lq - l0 : l0;
-}
-
-// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); the
-// workgroups past the groups take the decays of kSsmDecayHeads heads each.
-constexpr int kSsmDecayHeads = 16;
-
-template <class E, int NT>
-__global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
-  constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
-  typedef SsmBlock<NT, PY> Blk;
-  __shared__ __align__(16) float lb[kSsmQ * LD];
-  __shared__ __align__(16) float lc[kSsmQ * LD];
-  int seq, num, chunks;
-  if (!ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
-  if ((int)blockIdx.x >= w.blocks) return;
-  int t0, t1;
-  ssm_rows(c, seq, t0, t1);
-  const int s = ssm_slot(c.src, seq, c.slots), g = (int)blockIdx.y, r0 = t0 + num * kSsmQ;
-  const int tid = (int)threadIdx.x, rows = min(kSsmQ, t1 - r0);
-  if (g >= c.G) {
-    const int h0 = (g - c.G) * kSsmDecayHeads, h1 = min(h0 + kSsmDecayHeads, c.H);
-    for (int h = h0 + tid / 64; h < h1; h += 4) ssm_decays<E>(c, w, (int)blockIdx.x, r0, rows, h);
-    return;
-  }
-  // a thread convolves one channel along a quarter of the chunk's rows
-  constexpr int RUN = kSsmQ / 4;
-  for (int k = tid; k < 2 * NP * 4; k += 256) {
-    const int col = k % (2 * NP), run = k / (2 * NP) * RUN;
-    const int n = col % NP;
-    float* to = (col < NP ? lb : lc) + run * LD + n;
-    if (n >= c.N) {
-      for (int t = 0; t < RUN; ++t) to[t * LD] = 0.f;
-      continue;
-    }
-    const int ch = c.D + (col < NP ? 0 : c.G * c.N) + g * c.N + n;
-    float tap[4] = {0.f, 0.f, 0.f, 0.f}, x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < c.W) tap[3 - j] = c.conv_w[(size_t)ch * c.W + c.W - 1 - j];
-    const float bias = c.conv_b[ch];
-#pragma unroll
-    for (int j = 1; j < 4; ++j)
-      if (j < c.W && run - j < rows) x[3 - j] = (float)ssm_row<E>(c, r0 + run - j, t0, s, ch);
-#pragma unroll
-    for (int t = 0; t < RUN; ++t) {
-      float v = 0.f;
-      if (run + t < rows) {
-        x[3] = (float)static_cast<const E*>(c.xbc)[(size_t)(r0 + run + t) * c.xbc_stride + ch];
-        v = bias;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (3 - j < c.W) v = fmaf(tap[j], x[j], v);
-        v = silu(v);
-        x[0] = x[1];
-        x[1] = x[2];
-        x[2] = x[3];
-      }
-      to[t * LD] = v;
-    }
-  }
-  __syncthreads();
-  char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * Blk::BYTES;
-  const int lane = tid & 63, wv = tid >> 6, q = lane >> 4, l = lane & 15;
-  auto put = [&](int at, int step, float (&v)[8], auto parts) {
-    v8bf w[decltype(parts)::value];
-    split(v, w);
-#pragma unroll
-    for (int k = 0; k < decltype(parts)::value; ++k) reinterpret_cast<v8bf*>(out + at + k * step)[lane] = w[k];
-  };
-  const std::integral_constant<int, PY> py;
-  const std::integral_constant<int, kSsmParts> ps;
-  for (int f = wv; f < 4 * NT; f += 4) {
-    const int tt = f / NT, cc = f % NT;
-    const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
-    float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
-    put(Blk::c_at(tt, cc), Blk::PART, v, py);
-  }
-  for (int f = wv; f < 4 * NT; f += 4) {
-    const int a = f / 2, b = f % 2;
-    const float* p = lb + (32 * b + 4 * q) * LD + 16 * a + l;
-    float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
-    put(Blk::b_at(a, b), Blk::PART, v, ps);
-  }
-  // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
-  // are the lane's slots
-  for (int f = wv; f < 6; f += 4) {
-    const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
-    float v[8];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int st = 2 * cc + half;
-      v4f acc = {0.f, 0.f, 0.f, 0.f};
-      if (st <= tt) {
-        const float* pb = lb + (16 * st + l) * LD + q;
-        const float* pc = lc + (16 * tt + l) * LD + q;
-#pragma unroll 8
-        for (int k = 0; k < NP / 4; ++k)
-          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(pb[4 * k], pc[4 * k], acc, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[4 * half + i] = 16 * st + 4 * q + i <= 16 * tt + l ? acc[i] : 0.f;
-    }
-    put(Blk::g_at(f), Blk::GPART, v, py);
-  }
-}
-
 // Two neighbouring channels as they come.
 template <class E>
 struct Two {
@@ -318,6 +177,11 @@ __device__ __forceinline__ Two<E> load_two(__amdgpu_buffer_rsrc_t r, unsigned at
   }
   return t;
 }
+template <class E>
+__device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, unsigned at) {
+  if constexpr (sizeof(E) == 4) return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+  else return (float)__builtin_bit_cast(E, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
+}
 // `second`: where the second channel goes by itself.
 template <class E, bool PAIR>
 __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, unsigned at, unsigned second) {
@@ -334,6 +198,143 @@ __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, un
   } else {
     __builtin_amdgcn_raw_buffer_store_b16((unsigned short)t.v, r, at, 0, 0);
     __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(t.v >> 16), r, second, 0, 0);
+  }
+}
+
+// What a chunk's positions have of a head, a position a lane: w, then E where
+// the chunk is `fast`, else step and l in two parts.
+__device__ __forceinline__ bool ssm_fast(double l0, double l1) { return fabs(l0) < 64.0 && fabs(l1) < 64.0; }
+
+template <class E>
+__device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h) {
+  const int lane = (int)threadIdx.x & 63;
+  float step = 0.f;
+  if (lane < rows)
+    step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + c.dt_bias[h]);
+  // fp64: l reaches thousands where steps are long, and its differences count
+  double l = (double)(step * c.A[h]) * 1.4426950408889634;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const double v = __shfl_up(l, m);
+    if (lane >= m) l += v;
+  }
+  const double l0 = __shfl(l, 31), lq = __shfl(l, 63), le = lane < 32 ? l0 : lq;
+  const size_t at = (size_t)block * c.H + h;
+  float* to = w.scal + at * 4 * kSsmQ + lane;
+  to[0] = step * exp2_hw((float)(le - l));
+  const float hi = (float)l;
+  to[kSsmQ] = ssm_fast(l0, lq - l0) ? exp2_hw((float)(l - le)) : step;
+  to[2 * kSsmQ] = hi;
+  to[3 * kSsmQ] = (float)(l - (double)hi);
+  if (lane < 2) w.lq[2 * at + lane] = lane ? lq - l0 : l0;
+}
+
+// A wave per chunk and head.
+template <class E>
+__global__ __launch_bounds__(256) void k_ssm_decays(SsmCall c, SsmScratch w) {
+  const int h = (int)blockIdx.y * 4 + (int)threadIdx.x / 64;
+  int seq, num, chunks;
+  if (h >= c.H || (int)blockIdx.x >= w.blocks || !ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
+  int t0, t1;
+  ssm_rows(c, seq, t0, t1);
+  const int r0 = t0 + num * kSsmQ;
+  ssm_decays<E>(c, w, (int)blockIdx.x, r0, min(kSsmQ, t1 - r0), h);
+}
+
+// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock).
+template <class E, int NT>
+__global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
+  constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
+  typedef SsmBlock<NT, PY> Blk;
+  __shared__ __align__(16) float lb[kSsmQ * LD];
+  __shared__ __align__(16) float lc[kSsmQ * LD];
+  int seq, num, chunks;
+  if (!ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
+  if ((int)blockIdx.x >= w.blocks) return;
+  int t0, t1;
+  ssm_rows(c, seq, t0, t1);
+  const int s = ssm_slot(c.src, seq, c.slots), g = (int)blockIdx.y, r0 = t0 + num * kSsmQ;
+  const int tid = (int)threadIdx.x, rows = min(kSsmQ, t1 - r0);
+  // a thread convolves one channel along a quarter of the chunk's rows, all of
+  // which are loaded at once (zeros before the sequence and past it)
+  constexpr int RUN = kSsmQ / 4;
+  for (int k = tid; k < 2 * NP * 4; k += 256) {
+    // (whole waves have the same rows: 64 divides 2 NP, or they are padding)
+    const int col = k % (2 * NP), run = __builtin_amdgcn_readfirstlane(k / (2 * NP)) * RUN;
+    const int n = col % NP;
+    const int ch = c.D + (col < NP ? 0 : c.G * c.N) + g * c.N + min(n, c.N - 1);
+    const int up = num == 0 && run == 0 ? 0 : 3, base = r0 + run - up;
+    const auto r = row_buffer<E>(c.xbc, base, c.xbc_stride, min(t1 - base, RUN + 3), c.C);
+    const unsigned xs = (unsigned)c.xbc_stride * (unsigned)sizeof(E), at = (unsigned)ch * (unsigned)sizeof(E);
+    float x[RUN + 3];
+#pragma unroll
+    for (int j = 0; j < RUN + 3; ++j) x[j] = load_one<E>(r, at + (unsigned)(j - 3 + up) * xs);
+    if (up == 0 && s >= 0) {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (3 - j < c.W)
+          x[j] = (float)static_cast<const E*>(c.window)[((size_t)s * (c.W - 1) + j - 3 + c.W - 1) * c.C + ch];
+    }
+    float tap[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tap[j] = 3 - j < c.W ? c.conv_w[(size_t)ch * c.W + c.W - 4 + j] : 0.f;
+    const float bias = c.conv_b[ch];
+    float* to = (col < NP ? lb : lc) + run * LD + n;
+    float v[RUN];
+#pragma unroll
+    for (int t = 0; t < RUN; ++t) v[t] = bias;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (3 - j >= c.W) continue;
+#pragma unroll
+      for (int t = 0; t < RUN; ++t) v[t] = fmaf(tap[j], x[t + j], v[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < RUN; ++t) to[t * LD] = run + t < rows && n < c.N ? silu(v[t]) : 0.f;
+  }
+  __syncthreads();
+  char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * Blk::BYTES;
+  const int lane = tid & 63, wv = tid >> 6, q = lane >> 4, l = lane & 15;
+  auto put = [&](int at, int step, float (&v)[8], auto parts) {
+    v8bf w[decltype(parts)::value];
+    split(v, w);
+#pragma unroll
+    for (int k = 0; k < decltype(parts)::value; ++k) reinterpret_cast<v8bf*>(out + at + k * step)[lane] = w[k];
+  };
+  const std::integral_constant<int, PY> py;
+  const std::integral_constant<int, kSsmParts> ps;
+  for (int f = wv; f < 4 * NT; f += 4) {
+    const int tt = f / NT, cc = f % NT;
+    const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
+    float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
+    put(Blk::c_at(tt, cc), Blk::PART, v, py);
+  }
+  for (int f = wv; f < 4 * NT; f += 4) {
+    const int a = f / 2, b = f % 2;
+    const float* p = lb + (32 * b + 4 * q) * LD + 16 * a + l;
+    float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
+    put(Blk::b_at(a, b), Blk::PART, v, ps);
+  }
+  // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
+  // are the lane's slots
+  for (int f = wv; f < 6; f += 4) {
+    const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
+    float v[8];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int st = 2 * cc + half;
+      v4f acc = {0.f, 0.f, 0.f, 0.f};
+      if (st <= tt) {
+        const float* pb = lb + (16 * st + l) * LD + q;
+        const float* pc = lc + (16 * tt + l) * LD + q;
+#pragma unroll 8
+        for (int k = 0; k < NP / 4; ++k)
+          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(pb[4 * k], pc[4 * k], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * half + i] = 16 * st + 4 * q + i <= 16 * tt + l ? acc[i] : 0.f;
+    }
+    put(Blk::g_at(f), Blk::GPART, v, py);
   }
 }
 
@@ -506,23 +507,31 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   };
   auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
   if (k0 < k1) {
-    if (AHEAD) load_rows(k0);
-    fetch_stage(k0, 0);
+    const int k = OUT ? k0 : k1 - 1;
+    if (AHEAD) load_rows(k);
+    fetch_stage(k, 0);
     arrived();
   }
 
   double total = 0.0;  // log2 of the segment's decay
-  for (int k = k0; k < k1; ++k) {
+  // A segment's own contribution is taken from its end: with the decay from there
+  // in w, its chunks only add up.
+  for (int turn = k0; turn < k1; ++turn) {
+    // (kept in a vector register otherwise)
+    const int k = __builtin_amdgcn_readfirstlane(OUT ? turn : k0 + k1 - 1 - turn);
+    const int next = OUT ? k + 1 : k - 1;
+    const bool more = turn + 1 < k1;
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
     if (!AHEAD) load_rows(k);
     lds_barrier();  // the stage before has been read, this one is there
     if (STAGES > 1)
       fetch_stage(k, 1);
-    else if (k + 1 < k1)
-      fetch_stage(k + 1, 0);
+    else if (more)
+      fetch_stage(next, 0);
     if (OUT) fetch_part(operands_of(k), Blk::G, Lds::G, Blk::GBYTES);
     const double* lq = w.lq + 2 * ((size_t)(block0 + k) * c.H + h);
     const double l0 = lq[0], l1 = lq[1];
+    const float f1 = OUT ? 1.f : exp2_hw((float)total), f0 = OUT ? 1.f : exp2_hw((float)(total + l1));
     total += l0 + l1;
     const bool fast = ssm_fast(l0, l1);
     const float dq0 = exp2_hw((float)l0), dq1 = exp2_hw((float)l1);
@@ -568,8 +577,12 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     }
     // u by a factor for every position, as the right operand of position block b
     auto operand = [&](const float* by, int b, int e, auto& to) {
-      const v4f w0 = *reinterpret_cast<const v4f*>(by + 32 * b + 4 * q);
-      const v4f w1 = *reinterpret_cast<const v4f*>(by + 32 * b + 16 + 4 * q);
+      v4f w0 = *reinterpret_cast<const v4f*>(by + 32 * b + 4 * q);
+      v4f w1 = *reinterpret_cast<const v4f*>(by + 32 * b + 16 + 4 * q);
+      if (!OUT) {
+        w0 *= b ? f1 : f0;
+        w1 *= b ? f1 : f0;
+      }
       float v[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -583,6 +596,13 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       for (int k = 0; k < (int)(sizeof(to) / sizeof(to[0])); ++k)
         to[k] = *reinterpret_cast<const v8bf*>(lds + at + k * step + lane * 16);
     };
+    v8bf xs[2][2][PS];  // w o x, made once where there are registers to keep it
+    if (!OUT) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) operand(pw, b, e, xs[b][e]);
+    }
     v4f y[4][2];
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
@@ -599,8 +619,8 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         lds_barrier();  // the stage before has been read, this one is there
         if (!final)
           fetch_stage(k, stage + 1);
-        else if (k + 1 < k1)
-          fetch_stage(k + 1, 0);
+        else if (more)
+          fetch_stage(next, 0);
       } else if (OUT && STAGES == 1) {
         arrived();
         lds_barrier();  // G is there
@@ -616,7 +636,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, from + i * zs);
           }
         }
-        if (AHEAD) load_rows(k + 1);  // (past the segment's end too: nothing then depends on them)
+        if (AHEAD) load_rows(OUT ? next : max(next, k0));  // (once more than is needed: nothing depends on them then)
       }
       if (OUT) {
         if (fast) {
@@ -660,7 +680,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
             }
         }
       }
-      if (!OUT || !fast) {
+      if (OUT && !fast) {
 #pragma unroll
         for (int a = a0; a < a1; ++a)
 #pragma unroll
@@ -671,8 +691,15 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         v8bf xp[2][PS], bp[2][PS];  // w o x; B
         frag(lds_b + b * 1024, Blk::PART, bp[0]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) operand(pw, b, e, xp[e]);
-        if (b) {
+        for (int e = 0; e < 2; ++e) {
+          if (OUT) {
+            operand(pw, b, e, xp[e]);
+          } else {
+#pragma unroll
+            for (int p = 0; p < PS; ++p) xp[e][p] = xs[b][e][p];
+          }
+        }
+        if (OUT && b) {
 #pragma unroll
           for (int a = a0; a < a1; ++a)
 #pragma unroll
@@ -865,7 +892,8 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
   hipError_t e = hipSuccess;
   if (w.blocks) {
-    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + (c.H + kSsmDecayHeads - 1) / kSsmDecayHeads)), dim3(256), 0, st, c, w);
+    hipLaunchKernelGGL(k_ssm_decays<E>, dim3((unsigned)w.blocks, (unsigned)(c.H + 3) / 4), dim3(256), 0, st, c, w);
+    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)c.G), dim3(256), 0, st, c, w);
     e = hipGetLastError();
   }
   auto allow = [&](const void* f, int bytes) {
