@@ -79,7 +79,7 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
 
 /* What a call reads and writes, rows of tokens in the context's type.  A row
  * is contiguous, rows are `_stride` elements apart (at least the row's
- * length, at most 2^25): slices of one wide projection's rows can be handed in as they are.
+ * length, at most 2^24): slices of one wide projection's rows can be handed in as they are.
  *   xbc [rows][D + 2 G N], dt [rows][H], z [rows][D] or NULL (no gate),
  *   y [rows][D] receives the outputs; it may be z itself (same stride), and
  *   overlaps nothing else.

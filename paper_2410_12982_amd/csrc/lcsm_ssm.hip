@@ -16,6 +16,35 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kSsmMaxN = 256;
 constexpr int kSsmMaxW = 4;
+// The value of the lane whose number differs in bit M.
+template <int M>
+__device__ __forceinline__ float xor_lane(float v) {
+  const int x = __builtin_bit_cast(int, v);
+  int r;
+  if constexpr (M == 1)
+    r = __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false);  // quad_perm 1 0 3 2
+  else if constexpr (M == 2)
+    r = __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false);  // quad_perm 2 3 0 1
+  else if constexpr (M == 8)
+    r = __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false);  // row_ror 8
+  else if constexpr (M < 32)
+    r = __builtin_amdgcn_ds_swizzle(x, M << 10 | 0x1f);
+  else
+    r = __shfl_xor(x, M);
+  return __builtin_bit_cast(float, r);
+}
+// Of 2 HALF sums, lanes with bit M keep the upper ones and lanes without the
+// lower ones, both with the other's share added.
+template <int M, int HALF>
+__device__ __forceinline__ void halve(float* y, int lane) {
+  const bool up = lane & M;
+#pragma unroll
+  for (int j = 0; j < HALF; ++j) {
+    const float mine = up ? y[j + HALF] : y[j], theirs = up ? y[j] : y[j + HALF];
+    y[j] = mine + xor_lane<M>(theirs);
+  }
+}
+
 // The recurrence as it is written, for single tokens and short prompts.  A
 // workgroup takes ROWS channels of a head of one sequence and keeps their states
 // in registers (L lanes a channel, four states each); TB positions at a time it
@@ -87,35 +116,52 @@ __global__ __launch_bounds__(256) void k_ssm_scan(SsmCall c) {
   for (int b = t0; b < t1; b += TB) {
     const int nt = min(TB, t1 - b);
     if (TB > 1 && b > t0) __syncthreads();  // the positions before have been read
-    for (int k = tid; k < NC; k += 256) {
-      const int ch = channel(k);
-      if (ch < 0) {
-        for (int t = 0; t < nt; ++t) su[t][k] = 0.f;
-        continue;
+    // a thread convolves a channel along RUN positions; the rows of all that it
+    // takes of them are on their way before the first is used
+    constexpr int RUN = TB < 8 ? TB : 8, ITEMS = NC * (TB / RUN), EACH = (ITEMS + 255) / 256;
+    constexpr int AT = TB == 1 ? 1 : EACH < 5 ? EACH : 5;  // (one token: registers count for more)
+    const int up = b == t0 ? 0 : 3;  // rows between the base and row b; those before t0 are the window's
+    const auto rows = row_buffer<E>(c.xbc, (size_t)(b - up), c.xbc_stride, nt + up, c.C);
+    const unsigned xs = (unsigned)c.xbc_stride * (unsigned)sizeof(E);
+#pragma unroll 1
+    for (int e0 = 0; e0 < EACH; e0 += AT) {
+      float v[AT][RUN + 3];
+#pragma unroll
+      for (int e = 0; e < AT; ++e) {
+        const int it = (e0 + e) * 256 + tid, run = it / NC * RUN, ch = max(channel(it % NC), 0);
+        const unsigned at = (unsigned)ch * (unsigned)sizeof(E) + (unsigned)(run - 3 + up) * xs;
+#pragma unroll
+        for (int j = 0; j < RUN + 3; ++j) v[e][j] = load_one<E>(rows, at + (unsigned)j * xs);
+        if (up == 0 && run == 0 && s >= 0) {
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (3 - j < c.W) v[e][j] = (float)win[((size_t)s * W1 + j - 3 + W1) * c.C + ch];
+        }
       }
-      float tap[4], v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) tap[j] = 3 - j < c.W ? c.conv_w[(size_t)ch * c.W + c.W - 4 + j] : 0.f;
-      const float bias = c.conv_b[ch];
+      for (int e = 0; e < AT; ++e) {
+        const int it = (e0 + e) * 256 + tid, k = it % NC, run = it / NC * RUN, ch = channel(k);
+        float tap[4];
 #pragma unroll
-      for (int j = 0; j < 3; ++j)
-        if (3 - j < c.W) v[j] = (float)raw(b - 3 + j, ch);
-#pragma unroll 8
-      for (int t = 0; t < nt; ++t) {
-        v[3] = (float)x[(size_t)(b + t) * c.xbc_stride + ch];
-        float a = bias;
+        for (int j = 0; j < 4; ++j) tap[j] = 3 - j < c.W ? c.conv_w[(size_t)max(ch, 0) * c.W + c.W - 4 + j] : 0.f;
+        const float bias = c.conv_b[max(ch, 0)];
+        if (it >= ITEMS) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (3 - j < c.W) a = fmaf(tap[j], v[j], a);
-        su[t][k] = silu(a);
-        v[0] = v[1], v[1] = v[2], v[2] = v[3];
+        for (int t = 0; t < RUN; ++t) {
+          float a = bias;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (3 - j < c.W) a = fmaf(tap[j], v[e][t + j], a);
+          if (run + t < TB) su[run + t][k] = ch < 0 || run + t >= nt ? 0.f : silu(a);
+        }
       }
     }
-    if (tid < nt) {
-      const float step =
-          softplus((float)static_cast<const E*>(c.dt)[(size_t)(b + tid) * c.dt_stride + h] + c.dt_bias[h]);
+    if (tid < TB) {  // positions past the last one leave the states as they are
+      float step = 0.f;
+      if (tid < nt)
+        step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(b + tid) * c.dt_stride + h] + c.dt_bias[h]);
       sstep[tid] = step;
-      sdecay[tid] = __expf(step * c.A[h]);
+      sdecay[tid] = tid < nt ? __expf(step * c.A[h]) : 1.f;
     }
     __syncthreads();
     if constexpr (TB == 1) {
@@ -133,9 +179,14 @@ __global__ __launch_bounds__(256) void k_ssm_scan(SsmCall c) {
         y[r] = fmaf(C.x, S[r][0], fmaf(C.y, S[r][1], fmaf(C.z, S[r][2], C.w * S[r][3])));
       }
 #pragma unroll
-      for (int m = L / 2; m >= 1; m /= 2)
-#pragma unroll
-        for (int r = 0; r < R; ++r) y[r] += __shfl_xor(y[r], m);
+      for (int r = 0; r < R; ++r) {
+        y[r] += xor_lane<1>(y[r]);
+        y[r] += xor_lane<2>(y[r]);
+        if constexpr (L >= 8) y[r] += xor_lane<4>(y[r]);
+        if constexpr (L >= 16) y[r] += xor_lane<8>(y[r]);
+        if constexpr (L >= 32) y[r] += xor_lane<16>(y[r]);
+        if constexpr (L >= 64) y[r] += xor_lane<32>(y[r]);
+      }
       if (tid % L == 0)
 #pragma unroll
         for (int r = 0; r < R; ++r) sy[0][r0 + r * RPP] = y[r];
@@ -145,51 +196,42 @@ __global__ __launch_bounds__(256) void k_ssm_scan(SsmCall c) {
         float y[R][U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          // positions past the last one leave the states as they are
-          const bool in = u0 + u < nt;
-          const int t = in ? u0 + u : nt - 1;
+          const int t = u0 + u;
           const float step = sstep[t], decay = sdecay[t];
           const float4 B = *reinterpret_cast<const float4*>(&su[t][ROWS + n0]);
           const float4 C = *reinterpret_cast<const float4*>(&su[t][ROWS + NP + n0]);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const float dx = step * su[t][r0 + r * RPP];
-            if (in) {
-              S[r][0] = fmaf(S[r][0], decay, dx * B.x);
-              S[r][1] = fmaf(S[r][1], decay, dx * B.y);
-              S[r][2] = fmaf(S[r][2], decay, dx * B.z);
-              S[r][3] = fmaf(S[r][3], decay, dx * B.w);
-            }
+            S[r][0] = fmaf(S[r][0], decay, dx * B.x);
+            S[r][1] = fmaf(S[r][1], decay, dx * B.y);
+            S[r][2] = fmaf(S[r][2], decay, dx * B.z);
+            S[r][3] = fmaf(S[r][3], decay, dx * B.w);
             y[r][u] = fmaf(C.x, S[r][0], fmaf(C.y, S[r][1], fmaf(C.z, S[r][2], C.w * S[r][3])));
           }
         }
-        // lanes that differ in bit 0, 1, 2 share the eight sums among them
+        // lanes that differ in bit 0, 1, 3 (2 where there is none) share the eight
+        // sums among them
         const int lane = tid % L;
-        constexpr int HALVE = L >= 8 ? 3 : 2;
+        constexpr int M2 = L >= 16 ? 8 : 4, HALVE = L >= 8 ? 3 : 2, HAVE = U >> HALVE;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+          halve<1, 4>(y[r], lane);
+          halve<2, 2>(y[r], lane);
+          if constexpr (L >= 8) halve<M2, 1>(y[r], lane);
 #pragma unroll
-          for (int k = 0; k < HALVE; ++k) {
-            const int m = 1 << k, half = U >> (k + 1);
-            const bool up = lane & m;
-#pragma unroll
-            for (int j = 0; j < half; ++j) {
-              const float mine = up ? y[r][j + half] : y[r][j], theirs = up ? y[r][j] : y[r][j + half];
-              y[r][j] = mine + __shfl_xor(theirs, m);
-            }
+          for (int j = 0; j < HAVE; ++j) {
+            if constexpr (L >= 16) y[r][j] += xor_lane<4>(y[r][j]);
+            if constexpr (L >= 32) y[r][j] += xor_lane<16>(y[r][j]);
+            if constexpr (L >= 64) y[r][j] += xor_lane<32>(y[r][j]);
           }
+        }
+        const int u = (lane & 1 ? 4 : 0) + (lane & 2 ? 2 : 0) + (L >= 8 && lane & M2 ? 1 : 0);
+        if ((lane & ~(3 | (L >= 8 ? M2 : 0))) == 0) {
 #pragma unroll
-          for (int m = 1 << HALVE; m < L; m *= 2)
+          for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int j = 0; j < (U >> HALVE); ++j) y[r][j] += __shfl_xor(y[r][j], m);
-          if ((lane >> HALVE) == 0) {
-            int u = 0;
-#pragma unroll
-            for (int k = 0; k < HALVE; ++k) u += lane & (1 << k) ? U >> (k + 1) : 0;
-#pragma unroll
-            for (int j = 0; j < (U >> HALVE); ++j)
-              if (u0 + u + j < nt) sy[u0 + u + j][r0 + r * RPP] = y[r][j];
-          }
+            for (int j = 0; j < HAVE; ++j) sy[u0 + u + j][r0 + r * RPP] = y[r][j];
         }
       }
     }
@@ -301,9 +343,10 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
 }
 
 // Up to so many tokens a prompt call goes through k_ssm_scan.  One prompt of 32
-// heads x 64 x 128 takes 19 us for 29 tokens, 60 for 128, 114 for 256 with it,
-// and in chunks 41 for 29, 89 for 513 to 1024.
-constexpr int kSsmScanTokens = 192;
+// heads x 64 x 128 takes 14 us for 29 tokens, 37 for 128, 66 for 256 with it (a
+// quarter of a microsecond a token), and in chunks 66 for 256, 69 for 512, 76 for
+// 1024.
+constexpr int kSsmScanTokens = 256;
 
 // How a prompt call is cut: segments of `per` chunks so that about one
 // workgroup per compute unit is on its way, which is what LDS holds; sequences
@@ -431,7 +474,7 @@ int ssm_call(lcsm_ssm* c, int layer, int T, int n, const lcsm_ssm_io* io, lcsm::
         (io->z && io->z_stride < (size_t)c->D))
       return ssm_fail(c, LCSM_EINVAL, "a row stride is shorter than the row");
     for (size_t stride : {io->xbc_stride, io->dt_stride, io->y_stride, io->z ? io->z_stride : 0})
-      if (stride > lcsm::kSsmMaxStride) return ssm_fail(c, LCSM_EINVAL, "a row stride is above 2^25 elements");
+      if (stride > lcsm::kSsmMaxStride) return ssm_fail(c, LCSM_EINVAL, "a row stride is above 2^24 elements");
   }
   if (c->faulted) return LCSM_ESTATE;
   const size_t m = (size_t)layer, C = (size_t)c->C, H = (size_t)c->s.H;

@@ -37,10 +37,35 @@ __device__ __forceinline__ void ssm_rows(const SsmCall& c, int i, int& t0, int& 
   }
 }
 
+constexpr size_t kSsmMaxStride = (size_t)1 << 24;  // elements between rows
+
+// A buffer that is the same for all lanes (which the compiler does not always
+// see, and then loops over the lanes' values at every access).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_buffer(const void* p, unsigned bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)at), hi = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0,
+                                           __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
+}
+
+// Rows as a buffer of whole rows from a base row on: what lies past its end
+// reads as zero and is not stored.  `rows` of them, `width` elements in the
+// last; kSsmMaxStride keeps the offsets of 40 rows of fp32 below 2^32.
+template <class E>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size_t row, size_t stride, int rows,
+                                                             int width) {
+  const unsigned bytes = rows > 0 ? (unsigned)((rows - 1) * stride + width) * (unsigned)sizeof(E) : 0u;
+  return uniform_buffer(static_cast<const E*>(p) + row * stride, bytes);
+}
+template <class E>
+__device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, unsigned at) {
+  if constexpr (sizeof(E) == 4) return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+  else return (float)__builtin_bit_cast(E, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
+}
+
 // ---- prompts in chunks (lcsm_ssm_prompt.h)
 
 constexpr int kSsmQ = 64;  // positions of a chunk
-constexpr size_t kSsmMaxStride = (size_t)1 << 25;  // elements between rows: 25 rows of fp32 stay below 2^32 bytes
 
 // bf16 parts of a value in products that end in fp32 (states, fp32 outputs), and
 // in those whose sum is rounded to 16 bits.

@@ -900,13 +900,15 @@ class Ssm(_LayerContext):
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
 
     def _fill(self, rows, n, xbc, dt, z, y, src, dst):
-        io, dtype = self._io, self.dtype
-        if y is None:
-            y = torch.empty((rows, self.D), dtype=dtype, device=self.device)
+        io, dtype, D = self._io, self.dtype, self.D
         io.xbc, io.xbc_stride = self._rows(xbc, rows, self.C, dtype, "xbc")
         io.dt, io.dt_stride = self._rows(dt, rows, self.H, dtype, "dt")
-        io.z, io.z_stride = (None, 0) if z is None else self._rows(z, rows, self.D, dtype, "z")
-        io.y, io.y_stride = self._rows(y, rows, self.D, dtype, "y")
+        io.z, io.z_stride = (None, 0) if z is None else self._rows(z, rows, D, dtype, "z")
+        if y is None:
+            y = xbc.new_empty(rows, D)  # (a tuple, a type or a device would cost half a microsecond each)
+            io.y, io.y_stride = y.data_ptr(), D
+        else:
+            io.y, io.y_stride = self._rows(y, rows, D, dtype, "y")
         io.src, io.dst = self._slots(src, n, "src"), self._slots(dst, n, "dst")
         self._order()
         return y
@@ -976,16 +978,20 @@ class Norm(_LayerContext):
         """(r', n) of the rows o (None: no block before), res and gate, all [rows, D].  ``res_out`` and ``out`` receive
         them where given; False: that one is not wanted (None is returned for it)."""
         rows, D, io = res.shape[0], self.D, self._io
-        if res_out is None:
-            res_out = torch.empty((rows, D), dtype=self.res_dtype, device=self.device)
-        if out is None:
-            out = torch.empty((rows, D), dtype=self.dtype, device=self.device)
         io.r, io.r_stride = self._rows(res, rows, D, self.res_dtype, "res")
         io.o, io.o_stride = (None, 0) if o is None else self._rows(o, rows, D, self.dtype, "o")
         io.g, io.g_stride = (None, 0) if gate is None else self._rows(gate, rows, D, self.dtype, "gate")
-        io.r_out, io.r_out_stride = ((None, 0) if res_out is False
-                                     else self._rows(res_out, rows, D, self.res_dtype, "res_out"))
-        io.n, io.n_stride = (None, 0) if out is False else self._rows(out, rows, D, self.dtype, "out")
+        if res_out is None:
+            res_out = res.new_empty(rows, D)
+            io.r_out, io.r_out_stride = res_out.data_ptr(), D
+        else:
+            io.r_out, io.r_out_stride = ((None, 0) if res_out is False
+                                         else self._rows(res_out, rows, D, self.res_dtype, "res_out"))
+        if out is None:
+            out = (o if o is not None else res).new_empty(rows, D, dtype=self.dtype)
+            io.n, io.n_stride = out.data_ptr(), D
+        else:
+            io.n, io.n_stride = (None, 0) if out is False else self._rows(out, rows, D, self.dtype, "out")
         self._order()
         r = _lib.lcsm_norm_block(self._ctx, layer, rows, self._io_ref)
         if r:
@@ -1028,10 +1034,12 @@ class Q4(_LayerContext):
     def matvec(self, layer, x, y=None):
         """y [rows, N] = x [rows, K] times the layer's matrix, in x's type."""
         rows, dtype = x.shape[0], x.dtype
-        if y is None:
-            y = torch.empty((rows, self.N), dtype=dtype, device=self.device)
         px, sx = self._rows(x, rows, self.K, dtype, "x")
-        py, sy = self._rows(y, rows, self.N, dtype, "y")
+        if y is None:
+            y = x.new_empty(rows, self.N)
+            py, sy = y.data_ptr(), self.N
+        else:
+            py, sy = self._rows(y, rows, self.N, dtype, "y")
         self._order()
         r = _lib.lcsm_q4_matvec(self._ctx, layer, rows, _dtype_code(dtype), px, sx, py, sy)
         if r:
