@@ -55,9 +55,9 @@ typedef struct lcsm_ssm_shape {
 } lcsm_ssm_shape;
 
 /* Device bytes of the workspace: the states 4 M slots H P N, the windows,
- * copies of the parameters, and for prompts 3 H + 2 fp32 values and G N + 64
- * values a token (rounded up in pieces of 64 tokens of every sequence) and
- * the states of the pieces that a call is split into.  Host only.
+ * copies of the parameters, and for prompt calls beyond 256 tokens what all
+ * heads share of every 64 tokens (about 12 G N + 300 G + 17 H bytes a token) and
+ * the states of the segments that a call is cut into.  Host only.
  * Errors: LCSM_EINVAL for a bad shape (sizes < 1, P > 4096, N > 256, W > 4, G not a
  * divisor of H, an unknown type, D + 2 G N > 2^24, slots > 65535,
  * max_tokens < 0 or > 2^26, or a workspace beyond 2^46 bytes). */
@@ -79,7 +79,8 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
 
 /* What a call reads and writes, rows of tokens in the context's type.  A row
  * is contiguous, rows are `_stride` elements apart (at least the row's
- * length, at most 2^24): slices of one wide projection's rows can be handed in as they are.
+ * length, at most 2^24): slices of one wide projection's rows can be handed in
+ * as they are.
  *   xbc [rows][D + 2 G N], dt [rows][H], z [rows][D] or NULL (no gate),
  *   y [rows][D] receives the outputs; it may be z itself (same stride), and
  *   overlaps nothing else.

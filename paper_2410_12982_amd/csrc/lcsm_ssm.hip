@@ -348,10 +348,10 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
 // 1024.
 constexpr int kSsmScanTokens = 256;
 
-// How a prompt call is cut: segments of `per` chunks so that about one
-// workgroup per compute unit is on its way, which is what LDS holds; sequences
-// that are that many by themselves are not cut.
-constexpr int kSsmWorkgroups = 256;
+// How a prompt call is cut: segments of `per` chunks so that about as many
+// workgroups are on their way as there is room for at once (two or one a compute
+// unit); sequences that are that many by themselves are not cut.
+constexpr int ssm_workgroups(int N) { return N <= 64 ? 512 : 256; }
 
 int head_groups(int H, int G, int P, int N) {
   const int items = H / G * ((P + 31) / 32), nw = items < ssm_waves(N) ? items : ssm_waves(N);
@@ -361,20 +361,19 @@ int head_groups(int H, int G, int P, int N) {
 // of all chunks and one more for each of fewer than `want` sequences; `cuts`:
 // chunks and sequences of the largest call.
 size_t most_segments(int H, int G, int P, int N, size_t cuts) {
-  const size_t most = 2 * (size_t)kSsmWorkgroups / head_groups(H, G, P, N) + 2;
+  const size_t most = 2 * (size_t)ssm_workgroups(N) / head_groups(H, G, P, N) + 2;
   return most < cuts ? most : cuts;
 }
 
 hipError_t launch_prompt(const SsmCall& c, int dtype, SsmScratch w, hipStream_t st) {
   w.blocks = c.T / kSsmQ + c.n;  // a sequence's last chunk may be short
-  const int wgs = head_groups(c.H, c.G, c.P, c.N), want = kSsmWorkgroups / wgs;
+  const int wgs = head_groups(c.H, c.G, c.P, c.N), want = ssm_workgroups(c.N) / wgs;
   w.per = want > c.n ? (w.blocks + want - 1) / want : w.blocks;
   w.segments = want > c.n ? w.blocks / w.per + c.n : c.n;
   const size_t e = dtype_size(dtype);
   auto two = [&](const void* p, size_t stride) { return !p || ((uintptr_t)p % (2 * e) == 0 && stride % 2 == 0); };
   w.pair = c.P % 2 == 0 && two(c.xbc, c.xbc_stride) && two(c.z, c.z_stride) && two(c.y, c.y_stride);
   w.quads = c.N % 4 == 0;
-  if (c.T == 0) w.blocks = 0;
   hipError_t r = dtype == LCSM_F32 ? ssm_prompt_f32(c, w, st)
                  : dtype == LCSM_BF16 ? ssm_prompt_bf16(c, w, st) : ssm_prompt_f16(c, w, st);
   if (r != hipSuccess || c.W == 1) return r;
@@ -437,7 +436,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   take(&p->A, M * H * 4);
   take(&p->skip, M * H * 4);
   take(&p->dt_bias, M * H * 4);
-  if (s->max_tokens) {
+  if (s->max_tokens > lcsm::kSsmScanTokens) {
     const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
     const size_t each = lcsm::ssm_block_bytes(s->N, lcsm::dtype_size(s->dtype));
     const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
@@ -532,7 +531,7 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
   c->A = (float*)(c->mem + p.A);
   c->skip = (float*)(c->mem + p.skip);
   c->dt_bias = (float*)(c->mem + p.dt_bias);
-  if (shape->max_tokens) {
+  if (shape->max_tokens > lcsm::kSsmScanTokens) {
     c->scratch.bc = c->mem + p.bc;
     c->scratch.scal = (float*)(c->mem + p.scal);
     c->scratch.lq = (double*)(c->mem + p.lq);

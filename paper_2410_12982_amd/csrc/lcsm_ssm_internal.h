@@ -88,16 +88,21 @@ struct SsmBlock {
   static constexpr int g_at(int f) { return G + f * 1024; }
 };
 
-// What a workgroup of `waves` keeps in LDS: two stages (C and B; B alone where
-// only the states are wanted), so that the next one is fetched while one is
-// used, G of the chunk, and twice what each wave's positions have of its head.
+// What a workgroup of `waves` keeps in LDS: a stage (C and B; B alone where only
+// the states are wanted), G of the chunk, and what each wave's positions have of
+// its head.  TWICE: two of the first and the last, so that the next ones are
+// fetched while these are used; where they are small, two workgroups a compute
+// unit take turns instead (4 x 2048 tokens of 24 heads x 64 x 64 in fp32 103
+// against 109 us; 16384 tokens of 64 heads x 64 x 128 401 twice, 440 once and four
+// waves).
 template <int NT, int PY, bool OUT>
 struct SsmLds {
   typedef SsmBlock<NT, PY> Blk;
   static constexpr int C = OUT ? PY * Blk::PART : 0, STAGE = C + kSsmParts * Blk::PART;
-  static constexpr int G = 2 * STAGE, WAVES = G + (OUT ? Blk::GBYTES : 0);
+  static constexpr bool TWICE = NT > 2;
+  static constexpr int G = (TWICE ? 2 : 1) * STAGE, WAVES = G + (OUT ? Blk::GBYTES : 0);
   static constexpr int SCAL = 4 * kSsmQ * (int)sizeof(float);
-  static constexpr int bytes(int waves) { return WAVES + 2 * waves * SCAL; }
+  static constexpr int bytes(int waves) { return WAVES + (TWICE ? 2 : 1) * waves * SCAL; }
 };
 
 inline int ssm_blocks_of(int N) { return N <= 32 ? 1 : N <= 64 ? 2 : N <= 128 ? 4 : 8; }
@@ -106,8 +111,8 @@ inline size_t ssm_block_bytes(int N, size_t elem) {
   return (size_t)4096 * nt * (py + kSsmParts) + (size_t)py * 6144;
 }
 // Waves of a workgroup, 32 channels of a head each: they share the operands in
-// LDS, and have the registers of a compute unit to themselves.
-inline int ssm_waves(int N) { return N <= 128 ? 8 : 4; }
+// LDS.  256 registers are what they have up to N = 128, 512 above.
+inline int ssm_waves(int N) { return N > 64 && N <= 128 ? 8 : 4; }
 
 struct SsmScratch {
   char* bc;       // [blocks][G] SsmBlock

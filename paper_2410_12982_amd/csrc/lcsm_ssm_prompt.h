@@ -329,7 +329,7 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
 template <class E, int NT, bool OUT, bool PAIR>
-__global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, SsmScratch w) {
+__global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
   typedef SsmBlock<NT, PY> Blk;
   typedef SsmLds<NT, PY, OUT> Lds;
@@ -474,8 +474,8 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   auto operands_of = [&](int k) {
     return uniform_buffer(w.bc + ((size_t)(block0 + k) * c.G + g) * Blk::BYTES, Blk::BYTES);
   };
-  auto stage_at = [&](int k, int stage) { return (k * STAGES + stage) % 2 * Lds::STAGE; };
-  auto scal_at = [&](int k) { return Lds::WAVES + (k % 2 * nw + wv) * Lds::SCAL; };
+  auto stage_at = [&](int k, int stage) { return Lds::TWICE ? (k * STAGES + stage) % 2 * Lds::STAGE : 0; };
+  auto scal_at = [&](int k) { return Lds::WAVES + ((Lds::TWICE ? k % 2 * nw : 0) + wv) * Lds::SCAL; };
   // stage `stage` of chunk k; with the first one what the positions have, with
   // the last one G
   auto fetch_stage = [&](int k, int stage) {
@@ -486,8 +486,10 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
   if (k0 < k1) {
     const int k = OUT ? k0 : k1 - 1;
     if (AHEAD) load_rows(k);
-    fetch_stage(k, 0);
-    arrived();
+    if (Lds::TWICE) {
+      fetch_stage(k, 0);
+      arrived();
+    }
   }
 
   double total = 0.0;  // log2 of the segment's decay
@@ -500,8 +502,10 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
     const bool more = turn + 1 < k1;
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
     if (!AHEAD) load_rows(k);
-    lds_barrier();  // the stage before has been read, this one is there
-    if (STAGES > 1)
+    lds_barrier();  // the stage before has been read (TWICE: this one is there)
+    if (!Lds::TWICE)
+      fetch_stage(k, 0);
+    else if (STAGES > 1)
       fetch_stage(k, 1);
     else if (more)
       fetch_stage(next, 0);
@@ -591,7 +595,14 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
       constexpr int NF = 4 * NB;  // fragments of C
       const int a0 = 2 * stage * NB, a1 = a0 + 2 * NB, lds_c = stage_at(k, stage), lds_b = lds_c + Lds::C;
       const bool final = stage == STAGES - 1;
-      if (stage > 0) {
+      if (!Lds::TWICE) {
+        if (stage > 0) {
+          lds_barrier();
+          fetch_stage(k, stage);
+        }
+        arrived();
+        lds_barrier();
+      } else if (stage > 0) {
         arrived();
         lds_barrier();  // the stage before has been read, this one is there
         if (!final)
@@ -751,7 +762,7 @@ __global__ __launch_bounds__(NT > 4 ? 256 : 512) void k_ssm_chunks(SsmCall c, Ss
         }
       }
     }
-    arrived();  // the next chunk's first stage, before the stores are on their way
+    if (Lds::TWICE) arrived();  // the next chunk's first stage, before the stores are on their way
     if (!OUT) continue;
     if (__ballot(bad[0] < kSsmQ || bad[1] < kSsmQ)) {
 #pragma unroll
