@@ -61,7 +61,8 @@ int lcsm_q4_init(lcsm_q4** out, const lcsm_q4_shape* shape, const void* codes, c
 
 /* y [rows][N] = x [rows][K] times the layer's matrix, both of type dtype; a
  * row is contiguous, rows are `_stride` elements apart.  x and y do not
- * overlap.  rows = 0 queues nothing.  Errors: LCSM_EINVAL (null pointers,
+ * overlap.  rows = 0 queues nothing, more than 2^20 - 16 are refused.
+ * Errors: LCSM_EINVAL (null pointers,
  * layer, rows, dtype or strides out of range), LCSM_ESTATE after a fault
  * (until lcsm_q4_reset), LCSM_EDEVICE. */
 int lcsm_q4_matvec(lcsm_q4* ctx, int layer, int rows, int dtype, const void* x, size_t x_stride,

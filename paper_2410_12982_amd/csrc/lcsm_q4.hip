@@ -529,7 +529,7 @@ int lcsm_q4_matvec(lcsm_q4* ctx, int layer, int rows, int dtype, const void* x, 
     if (!x || !y) return q4_fail(ctx, LCSM_EINVAL, "null input or output pointer");
     if (x_stride < (size_t)s.K || y_stride < (size_t)s.N)
       return q4_fail(ctx, LCSM_EINVAL, "a row stride is shorter than the row");
-    if (rows > 65535 * 64) return q4_fail(ctx, LCSM_EINVAL, "too many rows");
+    if (rows > 65535 * 16) return q4_fail(ctx, LCSM_EINVAL, "too many rows");
   }
   if (ctx->faulted) return LCSM_ESTATE;
   if (!rows) return LCSM_OK;
