@@ -358,7 +358,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
   for (int i = lane; i < seq; i += 64) {
     int a, b;
     ssm_rows(c, i, a, b);
-    block0 += (b - a + kSsmQ - 1) / kSsmQ;
+    block0 = min(block0 + (b - a + kSsmQ - 1) / kSsmQ, w.blocks);  // (wrong offsets do not overflow it)
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) block0 += __shfl_xor(block0, m);
@@ -832,7 +832,7 @@ inline __device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScrat
   for (int i = (int)threadIdx.x & 63; i < seq; i += 64) {
     int a, b;
     ssm_rows(c, i, a, b);
-    base += max(((b - a + kSsmQ - 1) / kSsmQ + w.per - 1) / w.per, 1);
+    base = min(base + max(((b - a + kSsmQ - 1) / kSsmQ + w.per - 1) / w.per, 1), w.segments);
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) base += __shfl_xor(base, m);
