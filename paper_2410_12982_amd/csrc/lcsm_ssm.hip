@@ -289,33 +289,6 @@ __global__ __launch_bounds__(256) void k_ssm_scan(SsmCall c) {
   }
 }
 
-// The windows after a call: a thread per sequence and channel.
-template <class E>
-__global__ __launch_bounds__(256) void k_ssm_window(SsmCall c) {
-  const int ch = (int)blockIdx.x * 256 + (int)threadIdx.x, i = (int)blockIdx.y;
-  if (ch >= c.C) return;
-  int t0, t1;
-  ssm_rows(c, i, t0, t1);
-  const int s = ssm_slot(c.src, i, c.slots), d = ssm_slot(c.dst, i, c.slots);
-  if (d < 0) return;
-  const E* x = static_cast<const E*>(c.xbc);
-  E* w = static_cast<E*>(c.window);
-  E v[kSsmMaxW - 1];
-#pragma unroll
-  for (int k = 0; k < kSsmMaxW - 1; ++k) {
-    v[k] = (E)0.f;
-    if (k >= c.W - 1) continue;
-    const int tt = t1 - (c.W - 1) + k;
-    if (tt >= t0)
-      v[k] = x[(size_t)tt * c.xbc_stride + ch];
-    else if (s >= 0)
-      v[k] = w[((size_t)s * (c.W - 1) + (tt - t0 + c.W - 1)) * c.C + ch];
-  }
-#pragma unroll
-  for (int k = 0; k < kSsmMaxW - 1; ++k)
-    if (k < c.W - 1) w[((size_t)d * (c.W - 1) + k) * c.C + ch] = v[k];
-}
-
 template <class E, int L, int R, int TB>
 hipError_t launch_scan_of(const SsmCall& c, hipStream_t st) {
   constexpr int ROWS = R * 256 / L;
@@ -374,15 +347,7 @@ hipError_t launch_prompt(const SsmCall& c, int dtype, SsmScratch w, hipStream_t 
   auto two = [&](const void* p, size_t stride) { return !p || ((uintptr_t)p % (2 * e) == 0 && stride % 2 == 0); };
   w.pair = c.P % 2 == 0 && two(c.xbc, c.xbc_stride) && two(c.z, c.z_stride) && two(c.y, c.y_stride);
   w.quads = c.N % 4 == 0;
-  hipError_t r = dtype == LCSM_F32 ? ssm_prompt_f32(c, w, st)
-                 : dtype == LCSM_BF16 ? ssm_prompt_bf16(c, w, st) : ssm_prompt_f16(c, w, st);
-  if (r != hipSuccess || c.W == 1) return r;
-  const dim3 grid((unsigned)((c.C + 255) / 256), (unsigned)c.n);
-  with_dtype(dtype, [&](auto v) {
-    hipLaunchKernelGGL(k_ssm_window<decltype(v)>, grid, dim3(256), 0, st, c);
-    return 0;
-  });
-  return hipGetLastError();
+  return dtype == LCSM_F32 ? ssm_prompt_f32(c, w, st) : dtype == LCSM_BF16 ? ssm_prompt_bf16(c, w, st) : ssm_prompt_f16(c, w, st);
 }
 
 }  // namespace
@@ -408,7 +373,7 @@ namespace {
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
-  size_t state, window, tickets, conv_w, conv_b, A, skip, dt_bias, bc, scal, lq, states, decay, total;
+  size_t state, window, tickets, conv_w, conv_b, A, skip, dt_bias, windows, bc, scal, lq, states, decay, total;
 };
 
 bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
@@ -442,6 +407,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
     const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
     if ((double)blocks * (s->G * (double)each + H * 2048.0) + (double)segments * D * s->N * 4 > 70368744177664.0)
       return false;
+    take(&p->windows, (size_t)s->slots * (s->W - 1) * c * lcsm::dtype_size(s->dtype));
     take(&p->bc, blocks * s->G * each);
     take(&p->scal, blocks * H * 4 * lcsm::kSsmQ * 4);
     take(&p->lq, blocks * H * 16);
@@ -532,6 +498,7 @@ int lcsm_ssm_init(lcsm_ssm** out, const lcsm_ssm_shape* shape, const float* conv
   c->skip = (float*)(c->mem + p.skip);
   c->dt_bias = (float*)(c->mem + p.dt_bias);
   if (shape->max_tokens > lcsm::kSsmScanTokens) {
+    c->scratch.windows = c->mem + p.windows;
     c->scratch.bc = c->mem + p.bc;
     c->scratch.scal = (float*)(c->mem + p.scal);
     c->scratch.lq = (double*)(c->mem + p.lq);

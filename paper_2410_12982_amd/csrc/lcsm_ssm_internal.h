@@ -115,6 +115,7 @@ inline size_t ssm_block_bytes(int N, size_t elem) {
 inline int ssm_waves(int N) { return N > 64 && N <= 128 ? 8 : 4; }
 
 struct SsmScratch {
+  void* windows;  // [sequences][W-1][C]: the windows that the call begins from
   char* bc;       // [blocks][G] SsmBlock
   float* scal;    // [blocks][H][4][64]: what a chunk's positions have of a head
   double* lq;     // [blocks][H][2]: log2 of the decays of a chunk's halves

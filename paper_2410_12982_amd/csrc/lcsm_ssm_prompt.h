@@ -182,56 +182,103 @@ __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, un
 // the chunk is `fast`, else step and l in two parts.
 __device__ __forceinline__ bool ssm_fast(double l0, double l1) { return fabs(l0) < 64.0 && fabs(l1) < 64.0; }
 
+constexpr int kSsmHeads = 4;  // heads a wave, at once
+
 template <class E>
-__device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h) {
+__device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h0) {
   const int lane = (int)threadIdx.x & 63;
-  float step = 0.f;
-  if (lane < rows)
-    step = softplus((float)static_cast<const E*>(c.dt)[(size_t)(r0 + lane) * c.dt_stride + h] + c.dt_bias[h]);
-  // fp64: l reaches thousands where steps are long, and its differences count
-  double l = (double)(step * c.A[h]) * 1.4426950408889634;
+  float step[kSsmHeads];
+  double l[kSsmHeads];  // fp64: l reaches thousands where steps are long, and its differences count
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const double v = __shfl_up(l, m);
-    if (lane >= m) l += v;
+  for (int j = 0; j < kSsmHeads; ++j)
+    step[j] = (float)static_cast<const E*>(c.dt)[(size_t)(r0 + min(lane, rows - 1)) * c.dt_stride + min(h0 + j, c.H - 1)];
+#pragma unroll
+  for (int j = 0; j < kSsmHeads; ++j) {
+    const int h = min(h0 + j, c.H - 1);
+    step[j] = lane < rows ? softplus(step[j] + c.dt_bias[h]) : 0.f;
+    l[j] = (double)(step[j] * c.A[h]) * 1.4426950408889634;
   }
-  const double l0 = __shfl(l, 31), lq = __shfl(l, 63), le = lane < 32 ? l0 : lq;
-  const size_t at = (size_t)block * c.H + h;
-  float* to = w.scal + at * 4 * kSsmQ + lane;
-  to[0] = step * exp2_hw((float)(le - l));
-  const float hi = (float)l;
-  to[kSsmQ] = ssm_fast(l0, lq - l0) ? exp2_hw((float)(l - le)) : step;
-  to[2 * kSsmQ] = hi;
-  to[3 * kSsmQ] = (float)(l - (double)hi);
-  if (lane < 2) w.lq[2 * at + lane] = lane ? lq - l0 : l0;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2)
+#pragma unroll
+    for (int j = 0; j < kSsmHeads; ++j) {
+      const double v = __shfl_up(l[j], m);
+      if (lane >= m) l[j] += v;
+    }
+#pragma unroll
+  for (int j = 0; j < kSsmHeads; ++j) {
+    if (h0 + j >= c.H) break;
+    const double l0 = __shfl(l[j], 31), lq = __shfl(l[j], 63), le = lane < 32 ? l0 : lq;
+    const size_t at = (size_t)block * c.H + h0 + j;
+    float* to = w.scal + at * 4 * kSsmQ + lane;
+    to[0] = step[j] * exp2_hw((float)(le - l[j]));
+    const float hi = (float)l[j];
+    to[kSsmQ] = ssm_fast(l0, lq - l0) ? exp2_hw((float)(l[j] - le)) : step[j];
+    to[2 * kSsmQ] = hi;
+    to[3 * kSsmQ] = (float)(l[j] - (double)hi);
+    if (lane < 2) w.lq[2 * at + lane] = lane ? lq - l0 : l0;
+  }
 }
 
-// A wave per chunk and head.
+// The windows that the call begins from, put where no sequence of the call
+// writes (zeros for a new one): a workgroup a sequence.
 template <class E>
-__global__ __launch_bounds__(256) void k_ssm_decays(SsmCall c, SsmScratch w) {
-  const int h = (int)blockIdx.y * 4 + (int)threadIdx.x / 64;
-  int seq, num, chunks;
-  if (h >= c.H || (int)blockIdx.x >= w.blocks || !ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
+__device__ __forceinline__ void ssm_keep_window(const SsmCall& c, const SsmScratch& w, int seq) {
+  const int s = ssm_slot(c.src, seq, c.slots);
+  const size_t each = (size_t)(c.W - 1) * c.C;
+  const E* from = static_cast<const E*>(c.window) + (s >= 0 ? s * each : 0);
+  E* to = static_cast<E*>(w.windows) + seq * each;
+  for (size_t k = threadIdx.x; k < each; k += 256) to[k] = s >= 0 ? from[k] : (E)0.f;
+}
+
+// The windows after a call: channels `first`, `first` + `step` .. of a sequence.
+template <class E>
+__device__ __forceinline__ void ssm_window(const SsmCall& c, const SsmScratch& w, int seq, int first, int step) {
   int t0, t1;
   ssm_rows(c, seq, t0, t1);
-  const int r0 = t0 + num * kSsmQ;
-  ssm_decays<E>(c, w, (int)blockIdx.x, r0, min(kSsmQ, t1 - r0), h);
+  const int d = ssm_slot(c.dst, seq, c.slots), W1 = c.W - 1;
+  if (d < 0) return;
+  const E* x = static_cast<const E*>(c.xbc);
+  const E* before = static_cast<const E*>(w.windows) + (size_t)seq * W1 * c.C;
+  E* to = static_cast<E*>(c.window) + (size_t)d * W1 * c.C;
+  for (int ch = first; ch < c.C; ch += step)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      if (k >= W1) continue;
+      const int t = t1 - W1 + k;
+      to[(size_t)k * c.C + ch] = t >= t0 ? x[(size_t)t * c.xbc_stride + ch] : before[(size_t)(t - t0 + W1) * c.C + ch];
+    }
+}
+template <class E>
+__global__ __launch_bounds__(256) void k_ssm_window(SsmCall c, SsmScratch w) {
+  ssm_window<E>(c, w, (int)blockIdx.y, (int)(blockIdx.x * 256 + threadIdx.x), (int)gridDim.x * 256);
 }
 
-// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock).
+// B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); and in
+// workgroups of their own, at the same time, what the chunk's positions have of
+// the heads, and the windows: 13 us for a few thousand tokens (two launches less,
+// 62 -> 56 us in all), 26 for 16384 tokens of 64 heads x 64 x 128.
 template <class E, int NT>
 __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
   typedef SsmBlock<NT, PY> Blk;
   __shared__ __align__(16) float lb[kSsmQ * LD];
   __shared__ __align__(16) float lc[kSsmQ * LD];
+  const int g = (int)blockIdx.y, tid = (int)threadIdx.x;
+  if ((int)blockIdx.y == (int)gridDim.y - 1) {
+    if ((int)blockIdx.x < c.n) ssm_keep_window<E>(c, w, (int)blockIdx.x);
+    return;
+  }
   int seq, num, chunks;
-  if (!ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
-  if ((int)blockIdx.x >= w.blocks) return;
+  if ((int)blockIdx.x >= w.blocks || !ssm_piece(c, (int)blockIdx.x, 1, 0, seq, num, chunks)) return;
   int t0, t1;
   ssm_rows(c, seq, t0, t1);
-  const int s = ssm_slot(c.src, seq, c.slots), g = (int)blockIdx.y, r0 = t0 + num * kSsmQ;
-  const int tid = (int)threadIdx.x, rows = min(kSsmQ, t1 - r0);
+  const int s = ssm_slot(c.src, seq, c.slots), r0 = t0 + num * kSsmQ, rows = min(kSsmQ, t1 - r0);
+  if (g >= c.G) {
+    const int h = ((g - c.G) * 4 + __builtin_amdgcn_readfirstlane(tid / 64)) * kSsmHeads;
+    if (h < c.H) ssm_decays<E>(c, w, (int)blockIdx.x, r0, rows, h);
+    return;
+  }
   // a thread convolves one channel along a quarter of the chunk's rows, all of
   // which are loaded at once (zeros before the sequence and past it)
   constexpr int RUN = kSsmQ / 4;
@@ -525,7 +572,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
 #pragma unroll
       for (int j = 0; j < 3; ++j)
         if (3 - j < c.W) {
-          const E* at = static_cast<const E*>(c.window) + ((size_t)src * (c.W - 1) + (j - 3 + c.W - 1)) * c.C + ch;
+          const E* at = static_cast<const E*>(w.windows) + ((size_t)seq * (c.W - 1) + (j - 3 + c.W - 1)) * c.C + ch;
           raw[0][j].set(have > 0 ? (float)at[0] : 0.f, have > 1 ? (float)at[1] : 0.f);
         }
     }
@@ -822,7 +869,8 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
 }
 
 // The states before the segments of a cut sequence, in place of the segments'
-// contributions: a thread per state of a head (grid: states, heads, sequences).
+// contributions: a thread per state of a head (grid: states, heads, sequences;
+// one row of heads more moves the windows).
 constexpr int kSsmJoin = 8;  // contributions on their way
 
 inline __device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScratch& w) {
@@ -866,7 +914,10 @@ inline __device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScrat
 }
 template <class E>  // one for each source that has this header
 __global__ __launch_bounds__(256) void k_ssm_join(SsmCall c, SsmScratch w) {
-  ssm_join(c, w);
+  if ((int)blockIdx.y == c.H)
+    ssm_window<E>(c, w, (int)blockIdx.z, (int)(blockIdx.x * 256 + threadIdx.x), (int)gridDim.x * 256);
+  else
+    ssm_join(c, w);
 }
 
 template <class E, int NT>
@@ -878,12 +929,9 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   const int lds_out = SsmLds<NT, PY, true>::bytes(nw), lds_sum = SsmLds<NT, PY, false>::bytes(nw);
   auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
-  hipError_t e = hipSuccess;
-  if (w.blocks) {
-    hipLaunchKernelGGL(k_ssm_decays<E>, dim3((unsigned)w.blocks, (unsigned)(c.H + 3) / 4), dim3(256), 0, st, c, w);
-    hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)c.G), dim3(256), 0, st, c, w);
-    e = hipGetLastError();
-  }
+  const int decays = (c.H + 4 * kSsmHeads - 1) / (4 * kSsmHeads);
+  hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + decays + 1)), dim3(256), 0, st, c, w);
+  hipError_t e = hipGetLastError();
   auto allow = [&](const void* f, int bytes) {
     if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
@@ -891,12 +939,14 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   if (w.segments > c.n) allow(reinterpret_cast<const void*>(sum), lds_sum);
   if (e == hipSuccess && w.segments > c.n) {
     hipLaunchKernelGGL(sum, grid, dim3(64 * nw), lds_sum, st, c, w);
-    hipLaunchKernelGGL(k_ssm_join<E>, dim3((unsigned)((c.P * c.N + 255) / 256), (unsigned)c.H, (unsigned)c.n), dim3(256), 0,
-                       st, c, w);
+    hipLaunchKernelGGL(k_ssm_join<E>, dim3((unsigned)((c.P * c.N + 255) / 256), (unsigned)(c.H + 1), (unsigned)c.n),
+                       dim3(256), 0, st, c, w);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(out, grid, dim3(64 * nw), lds_out, st, c, w);
+  if (w.segments == c.n)  // (no join that moves them)
+    hipLaunchKernelGGL(k_ssm_window<E>, dim3((unsigned)((c.C + 255) / 256), (unsigned)c.n), dim3(256), 0, st, c, w);
   return hipGetLastError();
 }
 
