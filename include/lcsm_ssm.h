@@ -55,7 +55,7 @@ typedef struct lcsm_ssm_shape {
 } lcsm_ssm_shape;
 
 /* Device bytes of the workspace: the states 4 M slots H P N, the windows,
- * copies of the parameters, and for prompt calls beyond 256 tokens what all
+ * copies of the parameters, and for prompt calls beyond 192 tokens what all
  * heads share of every 64 tokens (about 12 G N + 300 G + 17 H bytes a token) and
  * the states of the segments that a call is cut into.  Host only.
  * Errors: LCSM_EINVAL for a bad shape (sizes < 1, P > 4096, N > 256, W > 4, G not a

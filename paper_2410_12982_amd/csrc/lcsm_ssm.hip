@@ -315,11 +315,11 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
   return launch_scan_rows<E, 64, 4, 16>(c, st);
 }
 
-// Up to so many tokens a prompt call goes through k_ssm_scan.  One prompt of 32
-// heads x 64 x 128 takes 14 us for 29 tokens, 37 for 128, 66 for 256 with it (a
-// quarter of a microsecond a token), and in chunks 66 for 256, 69 for 512, 76 for
-// 1024.
-constexpr int kSsmScanTokens = 256;
+// Up to so many tokens a prompt call goes through k_ssm_scan: one prompt of 32
+// heads x 64 x 128 takes 14 us for 29 tokens, 37 for 128, 52 for 192, 67 for 256
+// with it (a quarter of a microsecond a token), and in chunks 61 for 257, 63 for
+// 512; one of 24 heads x 64 x 64 in fp32 37 for 192 and 47 for 256, in chunks 37.
+constexpr int kSsmScanTokens = 192;
 
 // How a prompt call is cut: segments of `per` chunks so that about as many
 // workgroups are on their way as there is room for at once (two or one a compute

@@ -1,5 +1,5 @@
 """The state space mixer's two ways through a prompt, where each can go wrong:
-calls of up to 256 tokens position by position, longer ones in chunks (needs an
+calls of up to 192 tokens position by position, longer ones in chunks (needs an
 MI355X).  Tolerances are those of test_gpu_ssm.py, and derived there."""
 import ctypes
 
@@ -18,14 +18,14 @@ pytestmark = pytest.mark.gpu
 def test_ragged_short_prompts(shape, dtype):
     """Position by position: blocks of 32 that end inside, an empty sequence, and on from there."""
     lay = Layer(*shape, dtype=dtype, slots=5, seed=1 + sum(shape))
-    for lens in ([33, 0, 1, 130, 64], [2, 31, 32, 3, 0], [256, 0, 0, 0, 0]):
+    for lens in ([33, 0, 1, 130, 64], [2, 31, 32, 3, 0], [256, 0, 0, 0, 0], [33, 0, 1, 94, 64], [192, 0, 0, 0, 0]):
         offs = np.concatenate([[0], np.cumsum(lens)]).tolist()
         x, xr = lay.inputs(offs[-1])
         y = lay.ctx.prompt(0, x[0], x[1], z=x[2], offsets=ints(offs))
         lay.check(y, lay.want(xr, offs), str(lens))
 
 
-@pytest.mark.parametrize("T", [255, 256, 257, 320, 321])
+@pytest.mark.parametrize("T", [191, 192, 193, 255, 256, 257, 320, 321])
 def test_lengths_around_the_change(T):
     lay = Layer(3, 40, 64, 1, 4, slots=1, max_tokens=T, seed=T)
     x, xr = lay.inputs(T)
