@@ -183,6 +183,7 @@ __device__ __forceinline__ void store_two(Two<E> t, __amdgpu_buffer_rsrc_t r, un
 __device__ __forceinline__ bool ssm_fast(double l0, double l1) { return fabs(l0) < 64.0 && fabs(l1) < 64.0; }
 
 constexpr int kSsmHeads = 4;  // heads a wave, at once
+constexpr int kSsmWaves = 8;  // waves of a workgroup of k_ssm_bc
 
 template <class E>
 __device__ __forceinline__ void ssm_decays(const SsmCall& c, const SsmScratch& w, int block, int r0, int rows, int h0) {
@@ -228,7 +229,7 @@ __device__ __forceinline__ void ssm_keep_window(const SsmCall& c, const SsmScrat
   const size_t each = (size_t)(c.W - 1) * c.C;
   const E* from = static_cast<const E*>(c.window) + (s >= 0 ? s * each : 0);
   E* to = static_cast<E*>(w.windows) + seq * each;
-  for (size_t k = threadIdx.x; k < each; k += 256) to[k] = s >= 0 ? from[k] : (E)0.f;
+  for (size_t k = threadIdx.x; k < each; k += 64 * kSsmWaves) to[k] = s >= 0 ? from[k] : (E)0.f;
 }
 
 // The windows after a call: channels `first`, `first` + `step` .. of a sequence.
@@ -256,10 +257,12 @@ __global__ __launch_bounds__(256) void k_ssm_window(SsmCall c, SsmScratch w) {
 
 // B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); and in
 // workgroups of their own, at the same time, what the chunk's positions have of
-// the heads, and the windows: 13 us for a few thousand tokens (two launches less,
-// 62 -> 56 us in all), 26 for 16384 tokens of 64 heads x 64 x 128.
+// the heads, and the windows (two launches less: 62 -> 56 us for 4198 tokens of 15
+// heads x 48 x 40).  Bound by the latency of a chunk's three steps, so by eight
+// waves: 16384 tokens of 64 heads x 64 x 128 20 us, 26 with four; 11 and 13 for
+// the former.
 template <class E, int NT>
-__global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
+__global__ __launch_bounds__(64 * kSsmWaves) void k_ssm_bc(SsmCall c, SsmScratch w) {
   constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
   typedef SsmBlock<NT, PY> Blk;
   __shared__ __align__(16) float lb[kSsmQ * LD];
@@ -275,14 +278,14 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   ssm_rows(c, seq, t0, t1);
   const int s = ssm_slot(c.src, seq, c.slots), r0 = t0 + num * kSsmQ, rows = min(kSsmQ, t1 - r0);
   if (g >= c.G) {
-    const int h = ((g - c.G) * 4 + __builtin_amdgcn_readfirstlane(tid / 64)) * kSsmHeads;
+    const int h = ((g - c.G) * kSsmWaves + __builtin_amdgcn_readfirstlane(tid / 64)) * kSsmHeads;
     if (h < c.H) ssm_decays<E>(c, w, (int)blockIdx.x, r0, rows, h);
     return;
   }
   // a thread convolves one channel along a quarter of the chunk's rows, all of
   // which are loaded at once (zeros before the sequence and past it)
   constexpr int RUN = kSsmQ / 4;
-  for (int k = tid; k < 2 * NP * 4; k += 256) {
+  for (int k = tid; k < 2 * NP * 4; k += 64 * kSsmWaves) {
     // (whole waves have the same rows: 64 divides 2 NP, or they are padding)
     const int col = k % (2 * NP), run = __builtin_amdgcn_readfirstlane(k / (2 * NP)) * RUN;
     const int n = col % NP;
@@ -327,13 +330,13 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   };
   const std::integral_constant<int, PY> py;
   const std::integral_constant<int, kSsmParts> ps;
-  for (int f = wv; f < 4 * NT; f += 4) {
+  for (int f = wv; f < 4 * NT; f += kSsmWaves) {
     const int tt = f / NT, cc = f % NT;
     const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
     float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
     put(Blk::c_at(tt, cc), Blk::PART, v, py);
   }
-  for (int f = wv; f < 4 * NT; f += 4) {
+  for (int f = wv; f < 4 * NT; f += kSsmWaves) {
     const int a = f / 2, b = f % 2;
     const float* p = lb + (32 * b + 4 * q) * LD + 16 * a + l;
     float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(256) void k_ssm_bc(SsmCall c, SsmScratch w) {
   }
   // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
   // are the lane's slots
-  for (int f = wv; f < 6; f += 4) {
+  for (int f = wv; f < 6; f += kSsmWaves) {
     const int tt = f < 2 ? f : 2 + (f - 2) / 2, cc = f < 2 ? 0 : (f - 2) % 2;
     float v[8];
 #pragma unroll
@@ -929,8 +932,9 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   const int lds_out = SsmLds<NT, PY, true>::bytes(nw), lds_sum = SsmLds<NT, PY, false>::bytes(nw);
   auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
-  const int decays = (c.H + 4 * kSsmHeads - 1) / (4 * kSsmHeads);
-  hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + decays + 1)), dim3(256), 0, st, c, w);
+  const int decays = (c.H + kSsmWaves * kSsmHeads - 1) / (kSsmWaves * kSsmHeads);
+  hipLaunchKernelGGL((k_ssm_bc<E, NT>), dim3((unsigned)w.blocks, (unsigned)(c.G + decays + 1)), dim3(64 * kSsmWaves), 0, st,
+                     c, w);
   hipError_t e = hipGetLastError();
   auto allow = [&](const void* f, int bytes) {
     if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
