@@ -265,7 +265,7 @@ _F32 = torch.float32
 
 class _Order:
     """The stream of a context, to be called before work is queued on it:
-    ``_after_current`` when another stream is current."""
+    ``_after_current`` when another stream is current (and then true)."""
     __slots__ = ("stream", "device", "index", "raw")
 
     def __init__(self, stream, device):
@@ -276,6 +276,8 @@ class _Order:
     def __call__(self):
         if self.index is None or _current_raw(self.index) != self.raw:
             _after_current(self.stream, self.device)
+            return True
+        return False
 
 
 def _slab_ptr(tensor, shape, name):
@@ -778,13 +780,17 @@ def _weight(tensor, shape, name, device, dtype=_F32):
     return tensor.contiguous()
 
 
+def _used_on(stream, tensors):
+    """Tensors that work queued on ``stream`` reads or writes: where that is not
+    torch's current stream their memory must not be used anew before it has passed."""
+    for t in tensors:
+        if t is not None and t is not False:
+            t.record_stream(stream)
+
+
 def _handed_over(stream, device, tensors):
-    """Tensors whose copies are queued on ``stream``: where that is not torch's
-    current stream their memory must not be used anew before it has passed."""
     if torch.cuda.current_stream(device).cuda_stream != stream.cuda_stream:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+        _used_on(stream, tensors)
 
 
 def _cuda_device(device):
@@ -899,7 +905,7 @@ class Ssm(_LayerContext):
             return t.data_ptr()
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
 
-    def _fill(self, rows, n, xbc, dt, z, y, src, dst):
+    def _fill(self, rows, n, xbc, dt, z, y, src, dst, offsets=None):
         io, dtype, D = self._io, self.dtype, self.D
         io.xbc, io.xbc_stride = self._rows(xbc, rows, self.C, dtype, "xbc")
         io.dt, io.dt_stride = self._rows(dt, rows, self.H, dtype, "dt")
@@ -910,7 +916,8 @@ class Ssm(_LayerContext):
         else:
             io.y, io.y_stride = self._rows(y, rows, D, dtype, "y")
         io.src, io.dst = self._slots(src, n, "src"), self._slots(dst, n, "dst")
-        self._order()
+        if self._order():
+            _used_on(self.stream, (xbc, dt, z, y, src, dst, offsets))
         return y
 
     def step(self, layer, xbc, dt, z=None, y=None, src=None, dst=None):
@@ -926,12 +933,12 @@ class Ssm(_LayerContext):
     def prompt(self, layer, xbc, dt, z=None, y=None, offsets=None, src=None, dst=None):
         """The tokens of n sequences one after another, xbc [T, C] and so on: sequence i is rows offsets[i] ..
         offsets[i+1] (int32 [n + 1]; None: one sequence of all rows)."""
-        T, n = xbc.shape[0], 1
+        T, n, at = xbc.shape[0], 1, None
         if offsets is not None:
             n = offsets.shape[0] - 1
-            offsets = self._slots(offsets, n + 1, "offsets")
-        y = self._fill(T, n, xbc, dt, z, y, src, dst)
-        r = _lib.lcsm_ssm_prompt_layer(self._ctx, layer, T, n, offsets, self._io_ref)
+            at = self._slots(offsets, n + 1, "offsets")
+        y = self._fill(T, n, xbc, dt, z, y, src, dst, offsets)
+        r = _lib.lcsm_ssm_prompt_layer(self._ctx, layer, T, n, at, self._io_ref)
         if r:
             self._check(r, "lcsm_ssm_prompt_layer")
         return y
@@ -992,7 +999,8 @@ class Norm(_LayerContext):
             io.n, io.n_stride = out.data_ptr(), D
         else:
             io.n, io.n_stride = (None, 0) if out is False else self._rows(out, rows, D, self.dtype, "out")
-        self._order()
+        if self._order():
+            _used_on(self.stream, (o, res, gate, res_out, out))
         r = _lib.lcsm_norm_block(self._ctx, layer, rows, self._io_ref)
         if r:
             self._check(r, "lcsm_norm_block")
@@ -1040,7 +1048,8 @@ class Q4(_LayerContext):
             py, sy = y.data_ptr(), self.N
         else:
             py, sy = self._rows(y, rows, self.N, dtype, "y")
-        self._order()
+        if self._order():
+            _used_on(self.stream, (x, y))
         r = _lib.lcsm_q4_matvec(self._ctx, layer, rows, _dtype_code(dtype), px, sx, py, sy)
         if r:
             self._check(r, "lcsm_q4_matvec")
