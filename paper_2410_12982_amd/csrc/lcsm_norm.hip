@@ -3,7 +3,12 @@
 // A row is held in the registers of TPR threads from its first load to its last
 // store, so that it is read and written once; the statistics are sums over
 // those registers (the variance a second sum, of the differences from the
-// mean).
+// mean).  Memory bounds it: 16384 rows of 2048 bf16 values with an fp32 residual
+// take 90 us, 4.5 TB/s of the 403 MB that have to move (a large copy reaches
+// 4.8); a few rows take the 6 us of a launch and its two round trips.  Rows that
+// are not aligned to 16 bytes, or not of whole eights, go through the same
+// kernels with accesses of the elements' alignment: 2047 values 134 us (232 one
+// element at a time), 1025 57 (98).
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -28,24 +33,40 @@ struct NormCall {
   const float *post_w, *post_b, *scale, *pre_w, *pre_b;  // of the layer, NULL where not given
 };
 
-// VEC consecutive elements from p, which VEC = 8 has aligned to 16 bytes.
-template <int VEC, class E>
-__device__ __forceinline__ void load(const E* p, float (&v)[VEC]) {
-  struct alignas(VEC == 1 ? sizeof(E) : 16) Pack {
-    E e[VEC];
+constexpr int kVec = 8;  // elements of a thread side by side
+
+// Eight elements from p, of which `have` (at least one) are there, the others
+// zero.  WHOLE: all are, and p is aligned to 16 bytes; else p has the alignment
+// of one element, which wide accesses of global memory allow.
+template <bool WHOLE, class E>
+__device__ __forceinline__ void load(const E* p, int have, float (&v)[kVec]) {
+  struct __attribute__((packed, aligned(WHOLE ? 16 : sizeof(E)))) Pack {
+    E e[kVec];
   };
-  const Pack k = *reinterpret_cast<const Pack*>(p);
+  if (WHOLE || have >= kVec) {
+    const Pack k = *reinterpret_cast<const Pack*>(p);
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = (float)k.e[i];
+    for (int i = 0; i < kVec; ++i) v[i] = (float)k.e[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+  }
 }
-template <int VEC, class E>
-__device__ __forceinline__ void store(E* p, const float (&v)[VEC]) {
-  struct alignas(VEC == 1 ? sizeof(E) : 16) Pack {
-    E e[VEC];
-  } k;
+template <bool WHOLE, class E>
+__device__ __forceinline__ void store(E* p, int have, const float (&v)[kVec]) {
+  struct __attribute__((packed, aligned(WHOLE ? 16 : sizeof(E)))) Pack {
+    E e[kVec];
+  };
+  if (WHOLE || have >= kVec) {
+    Pack k;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) k.e[i] = (E)v[i];
-  *reinterpret_cast<Pack*>(p) = k;
+    for (int i = 0; i < kVec; ++i) k.e[i] = (E)v[i];
+    *reinterpret_cast<Pack*>(p) = k;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (i < have) p[i] = (E)v[i];
+  }
 }
 
 // Sum over the TPR threads of a row, in a fixed order; every thread gets it.
@@ -64,12 +85,12 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-template <class E, class RE, int VEC, int NV, int TPR, bool GROUPED>
+template <class E, class RE, bool WHOLE, int NV, int TPR, bool GROUPED>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;  // rows a workgroup
-  constexpr int FP = VEC * NV;
+  constexpr int VEC = kVec, FP = VEC * NV;
   __shared__ float part[TPR / 64];
-  extern __shared__ float lds[];  // GROUPED: the row, then mean and factor of every group
+  extern __shared__ float all[];  // GROUPED: the row, then mean and factor of every group; of each row
   const int lane = (int)threadIdx.x % TPR;
   const int row = (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
   // rows past the last one are computed again by whoever takes them, and not
@@ -77,6 +98,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
   const bool live = row < c.rows;
   const size_t at = (size_t)(live ? row : c.rows - 1);
   const int D = c.D;
+  float* lds = all + (size_t)(threadIdx.x / TPR) * (D + 2 * c.groups);
   auto index = [&](int k) { return (k * TPR + lane) * VEC; };
 
   float v[FP], res[FP];
@@ -85,7 +107,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       float t[VEC] = {};
-      if (index(k) < D) load<VEC>(r + index(k), t);
+      if (index(k) < D) load<WHOLE>(r + index(k), D - index(k), t);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) res[k * VEC + e] = c.alpha * t[e];
     }
@@ -97,8 +119,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
     for (int k = 0; k < NV; ++k) {
       float t[VEC] = {}, u[VEC] = {};
       if (index(k) < D) {
-        load<VEC>(o + index(k), t);
-        if (c.act != LCSM_ACT_NONE) load<VEC>(g + index(k), u);
+        load<WHOLE>(o + index(k), D - index(k), t);
+        if (c.act != LCSM_ACT_NONE) load<WHOLE>(g + index(k), D - index(k), u);
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -112,22 +134,31 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
       if constexpr (GROUPED) {
         // the row meets in LDS, every wave takes groups of it
         const int per = D / c.groups;
+        int team = 64;  // lanes a group: several groups a wave where they are short
+        while (team > per) team /= 2;
+        auto team_sum = [&](float x) {
+          for (int m = 1; m < team; m *= 2) x += __shfl_xor(x, m);
+          return x;
+        };
+        const int who = lane % team;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
           for (int e = 0; e < VEC; ++e)
             if (index(k) + e < D) lds[index(k) + e] = v[k * VEC + e];
         __syncthreads();
-        for (int q = (int)threadIdx.x / 64; q < c.groups; q += TPR / 64) {
-          const float* x = lds + q * per;
+        // (all lanes take every turn: their sums go through each other's registers)
+        for (int q0 = 0; q0 < c.groups; q0 += TPR / team) {
+          const int q = q0 + lane / team;
+          const float* x = lds + min(q, c.groups - 1) * per;
           float mean = 0.f, var = 0.f;
           if (c.post == LCSM_NORM_LAYER) {
-            for (int i = (int)threadIdx.x % 64; i < per; i += 64) mean += x[i];
-            mean = row_sum<64>(mean, nullptr) / per;
+            for (int i = who; i < per; i += team) mean += x[i];
+            mean = team_sum(mean) / per;
           }
-          for (int i = (int)threadIdx.x % 64; i < per; i += 64) var += (x[i] - mean) * (x[i] - mean);
-          var = row_sum<64>(var, nullptr) / per;
-          if (threadIdx.x % 64 == 0) {
+          for (int i = who; i < per; i += team) var += (x[i] - mean) * (x[i] - mean);
+          var = team_sum(var) / per;
+          if (who == 0 && q < c.groups) {
             lds[D + 2 * q] = mean;
             lds[D + 2 * q + 1] = 1.f / sqrtf(var + c.eps);
           }
@@ -144,7 +175,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
         float mean = 0.f, var = 0.f;
         if (c.post == LCSM_NORM_LAYER) {
 #pragma unroll
-          for (int i = 0; i < FP; ++i) mean += v[i];
+          for (int i = 0; i < FP; ++i) mean += v[i];  // (zeros past the row)
           mean = row_sum<TPR>(mean, part) / D;
         }
 #pragma unroll
@@ -163,12 +194,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
       float w[VEC], b[VEC], s[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) w[e] = s[e] = 1.f, b[e] = 0.f;
-      if (c.post_w) load<VEC>(c.post_w + index(k), w);
-      if (c.post_b) load<VEC>(c.post_b + index(k), b);
-      if (c.scale) load<VEC>(c.scale + index(k), s);
+      if (c.post_w) load<WHOLE>(c.post_w + index(k), D - index(k), w);
+      if (c.post_b) load<WHOLE>(c.post_b + index(k), D - index(k), b);
+      if (c.scale) load<WHOLE>(c.scale + index(k), D - index(k), s);
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        res[k * VEC + e] = fmaf(s[e], fmaf(v[k * VEC + e], w[e], b[e]), res[k * VEC + e]);
+        if (WHOLE || index(k) + e < D) res[k * VEC + e] = fmaf(s[e], fmaf(v[k * VEC + e], w[e], b[e]), res[k * VEC + e]);
     }
   }
   if (c.r_out && live) {
@@ -178,7 +209,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
       float t[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) t[e] = res[k * VEC + e];
-      if (index(k) < D) store<VEC>(r + index(k), t);
+      if (index(k) < D) store<WHOLE>(r + index(k), D - index(k), t);
     }
   }
   if (!c.n) return;
@@ -205,48 +236,46 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
     float w[VEC], b[VEC], t[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) w[e] = 1.f, b[e] = 0.f;
-    if (c.pre_w) load<VEC>(c.pre_w + index(k), w);
-    if (c.pre_b) load<VEC>(c.pre_b + index(k), b);
+    if (c.pre_w) load<WHOLE>(c.pre_w + index(k), D - index(k), w);
+    if (c.pre_b) load<WHOLE>(c.pre_b + index(k), D - index(k), b);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) t[e] = fmaf((res[k * VEC + e] - mean) * f, w[e], b[e]);
-    store<VEC>(n + index(k), t);
+    store<WHOLE>(n + index(k), D - index(k), t);
   }
 }
 
-template <class E, class RE, int VEC, int NV, int TPR>
+template <class E, class RE, bool WHOLE, int NV, int TPR, bool GROUPED>
 hipError_t launch(const NormCall& c, hipStream_t st) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
   const dim3 grid((unsigned)((c.rows + RPB - 1) / RPB)), block(TPR < 256 ? 256 : TPR);
-  if constexpr (TPR > 64) {
-    if (c.groups > 1 && c.o && c.post != LCSM_NORM_NONE) {
-      const size_t bytes = ((size_t)c.D + 2 * (size_t)c.groups) * sizeof(float);
-      auto kernel = k_norm<E, RE, VEC, NV, TPR, true>;
-      if (bytes > 65536 - 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != hipSuccess) return e;
-      }
-      hipLaunchKernelGGL(kernel, grid, block, bytes, st, c);
-      return hipGetLastError();
-    }
+  const size_t bytes = GROUPED ? RPB * ((size_t)c.D + 2 * (size_t)c.groups) * sizeof(float) : 0;
+  auto kernel = k_norm<E, RE, WHOLE, NV, TPR, GROUPED>;
+  if (bytes > 65536 - 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_norm<E, RE, VEC, NV, TPR, false>), grid, block, 0, st, c);
+  hipLaunchKernelGGL(kernel, grid, block, bytes, st, c);
   return hipGetLastError();
 }
 
 // A wave holds a row of up to 2048 values, 256 threads one of up to 8192 and
-// 1024 threads the longest; parts normed on their own meet in LDS, which the
-// rows of a workgroup do not share.
-template <class E, class RE, int VEC>
-hipError_t launch_vec(const NormCall& c, hipStream_t st) {
-  const bool wave = c.D <= 2048 && (c.groups == 1 || !c.o || c.post == LCSM_NORM_NONE);
-  if (wave) {
-    if (c.D <= 512) return launch<E, RE, VEC, 8 / VEC, 64>(c, st);
-    return launch<E, RE, VEC, 32 / VEC, 64>(c, st);
+// 1024 threads the longest.  Parts normed on their own meet in LDS, where four
+// waves a row are faster from some length on (16384 rows of 2048 in four parts
+// 88 us, a wave 105; of 512 a wave 27, four 48).
+template <class E, class RE, bool WHOLE>
+hipError_t launch_rows(const NormCall& c, hipStream_t st) {
+  const bool grouped = c.groups > 1 && c.o && c.post != LCSM_NORM_NONE;
+  if (grouped) {
+    if (c.D <= 512) return launch<E, RE, WHOLE, 1, 64, true>(c, st);
+    if (c.D <= 2048) return launch<E, RE, WHOLE, 1, 256, true>(c, st);
+    if (c.D <= 8192) return launch<E, RE, WHOLE, 4, 256, true>(c, st);
+    return launch<E, RE, WHOLE, 4, 1024, true>(c, st);
   }
-  if (c.D <= 2048) return launch<E, RE, VEC, 8 / VEC, 256>(c, st);
-  if (c.D <= 8192) return launch<E, RE, VEC, 32 / VEC, 256>(c, st);
-  return launch<E, RE, VEC, 32 / VEC, 1024>(c, st);
+  if (c.D <= 512) return launch<E, RE, WHOLE, 1, 64, false>(c, st);
+  if (c.D <= 2048) return launch<E, RE, WHOLE, 4, 64, false>(c, st);
+  if (c.D <= 8192) return launch<E, RE, WHOLE, 4, 256, false>(c, st);
+  return launch<E, RE, WHOLE, 4, 1024, false>(c, st);
 }
 
 bool aligned(const void* p, size_t stride, size_t elem) {
@@ -255,10 +284,10 @@ bool aligned(const void* p, size_t stride, size_t elem) {
 
 template <class E, class RE>
 hipError_t launch_norm(const NormCall& c, hipStream_t st) {
-  const bool vec = c.D % 8 == 0 && aligned(c.o, c.o_stride, sizeof(E)) &&
+  const bool whole = c.D % kVec == 0 && aligned(c.o, c.o_stride, sizeof(E)) &&
                    aligned(c.g, c.g_stride, sizeof(E)) && aligned(c.n, c.n_stride, sizeof(E)) &&
                    aligned(c.r, c.r_stride, sizeof(RE)) && aligned(c.r_out, c.r_out_stride, sizeof(RE));
-  return vec ? launch_vec<E, RE, 8>(c, st) : launch_vec<E, RE, 1>(c, st);
+  return whole ? launch_rows<E, RE, true>(c, st) : launch_rows<E, RE, false>(c, st);
 }
 
 }  // namespace
