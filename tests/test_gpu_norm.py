@@ -197,3 +197,16 @@ def test_refusals():
     assert lib.lcsm_norm_block(c.ctx._ctx, 0, 4, None) == lcsm.LCSM_EINVAL
     assert lib.lcsm_norm_block(c.ctx._ctx, 0, -1, ctypes.byref(io)) == lcsm.LCSM_EINVAL
     assert lib.lcsm_norm_block(None, 0, 4, ctypes.byref(io)) == lcsm.LCSM_EINVAL
+
+
+@pytest.mark.parametrize("D,groups", [(24, 4), (64, 4), (512, 512), (300, 100), (510, 5), (513, 27), (1025, 41), (2047, 23), (1001, 1),
+                                      (8191, 1), (9001, 1)])
+@pytest.mark.parametrize("dtype,rdtype", [("bf16", "f32"), ("f16", "f16")])
+def test_parts_and_tails_stay_in_their_rows(D, groups, dtype, rdtype):
+    """Short parts, rows that end inside a vector and begin at odd places: nothing beside a row is written."""
+    c = Case(6, D, dtype, rdtype, "layer", "rms", "silu", groups=groups, pad=1, seed=D)
+    res = torch.full((6, D + 9), 7.0, dtype=TYPES[rdtype], device=dev())
+    out = torch.full((6, D + 9), 7.0, dtype=TYPES[dtype], device=dev())
+    c.check(c.ctx.block(0, c.o, c.r, gate=c.g, res_out=res[:, 3:3 + D], out=out[:, 5:5 + D]))
+    assert bool((res[:, :3] == 7).all()) and bool((res[:, 3 + D:] == 7).all())
+    assert bool((out[:, :5] == 7).all()) and bool((out[:, 5 + D:] == 7).all())
