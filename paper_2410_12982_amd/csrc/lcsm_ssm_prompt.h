@@ -30,6 +30,10 @@
 // three products (2^-16) where the sum is rounded to 16 bits.  bf16 alone would
 // add an error as large as that rounding for every operand.
 //
+// A call is four launches: k_ssm_bc; where sequences are cut into segments, what
+// each segment adds (k_ssm_chunks without OUT) and the states before them
+// (k_ssm_join); and the outputs.
+//
 // A product with a value that is not finite reaches positions before it as 0 *
 // inf; where the state shows such a value, the affected channels' products are
 // made without it and their rows from it on set to NaN.
@@ -378,6 +382,15 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
+//
+// 16384 tokens of 64 heads x 64 x 128 in bf16: OUT 265 us, the contributions 120
+// (join 14, operands 20).  What bounds it is issue: 1750 vector instructions (the
+// convolution, two SiLUs, parts of states and operands, decays) and 324 matrix
+// instructions of 16 cycles a wave and chunk keep a SIMD's vector unit 60 % and
+// its matrix unit 35 % of the time, and the two hardly overlap.  Tried: half of
+// the waves a stage behind the others, 412 against 383 us in all; 128 states at
+// once without a second copy, 447; wave priorities, nothing.  4198 tokens of 15
+// heads x 48 x 40 take 24 and 15 us, which is two chunks' latency.
 template <class E, int NT, bool OUT, bool PAIR>
 __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
