@@ -527,7 +527,9 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
   // the next chunk's rows are loaded under this one's products, where there are
   // registers for them
   constexpr bool AHEAD = sizeof(E) == 2 && (!OUT || NT < 4);
-  // 1024 bytes at `at` of a buffer into LDS, 16 a lane
+  // 1024 bytes at `at` of a buffer into LDS, 16 a lane.  The compiler does not wait
+  // for these where LDS is read: every read comes after an arrived() of the wave
+  // that fetched it, and after a barrier where that is another wave.
   auto fetch = [&](__amdgpu_buffer_rsrc_t r, int at, int to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + to), 16, lane * 16, at, 0, 0);
   };
@@ -642,6 +644,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
     };
     v8bf xs[2][2][PS];  // w o x, made once where there are registers to keep it
     if (!OUT) {
+      if (!Lds::TWICE) arrived();  // w, which this wave has fetched for itself (TWICE: in the turn before)
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
