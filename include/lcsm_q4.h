@@ -10,9 +10,13 @@
  *     y[r,n] = bias[n] + sum_k w[n,k] x[r,k]
  *
  * with codes 0 .. 15, zeros 0 .. 15 (8 where none are given) and any number of
- * rows r.  Products are exact, sums fp32; y is rounded once to x's type.  A
- * row of x with values that are not finite, or beyond 1e36, gives a row of y
- * that is not finite; other rows are not touched by it.
+ * rows r.  x is multiplied by code - 8, exactly (and what zeros other than 8
+ * leave of its sums is added); sums are fp32, and y is rounded once to x's type.
+ * A row of x with values that are not finite gives a row of y that is not
+ * finite; other rows are not touched by it.  Sums are taken over up to 128
+ * inputs before they are scaled: they are within fp32 for any codes and zeros
+ * where |x| stays below 1.7e35, and beyond that a row may be not finite where
+ * the formula's is.
  *
  * Conventions as in lcsm.h: device pointers, asynchronous on the context's
  * stream, LCSM_* return codes, arguments validated before any device work is

@@ -3,11 +3,14 @@
 // The codes are kept as tiles of 16 outputs x 128 inputs, 16 bytes a lane: lane
 // l's word j holds the eight codes of output l % 16 for the inputs 32 j + 8 (l
 // / 16) ..+7, which is the lane's share of a 16x16x32 matrix product's right
-// operand.  The eight lie so that a rotation brings two of them under the
-// exponent of 16.0 in the two halves of the word: 16 + code is exact in bf16
-// and in fp16, and costs an and-or.  A product of x with ones gives the sum of
-// x, in the same lanes, for what has to come off again: 16 + zero.  fp32 rows
-// are taken apart into three bf16 values that hold all of their bits.
+// operand.  What x is multiplied by is code - 8, exactly, whatever its type:
+// with anything larger in place of it (16 + code is one operation) sums of x
+// come off again that are up to six times the result's terms, which costs three
+// bits of them and overflows where the result does not.  A code is kept as sign
+// and magnitude, so that a byte of them is an 8-bit float (below 2^-5 those are
+// whole multiples of 2^-9), two of which are one conversion.  A product of x
+// with ones gives the sum of x, in the same lanes, for zeros other than 8.
+// fp32 rows are taken apart into three bf16 values that hold all of their bits.
 //
 // One token through 8512 x 2048 weights in groups of 128 takes 5.2 us, 1.7 TB/s of
 // the 9 MB that are read (1.9 us at the copy rate): a launch, a round trip for
@@ -49,16 +52,12 @@ struct Q4Call {
 template <class E>
 struct Mat {  // fp16
   typedef v8h V;
-  static constexpr int PARTS = 1, ROT = 29;
-  static constexpr float OFF = -16.f;  // (minus) what an operand has above its code
-  static constexpr unsigned BASE = 0x4C004C00u, MASK = 0x03C003C0u;  // codes at bits 6 and 22
+  static constexpr int PARTS = 1;
   static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 struct MatBf {
   typedef v8bf V;
-  static constexpr int PARTS = 1, ROT = 0;
-  static constexpr float OFF = -16.f;
-  static constexpr unsigned BASE = 0x41804180u, MASK = 0x00780078u;  // codes at bits 3 and 19
+  static constexpr int PARTS = 1;
   static __device__ v4f mul(V a, V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
@@ -66,30 +65,34 @@ struct Mat<bf16_t> : MatBf {};
 template <>
 struct Mat<float> : MatBf {
   static constexpr int PARTS = 3;
-  static constexpr float OFF = 8.f;
 };
 
+// v = code - 8 of a word's eight codes (word_of).
 template <class E>
 __device__ __forceinline__ typename Mat<E>::V weights(unsigned w) {
-  typedef Mat<E> T;
   v4u r;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const unsigned k = __builtin_rotateright32(w, (4 * t + T::ROT) % 32);
-    r[t] = (k & T::MASK) | T::BASE;
-  }
-  if constexpr (std::is_same<E, float>::value) {
-    // code - 8 instead, exact as well: sums that are to be good to fp32 must not
-    // lose bits to 24 sums of x that come off again
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
-      const v2bf two = {(bf16_t)(__builtin_bit_cast(float, r[t] << 16) - 24.f),
-                        (bf16_t)(__builtin_bit_cast(float, r[t] & 0xffff0000u) - 24.f)};
-      r[t] = __builtin_bit_cast(unsigned, two);
+  for (int half = 0; half < 2; ++half) {
+    const unsigned k = half ? __builtin_rotateright32(w, 4) : w;
+    // four bytes, the sign on top and |v|: what is kept is |v| - 1 of negative ones
+    const unsigned bytes = (k & 0x87878787u) + (k >> 7 & 0x01010101u);
+    if constexpr (std::is_same<E, f16_t>::value) {
+      r[2 * half] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(bytes, 512.f, false));
+      r[2 * half + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(bytes, 512.f, true));
+    } else {
+      r[2 * half] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, false));
+      r[2 * half + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, true));
     }
   }
-  return __builtin_bit_cast(typename T::V, r);
+  return __builtin_bit_cast(typename Mat<E>::V, r);
+}
+// Eight codes as a word: e < 4 with the sign of code - 8 at bit 8 e + 7 and three
+// bits of magnitude from 8 e on, the others likewise after a rotation by four.
+__device__ __forceinline__ unsigned word_of(const unsigned (&code)[8]) {
+  unsigned half[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) half[e / 4] |= (code[e] < 8 ? 0x80 | (7 - code[e]) : code[e] - 8) << (8 * (e % 4));
+  return half[0] | __builtin_rotateleft32(half[1], 4);
 }
 
 template <class E, int XV>
@@ -206,7 +209,7 @@ __global__ __launch_bounds__((q4_waves<E, SPG>(RT, NT)) * 64) void k_q4(Q4Call c
         const int at = SPG == 4 ? kb * kTileK / c.group : min(kb * GS + g, c.ng - 1);
         const size_t i = (nt * c.ng + at) * kTileN + col;
         to.s[t][g] = scale_at(c.scales, c.scale_dtype, i);
-        to.z[t][g] = Mat<E>::OFF - (c.zeros ? (float)c.zeros[i] : 8.f);
+        to.z[t][g] = 8.f - (c.zeros ? (float)c.zeros[i] : 8.f);
       }
     }
     if (RT == 1) {
@@ -288,14 +291,13 @@ __global__ __launch_bounds__(256) void k_q4_codes(const uint8_t* __restrict__ sr
     const int j = (int)(i % 4), lane = (int)(i / 4 % 64);
     const size_t tile = i / 256, tk = tile % kb, tn = tile / kb % nts, m = tile / kb / nts;
     const size_t out = tn * kTileN + lane % 16, k0 = tk * kTileK + 32 * j + 8 * (lane / 16);
-    unsigned w = 0;
+    unsigned code[8];
+#pragma unroll
     for (int e = 0; e < 8; ++e) {
       const size_t k = k0 + e;
-      unsigned v = 0;
-      if (out < (size_t)N && k < (size_t)K) v = src[(m * N + out) * bytes + k / 2] >> (4 * (k & 1)) & 15u;
-      w |= v << (4 * (e / 2) + 16 * (e & 1));
+      code[e] = out < (size_t)N && k < (size_t)K ? src[(m * N + out) * bytes + k / 2] >> (4 * (k & 1)) & 15u : 8u;
     }
-    dst[i] = w << 3 | w >> 29;
+    dst[i] = word_of(code);
   }
 }
 
