@@ -407,7 +407,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   take(&p->dt_bias, M * H * 4);
   if (s->max_tokens > lcsm::kSsmScanTokens) {
     const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
-    const size_t each = lcsm::ssm_block_bytes(s->N, lcsm::dtype_size(s->dtype));
+    const size_t each = lcsm::ssm_block_bytes(s->N);
     const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
     if ((double)blocks * (s->G * (double)each + H * 2048.0) + (double)segments * D * s->N * 4 > 70368744177664.0)
       return false;

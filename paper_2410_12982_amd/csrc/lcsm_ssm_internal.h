@@ -67,24 +67,21 @@ __device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, unsigned at)
 
 constexpr int kSsmQ = 64;  // positions of a chunk
 
-// bf16 parts of a value in products that end in fp32 (states, fp32 outputs), and
-// in those whose sum is rounded to 16 bits.
+// bf16 parts of a value in a product: all of fp32's bits.
 constexpr int kSsmParts = 3;
-inline constexpr int ssm_out_parts(size_t elem) { return elem == 4 ? kSsmParts : 2; }
 
 // Operands of one chunk and group for NT blocks of 32 states, in bytes; a
 // fragment of 64 lanes is 1024.  C: [position / 16][state block], B: [state /
 // 16][position block], G = tril(C B^T): the six blocks of 16 x 32 positions
-// that are not above the diagonal; every one part after part (PY of C and G, 3
-// of B).  C and B of NB state blocks at a time are what LDS holds (STAGE).
-template <int NT, int PY>
+// that are not above the diagonal; every one part after part.  C and B of NB state blocks at a time are what LDS holds (STAGE).
+template <int NT>
 struct SsmBlock {
   static constexpr int NB = NT < 2 ? NT : 2, STAGES = NT / NB;
   static constexpr int PART = 4096 * NB, GPART = 6144;
-  static constexpr int STAGE = (PY + kSsmParts) * PART, G = STAGES * STAGE, GBYTES = PY * GPART;
+  static constexpr int STAGE = 2 * kSsmParts * PART, G = STAGES * STAGE, GBYTES = kSsmParts * GPART;
   static constexpr int BYTES = G + GBYTES;
   static constexpr int c_at(int tt, int cc) { return cc / NB * STAGE + (tt * NB + cc % NB) * 1024; }
-  static constexpr int b_at(int a, int b) { return a / (2 * NB) * STAGE + PY * PART + (a % (2 * NB) * 2 + b) * 1024; }
+  static constexpr int b_at(int a, int b) { return a / (2 * NB) * STAGE + kSsmParts * PART + (a % (2 * NB) * 2 + b) * 1024; }
   static constexpr int g_at(int f) { return G + f * 1024; }
 };
 
@@ -95,10 +92,10 @@ struct SsmBlock {
 // unit take turns instead (4 x 2048 tokens of 24 heads x 64 x 64 in fp32 103
 // against 109 us; 16384 tokens of 64 heads x 64 x 128 401 twice, 440 once and four
 // waves).
-template <int NT, int PY, bool OUT>
+template <int NT, bool OUT>
 struct SsmLds {
-  typedef SsmBlock<NT, PY> Blk;
-  static constexpr int C = OUT ? PY * Blk::PART : 0, STAGE = C + kSsmParts * Blk::PART;
+  typedef SsmBlock<NT> Blk;
+  static constexpr int C = OUT ? kSsmParts * Blk::PART : 0, STAGE = C + kSsmParts * Blk::PART;
   static constexpr bool TWICE = NT > 2;
   static constexpr int G = (TWICE ? 2 : 1) * STAGE, WAVES = G + (OUT ? Blk::GBYTES : 0);
   static constexpr int SCAL = 4 * kSsmQ * (int)sizeof(float);
@@ -106,10 +103,7 @@ struct SsmLds {
 };
 
 inline int ssm_blocks_of(int N) { return N <= 32 ? 1 : N <= 64 ? 2 : N <= 128 ? 4 : 8; }
-inline size_t ssm_block_bytes(int N, size_t elem) {
-  const int nt = ssm_blocks_of(N), py = ssm_out_parts(elem);
-  return (size_t)4096 * nt * (py + kSsmParts) + (size_t)py * 6144;
-}
+inline size_t ssm_block_bytes(int N) { return (size_t)kSsmParts * (8192 * ssm_blocks_of(N) + 6144); }
 // Waves of a workgroup, 32 channels of a head each: they share the operands in
 // LDS.  256 registers are what they have up to N = 128, 512 above.
 inline int ssm_waves(int N) { return N > 64 && N <= 128 ? 8 : 4; }

@@ -24,11 +24,11 @@
 // do not (steps that forget everything), the factor 2^(l_t - l_s) <= 1 is put
 // into the elements of tril(C B^T) one by one instead (`fast` false).
 //
-// Values go into the products as sums of bf16 parts, which hold fp32's range
-// (fp16 would not): three parts and the six products above 2^-24 for the states
-// and for fp32 outputs, whose sums are then as good as fp32's, two parts and
-// three products (2^-16) where the sum is rounded to 16 bits.  bf16 alone would
-// add an error as large as that rounding for every operand.
+// Values go into the products as sums of three bf16 parts, which hold fp32's range
+// (fp16 would not) and all of its bits; the six products above 2^-24 make sums as
+// good as fp32's.  Two parts and three products would be good to 2^-16 of the
+// terms: enough for outputs of 16 bits as long as the terms do not cancel (16384
+// tokens of 64 heads x 64 x 128 in bf16 388 us in all, 462 now).
 //
 // A call is four launches: k_ssm_bc; where sequences are cut into segments, what
 // each segment adds (k_ssm_chunks without OUT) and the states before them
@@ -38,8 +38,6 @@
 // inf; where the state shows such a value, the affected channels' products are
 // made without it and their rows from it on set to NaN.
 #pragma once
-
-#include <type_traits>
 
 #include "lcsm_ssm_internal.h"
 
@@ -267,8 +265,8 @@ __global__ __launch_bounds__(256) void k_ssm_window(SsmCall c, SsmScratch w) {
 // the former.
 template <class E, int NT>
 __global__ __launch_bounds__(64 * kSsmWaves) void k_ssm_bc(SsmCall c, SsmScratch w) {
-  constexpr int NP = 32 * NT, LD = NP + 4, PY = ssm_out_parts(sizeof(E));
-  typedef SsmBlock<NT, PY> Blk;
+  constexpr int NP = 32 * NT, LD = NP + 4;
+  typedef SsmBlock<NT> Blk;
   __shared__ __align__(16) float lb[kSsmQ * LD];
   __shared__ __align__(16) float lc[kSsmQ * LD];
   const int g = (int)blockIdx.y, tid = (int)threadIdx.x;
@@ -326,25 +324,23 @@ __global__ __launch_bounds__(64 * kSsmWaves) void k_ssm_bc(SsmCall c, SsmScratch
   __syncthreads();
   char* out = w.bc + ((size_t)blockIdx.x * c.G + g) * Blk::BYTES;
   const int lane = tid & 63, wv = tid >> 6, q = lane >> 4, l = lane & 15;
-  auto put = [&](int at, int step, float (&v)[8], auto parts) {
-    v8bf w[decltype(parts)::value];
+  auto put = [&](int at, int step, float (&v)[8]) {
+    v8bf w[kSsmParts];
     split(v, w);
 #pragma unroll
-    for (int k = 0; k < decltype(parts)::value; ++k) reinterpret_cast<v8bf*>(out + at + k * step)[lane] = w[k];
+    for (int k = 0; k < kSsmParts; ++k) reinterpret_cast<v8bf*>(out + at + k * step)[lane] = w[k];
   };
-  const std::integral_constant<int, PY> py;
-  const std::integral_constant<int, kSsmParts> ps;
   for (int f = wv; f < 4 * NT; f += kSsmWaves) {
     const int tt = f / NT, cc = f % NT;
     const float* p = lc + (16 * tt + l) * LD + 32 * cc + 4 * q;
     float v[8] = {p[0], p[1], p[2], p[3], p[16], p[17], p[18], p[19]};
-    put(Blk::c_at(tt, cc), Blk::PART, v, py);
+    put(Blk::c_at(tt, cc), Blk::PART, v);
   }
   for (int f = wv; f < 4 * NT; f += kSsmWaves) {
     const int a = f / 2, b = f % 2;
     const float* p = lb + (32 * b + 4 * q) * LD + 16 * a + l;
     float v[8] = {p[0], p[LD], p[2 * LD], p[3 * LD], p[16 * LD], p[17 * LD], p[18 * LD], p[19 * LD]};
-    put(Blk::b_at(a, b), Blk::PART, v, ps);
+    put(Blk::b_at(a, b), Blk::PART, v);
   }
   // (C B^T)[t][s] with t a lane's column of the accumulator: rows 4q + i of it
   // are the lane's slots
@@ -365,7 +361,7 @@ __global__ __launch_bounds__(64 * kSsmWaves) void k_ssm_bc(SsmCall c, SsmScratch
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * half + i] = 16 * st + 4 * q + i <= 16 * tt + l ? acc[i] : 0.f;
     }
-    put(Blk::g_at(f), Blk::GPART, v, py);
+    put(Blk::g_at(f), Blk::GPART, v);
   }
 }
 
@@ -393,9 +389,9 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // heads x 48 x 40 take 24 and 15 us, which is two chunks' latency.
 template <class E, int NT, bool OUT, bool PAIR>
 __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chunks(SsmCall c, SsmScratch w) {
-  constexpr int PY = ssm_out_parts(sizeof(E)), PS = kSsmParts;
-  typedef SsmBlock<NT, PY> Blk;
-  typedef SsmLds<NT, PY, OUT> Lds;
+  constexpr int PS = kSsmParts;
+  typedef SsmBlock<NT> Blk;
+  typedef SsmLds<NT, OUT> Lds;
   constexpr int NA = 2 * NT, NB = Blk::NB, STAGES = Blk::STAGES;
   extern __shared__ __align__(16) char lds[];
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
@@ -525,8 +521,9 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
   };
 
   // the next chunk's rows are loaded under this one's products, where there are
-  // registers for them
-  constexpr bool AHEAD = sizeof(E) == 2 && (!OUT || NT < 4);
+  // registers for them (16384 tokens of 64 heads x 64 x 64 in bf16: with OUT 388 us
+  // in all, 357 without)
+  constexpr bool AHEAD = sizeof(E) == 2 && !OUT;
   // 1024 bytes at `at` of a buffer into LDS, 16 a lane.  The compiler does not wait
   // for these where LDS is read: every read comes after an arrived() of the wave
   // that fetched it, and after a barrier where that is another wave.
@@ -544,7 +541,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
   // stage `stage` of chunk k; with the first one what the positions have, with
   // the last one G
   auto fetch_stage = [&](int k, int stage) {
-    fetch_part(operands_of(k), stage * Blk::STAGE + (OUT ? 0 : PY * Blk::PART), stage_at(k, stage), Lds::STAGE);
+    fetch_part(operands_of(k), stage * Blk::STAGE + (OUT ? 0 : PS * Blk::PART), stage_at(k, stage), Lds::STAGE);
     if (stage == 0) fetch(uniform_buffer(w.scal + ((size_t)(block0 + k) * c.H + h) * 4 * kSsmQ, Lds::SCAL), 0, scal_at(k));
   };
   auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
@@ -690,7 +687,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
             for (int i = 0; i < 4; ++i) z[m][i] = load_two<E, PAIR>(r, from + i * zs);
           }
         }
-        if (AHEAD) load_rows(OUT ? next : max(next, k0));  // (once more than is needed: nothing depends on them then)
+        if (AHEAD) load_rows(max(next, k0));  // (once more than is needed: nothing depends on them then)
       }
       if (OUT) {
         if (fast) {
@@ -700,7 +697,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
             for (int e = 0; e < 2; ++e) S[a][e] *= dq0;
         }
         // fragments are read one ahead of their products
-        v8bf cp[2][PY], sp[2][PY];
+        v8bf cp[2][PS], sp[2][PS];
         frag(lds_c, Blk::PART, cp[0]);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
@@ -772,12 +769,12 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
 #pragma unroll
             for (int e = 0; e < 2; ++e) y[tt][e] *= dq1;
         }
-        v8bf yp[2][PY];
+        v8bf yp[2][PS];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           if (fast) {
 #pragma unroll
-            for (int k = 0; k < PY; ++k) yp[e][k] = xp[e][k];
+            for (int k = 0; k < PS; ++k) yp[e][k] = xp[e][k];
           } else {
             operand(pe, b, e, yp[e]);
           }
@@ -787,23 +784,23 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
         if (__ballot(odd)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            v4u part[PY];
+            v4u part[PS];
 #pragma unroll
-            for (int k = 0; k < PY; ++k) part[k] = __builtin_bit_cast(v4u, yp[e][k]);
+            for (int k = 0; k < PS; ++k) part[k] = __builtin_bit_cast(v4u, yp[e][k]);
 #pragma unroll
             for (int j = 7; j >= 0; --j) {
               const unsigned half = j & 1 ? 0xffff0000u : 0xffffu, top = half & 0x7f807f80u;
               if ((part[0][j / 2] & top) != top) continue;
 #pragma unroll
-              for (int k = 0; k < PY; ++k) part[k][j / 2] &= ~half;
+              for (int k = 0; k < PS; ++k) part[k][j / 2] &= ~half;
               bad[e] = min(bad[e], 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
             }
 #pragma unroll
-            for (int k = 0; k < PY; ++k) yp[e][k] = __builtin_bit_cast(v8bf, part[k]);
+            for (int k = 0; k < PS; ++k) yp[e][k] = __builtin_bit_cast(v8bf, part[k]);
           }
         }
         // the blocks of G that have positions of b as columns: 0, 1, 2, 4 or 3, 5
-        v8bf gp[2][PY];
+        v8bf gp[2][PS];
         auto g_at = [&](int tt) { return Lds::G + (tt < 2 ? tt : 2 * tt - 2 + b) * 1024; };
         frag(g_at(2 * b), Blk::GPART, gp[0]);
 #pragma unroll
@@ -817,9 +814,9 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
             for (int j = 0; j < 8; ++j) {
               const int s = 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
               const float d = exp2_hw((lt - plh[s]) + (rt - pll[s]));
-              float sum = (float)gp[tt & 1][PY - 1][j];
+              float sum = (float)gp[tt & 1][PS - 1][j];
 #pragma unroll
-              for (int k = PY - 2; k >= 0; --k) sum += (float)gp[tt & 1][k][j];
+              for (int k = PS - 2; k >= 0; --k) sum += (float)gp[tt & 1][k][j];
               v[j] = s <= t ? sum * d : 0.f;
             }
             split(v, gp[tt & 1]);
@@ -944,8 +941,7 @@ hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) 
   const int items = c.H / c.G * ((c.P + 31) / 32);
   const int nw = items < ssm_waves(c.N) ? items : ssm_waves(c.N);
   const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)) * (((unsigned)w.segments + 7) / 8 * 8));
-  constexpr int PY = ssm_out_parts(sizeof(E));
-  const int lds_out = SsmLds<NT, PY, true>::bytes(nw), lds_sum = SsmLds<NT, PY, false>::bytes(nw);
+  const int lds_out = SsmLds<NT, true>::bytes(nw), lds_sum = SsmLds<NT, false>::bytes(nw);
   auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
   const int decays = (c.H + kSsmWaves * kSsmHeads - 1) / (kSsmWaves * kSsmHeads);
