@@ -76,9 +76,11 @@ int lcsm_q4_matvec(lcsm_q4* ctx, int layer, int rows, int dtype, const void* x, 
  * [rows][ceil(K/2)], scales [rows][ceil(K / group)] of scale_dtype):
  *     scale = max |w| / 7 of the group, rounded to scale_dtype,
  *     code  = 8 + w / scale rounded to the nearest (ties to even), within
- *             0 .. 15; 8 where the scale is zero.
- * An odd K leaves the high bits of a row's last byte 8.  Needs no context; the
- * work is queued on `stream`.  Errors: LCSM_EINVAL, LCSM_EDEVICE. */
+ *             0 .. 15; 8 where the scale is zero or not finite.
+ * A group with a value that is not finite, or beyond 7 times what scale_dtype
+ * holds, has a scale that is not finite, and so weights that are not.  An odd
+ * K leaves the high bits of a row's last byte 8.  Needs no context; the work is
+ * queued on `stream`.  Errors: LCSM_EINVAL, LCSM_EDEVICE. */
 int lcsm_q4_quantize(const float* w, int rows, int K, int group, int scale_dtype, void* codes,
                      void* scales, void* stream);
 

@@ -312,8 +312,8 @@ __global__ __launch_bounds__(256) void k_q4_groups(const T* __restrict__ src, T*
   }
 }
 
-// A wave per group of a row: the largest magnitude, then the codes of two
-// neighbouring weights a lane at a time.
+// A wave per group of a row: the largest magnitude (NaN where one is), then the
+// codes of two neighbouring weights a lane at a time.
 __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w, int rows, int K, int group,
                                                      int ng, int scale_dtype, uint8_t* __restrict__ codes,
                                                      void* __restrict__ scales) {
@@ -324,9 +324,10 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w
   const int k0 = (int)(i % ng) * group, k1 = min(k0 + group, K);
   const float* p = w + row * K;
   float most = 0.f;
-  for (int k = k0 + lane; k < k1; k += 64) most = fmaxf(most, fabsf(p[k]));
+  auto larger = [](float a, float b) { return b > a || b != b ? b : a; };
+  for (int k = k0 + lane; k < k1; k += 64) most = larger(most, fabsf(p[k]));
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+  for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
   float s = __fdiv_rn(most, 7.f);
   if (scale_dtype == LCSM_BF16) s = (float)(bf16_t)s;
   if (scale_dtype == LCSM_F16) s = (float)(f16_t)s;
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w
     if (scale_dtype == LCSM_F32) static_cast<float*>(scales)[i] = s;
   }
   auto code = [&](int k) -> unsigned {
-    if (k >= k1 || s == 0.f) return 8u;
+    if (k >= k1 || s == 0.f || !(s < INFINITY)) return 8u;
     return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(p[k], s)) + 8.f, 0.f), 15.f);
   };
   const size_t bytes = ((size_t)K + 1) / 2;
