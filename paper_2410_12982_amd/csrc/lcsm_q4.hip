@@ -318,31 +318,31 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const float* __restrict__ w
                                                      int ng, int scale_dtype, uint8_t* __restrict__ codes,
                                                      void* __restrict__ scales) {
   const int lane = (int)threadIdx.x & 63;
-  const size_t i = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (i >= (size_t)rows * ng) return;
-  const size_t row = i / ng;
-  const int k0 = (int)(i % ng) * group, k1 = min(k0 + group, K);
-  const float* p = w + row * K;
-  float most = 0.f;
-  auto larger = [](float a, float b) { return b > a || b != b ? b : a; };
-  for (int k = k0 + lane; k < k1; k += 64) most = larger(most, fabsf(p[k]));
+  const size_t groups = (size_t)rows * ng, bytes = ((size_t)K + 1) / 2;
+  for (size_t i = (size_t)blockIdx.x * 4 + threadIdx.x / 64; i < groups; i += (size_t)gridDim.x * 4) {
+    const size_t row = i / ng;
+    const int k0 = (int)(i % ng) * group, k1 = min(k0 + group, K);
+    const float* p = w + row * K;
+    float most = 0.f;
+    auto larger = [](float a, float b) { return b > a || b != b ? b : a; };
+    for (int k = k0 + lane; k < k1; k += 64) most = larger(most, fabsf(p[k]));
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
-  float s = __fdiv_rn(most, 7.f);
-  if (scale_dtype == LCSM_BF16) s = (float)(bf16_t)s;
-  if (scale_dtype == LCSM_F16) s = (float)(f16_t)s;
-  if (lane == 0) {
-    if (scale_dtype == LCSM_BF16) static_cast<bf16_t*>(scales)[i] = (bf16_t)s;
-    if (scale_dtype == LCSM_F16) static_cast<f16_t*>(scales)[i] = (f16_t)s;
-    if (scale_dtype == LCSM_F32) static_cast<float*>(scales)[i] = s;
+    for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
+    float s = __fdiv_rn(most, 7.f);
+    if (scale_dtype == LCSM_BF16) s = (float)(bf16_t)s;
+    if (scale_dtype == LCSM_F16) s = (float)(f16_t)s;
+    if (lane == 0) {
+      if (scale_dtype == LCSM_BF16) static_cast<bf16_t*>(scales)[i] = (bf16_t)s;
+      if (scale_dtype == LCSM_F16) static_cast<f16_t*>(scales)[i] = (f16_t)s;
+      if (scale_dtype == LCSM_F32) static_cast<float*>(scales)[i] = s;
+    }
+    auto code = [&](int k) -> unsigned {
+      if (k >= k1 || s == 0.f || !(s < INFINITY)) return 8u;
+      return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(p[k], s)) + 8.f, 0.f), 15.f);
+    };
+    for (int k = k0 + 2 * lane; k < k1; k += 128)  // groups begin at even k
+      codes[row * bytes + k / 2] = (uint8_t)(code(k) | code(k + 1) << 4);
   }
-  auto code = [&](int k) -> unsigned {
-    if (k >= k1 || s == 0.f || !(s < INFINITY)) return 8u;
-    return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(p[k], s)) + 8.f, 0.f), 15.f);
-  };
-  const size_t bytes = ((size_t)K + 1) / 2;
-  for (int k = k0 + 2 * lane; k < k1; k += 128)  // groups begin at even k
-    codes[row * bytes + k / 2] = (uint8_t)(code(k) | code(k + 1) << 4);
 }
 
 template <class E, int SPG, int RT, int NT>
@@ -563,10 +563,10 @@ int lcsm_q4_quantize(const float* w, int rows, int K, int group, int scale_dtype
   if (!rows) return LCSM_OK;
   if (!w || !codes || !scales) return LCSM_EINVAL;
   const int ng = (int)(((long long)K + group - 1) / group);
-  const size_t b = ((size_t)rows * ng + 3) / 4;
-  if (b > 0x7fffffffu) return LCSM_EINVAL;
-  hipLaunchKernelGGL(lcsm::k_q4_quantize, dim3((unsigned)b), dim3(256), 0, (hipStream_t)stream, w, rows, K, group,
-                     ng, scale_dtype, (uint8_t*)codes, scales);
+  // (a wave a group, up to what a grid holds; 64 lanes each, as blocks() counts)
+  const size_t lanes = (size_t)rows * ng * 64;
+  hipLaunchKernelGGL(lcsm::k_q4_quantize, dim3(lcsm::blocks(lanes)), dim3(256), 0, (hipStream_t)stream, w, rows, K,
+                     group, ng, scale_dtype, (uint8_t*)codes, scales);
   return hipGetLastError() == hipSuccess ? LCSM_OK : LCSM_EDEVICE;
 }
 

@@ -43,3 +43,19 @@ def test_scales_beyond_their_type():
     codes, scales = lcsm_mod().Q4.quantize(w, 32, torch.float16)
     assert not torch.isfinite(scales[0]).any() and torch.isfinite(scales[1]).all()
     assert bool((codes[0] == 0x88).all()) and bool((codes[1] == 0xFF).all())
+
+
+def test_more_groups_than_one_grid_has_waves():
+    """2^26 + 3 groups of 32, what lies past the first rows different from them."""
+    rows = 2 ** 26 + 3
+    w = torch.zeros((rows, 32), device=dev())
+    w[:2, 0], w[-3:, 31], w[2 ** 25, 5] = 7.0, -14.0, 3.5
+    codes, scales = lcsm_mod().Q4.quantize(w, 32, torch.float32)
+    want = torch.zeros((rows, 1), device=dev())
+    want[:2], want[-3:], want[2 ** 25] = 1.0, 2.0, 0.5
+    assert torch.equal(scales, want)
+    got = codes[[0, 1, 2, 2 ** 25, rows - 4, rows - 3, rows - 1]].cpu()
+    plain = torch.full((16,), 0x88, dtype=torch.uint8)
+    first, last, middle = plain.clone(), plain.clone(), plain.clone()
+    first[0], last[15], middle[2] = 0x8F, 0x18, 0xF8
+    assert torch.equal(got, torch.stack([first, first, plain, middle, plain, last, last]))
