@@ -92,11 +92,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
   __shared__ float part[TPR / 64];
   extern __shared__ float all[];  // GROUPED: the row, then mean and factor of every group; of each row
   const int lane = (int)threadIdx.x % TPR;
-  const int row = (int)blockIdx.x * RPB + (int)threadIdx.x / TPR;
+  const size_t row = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / TPR;
   // rows past the last one are computed again by whoever takes them, and not
   // stored: every thread meets every barrier
-  const bool live = row < c.rows;
-  const size_t at = (size_t)(live ? row : c.rows - 1);
+  const bool live = row < (size_t)c.rows;
+  const size_t at = live ? row : (size_t)c.rows - 1;
   const int D = c.D;
   float* lds = all + (size_t)(threadIdx.x / TPR) * (D + 2 * c.groups);
   auto index = [&](int k) { return (k * TPR + lane) * VEC; };
@@ -247,7 +247,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormCall c) {
 template <class E, class RE, bool WHOLE, int NV, int TPR, bool GROUPED>
 hipError_t launch(const NormCall& c, hipStream_t st) {
   constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
-  const dim3 grid((unsigned)((c.rows + RPB - 1) / RPB)), block(TPR < 256 ? 256 : TPR);
+  // one axis of a launch takes fewer than 2^32 threads: 2^20 workgroups of it
+  const unsigned n = ((unsigned)c.rows + RPB - 1) / RPB, x = n < 1u << 20 ? n : 1u << 20;
+  const dim3 grid(x, (n + x - 1) / x), block(TPR < 256 ? 256 : TPR);
   const size_t bytes = GROUPED ? RPB * ((size_t)c.D + 2 * (size_t)c.groups) * sizeof(float) : 0;
   auto kernel = k_norm<E, RE, WHOLE, NV, TPR, GROUPED>;
   if (bytes > 65536 - 1024) {
