@@ -399,8 +399,8 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
   // workgroups of one segment share its operands: every eighth one, as an XCD
   // (and its L2) gets them
   const int hg = c.H / c.G, parts = (c.P + 31) / 32, items = hg * parts;
-  const int wgs = (items + nw - 1) / nw, wgx = c.G * wgs;
-  const int wg = (int)blockIdx.x / 8 % wgx, segment = (int)blockIdx.x / (8 * wgx) * 8 + (int)blockIdx.x % 8;
+  const int wgs = (items + nw - 1) / nw;
+  const int wg = (int)blockIdx.x / 8, segment = (int)blockIdx.y * 8 + (int)blockIdx.x % 8;
   if (segment >= w.segments) return;
   int seq, num, chunks;
   if (!ssm_piece(c, segment, w.per, 1, seq, num, chunks)) return;
@@ -940,7 +940,7 @@ template <class E, int NT>
 hipError_t ssm_prompt_nt(const SsmCall& c, const SsmScratch& w, hipStream_t st) {
   const int items = c.H / c.G * ((c.P + 31) / 32);
   const int nw = items < ssm_waves(c.N) ? items : ssm_waves(c.N);
-  const dim3 grid((unsigned)(c.G * ((items + nw - 1) / nw)) * (((unsigned)w.segments + 7) / 8 * 8));
+  const dim3 grid(8 * (unsigned)(c.G * ((items + nw - 1) / nw)), ((unsigned)w.segments + 7) / 8);
   const int lds_out = SsmLds<NT, true>::bytes(nw), lds_sum = SsmLds<NT, false>::bytes(nw);
   auto out = w.pair ? k_ssm_chunks<E, NT, true, true> : k_ssm_chunks<E, NT, true, false>;
   auto sum = w.pair ? k_ssm_chunks<E, NT, false, true> : k_ssm_chunks<E, NT, false, false>;
