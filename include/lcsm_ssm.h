@@ -59,8 +59,9 @@ typedef struct lcsm_ssm_shape {
  * heads share of every 64 tokens (about 12 G N + 300 G + 17 H bytes a token) and
  * the states of the segments that a call is cut into.  Host only.
  * Errors: LCSM_EINVAL for a bad shape (sizes < 1, P > 4096, N > 256, W > 4, G not a
- * divisor of H, an unknown type, D + 2 G N > 2^24, slots > 65535,
- * max_tokens < 0 or > 2^26, or a workspace beyond 2^46 bytes). */
+ * divisor of H, an unknown type, D + 2 G N > 2^24, slots > 65535, H > 65535,
+ * G + H / 32 > 65534 with max_tokens > 192, max_tokens < 0 or > 2^26, or a
+ * workspace beyond 2^46 bytes). */
 int lcsm_ssm_workspace_bytes(const lcsm_ssm_shape* shape, size_t* bytes);
 
 /* Create a context with all states and windows zero.

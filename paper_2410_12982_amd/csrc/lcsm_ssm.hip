@@ -406,6 +406,7 @@ bool ssm_plan(const lcsm_ssm_shape* s, Plan* p) {
   take(&p->skip, M * H * 4);
   take(&p->dt_bias, M * H * 4);
   if (s->max_tokens > lcsm::kSsmScanTokens) {
+    if (s->G + (s->H + 31) / 32 > 65534) return false;  // rows of k_ssm_bc's launch
     const size_t blocks = (size_t)s->max_tokens / lcsm::kSsmQ + s->slots;
     const size_t each = lcsm::ssm_block_bytes(s->N);
     const size_t segments = lcsm::most_segments(s->H, s->G, s->P, s->N, blocks + s->slots);
