@@ -771,6 +771,14 @@ def _dtype_code(dtype):
     return DTYPES[dtype]
 
 
+def _int(value, name):
+    """A size for the C side (ctypes would take it modulo 2^32)."""
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name} is out of range")
+    return value
+
+
 def _weight(tensor, shape, name, device, dtype=_F32):
     """A parameter as a contiguous tensor (None stays None)."""
     if tensor is None:
@@ -819,6 +827,10 @@ class _LayerContext:
         if r:
             raise LcsmError(r, where, self._last_error(self._ctx).decode() if self._ctx else "")
 
+    def _layer(self, layer):
+        """The layer for the C side, which refuses -1 (ctypes would take it modulo 2^32)."""
+        return layer if -1 < layer < self.M else -1
+
     def _rows(self, tensor, rows, width, dtype, name):
         """(address, stride between rows) of a tensor [rows, width] whose rows are contiguous."""
         if tensor.dtype is dtype and tensor.shape == (rows, width) and tensor.device == self.device:
@@ -861,12 +873,12 @@ class Ssm(_LayerContext):
         if not (conv_w.is_cuda and conv_w.dim() == 3 and A.dim() == 2):
             raise ValueError("conv_w must be a CUDA tensor [M, C, W] and A one [M, H]")
         (M, C, W), H = (int(v) for v in conv_w.shape), int(A.shape[1])
-        G, N = int(groups), int(states)
+        G, N = _int(groups, "groups"), _int(states, "states")
         if H < 1 or (C - 2 * G * N) < H or (C - 2 * G * N) % H:
             raise ValueError("conv_w's channels are not H * P + 2 * groups * states")
         P = (C - 2 * G * N) // H
         self.M, self.C, self.W, self.H, self.P, self.N, self.G = M, C, W, H, P, N, G
-        self.D, self.slots, self.dtype, self.max_tokens = H * P, int(slots), dtype, int(max_tokens)
+        self.D, self.slots, self.dtype, self.max_tokens = H * P, _int(slots, "slots"), dtype, _int(max_tokens, "max_tokens")
         self._shape = SsmShape(M, self.slots, H, P, N, G, W, _dtype_code(dtype), self.max_tokens)
         dev = conv_w.device
         params = [_weight(t, s, n, dev) for t, s, n in
@@ -925,7 +937,7 @@ class Ssm(_LayerContext):
         slots that states are read from (-1: zero) and written to (-1: not kept); None: slot i for sequence i."""
         n = xbc.shape[0]
         y = self._fill(n, n, xbc, dt, z, y, src, dst)
-        r = _lib.lcsm_ssm_step_layer(self._ctx, layer, n, self._io_ref)
+        r = _lib.lcsm_ssm_step_layer(self._ctx, self._layer(layer), n, self._io_ref)
         if r:
             self._check(r, "lcsm_ssm_step_layer")
         return y
@@ -938,7 +950,7 @@ class Ssm(_LayerContext):
             n = offsets.shape[0] - 1
             at = self._slots(offsets, n + 1, "offsets")
         y = self._fill(T, n, xbc, dt, z, y, src, dst, offsets)
-        r = _lib.lcsm_ssm_prompt_layer(self._ctx, layer, T, n, at, self._io_ref)
+        r = _lib.lcsm_ssm_prompt_layer(self._ctx, self._layer(layer), T, n, at, self._io_ref)
         if r:
             self._check(r, "lcsm_ssm_prompt_layer")
         return y
@@ -963,13 +975,13 @@ class Norm(_LayerContext):
                  layers=1, device="cuda:0", stream=None):
         given = [t for t in (post_weight, post_bias, scale, pre_weight, pre_bias) if t is not None]
         dev = _cuda_device(given[0].device if given else device)
-        self.M, self.D = int(given[0].shape[0] if given else layers), int(D)
+        self.M, self.D = _int(given[0].shape[0] if given else layers, "layers"), _int(D, "D")
         self.dtype, self.res_dtype = dtype, dtype if res_dtype is None else res_dtype
         self.act = act
         ws = [_weight(t, (self.M, self.D), n, dev) for t, n in
               ((post_weight, "post_weight"), (post_bias, "post_bias"), (scale, "scale"), (pre_weight, "pre_weight"),
                (pre_bias, "pre_bias"))]
-        shape = NormShape(self.M, self.D, NORMS[post], NORMS[pre], ACTS[act], int(groups), _dtype_code(dtype),
+        shape = NormShape(self.M, self.D, NORMS[post], NORMS[pre], ACTS[act], _int(groups, "groups"), _dtype_code(dtype),
                           _dtype_code(self.res_dtype), float(alpha), float(eps))
         self._open(dev, stream)
         self._order()
@@ -1001,7 +1013,7 @@ class Norm(_LayerContext):
             io.n, io.n_stride = (None, 0) if out is False else self._rows(out, rows, D, self.dtype, "out")
         if self._order():
             _used_on(self.stream, (o, res, gate, res_out, out))
-        r = _lib.lcsm_norm_block(self._ctx, layer, rows, self._io_ref)
+        r = _lib.lcsm_norm_block(self._ctx, self._layer(layer), rows, self._io_ref)
         if r:
             self._check(r, "lcsm_norm_block")
         return (None if res_out is False else res_out), (None if out is False else out)
@@ -1016,7 +1028,7 @@ class Q4(_LayerContext):
     def __init__(self, codes, scales, K, group, zeros=None, bias=None, stream=None):
         if not (codes.is_cuda and codes.dim() == 3 and scales.dim() == 3):
             raise ValueError("codes must be a CUDA tensor [M, N, ceil(K/2)] and scales one [M, N, ceil(K/group)]")
-        self.M, self.N, self.K, self.group = int(codes.shape[0]), int(codes.shape[1]), int(K), int(group)
+        self.M, self.N, self.K, self.group = int(codes.shape[0]), int(codes.shape[1]), _int(K, "K"), _int(group, "group")
         M, N, dev = self.M, self.N, codes.device
         if self.K < 1 or self.group < 1:
             raise ValueError("K and group must be positive")
@@ -1050,7 +1062,7 @@ class Q4(_LayerContext):
             py, sy = self._rows(y, rows, self.N, dtype, "y")
         if self._order():
             _used_on(self.stream, (x, y))
-        r = _lib.lcsm_q4_matvec(self._ctx, layer, rows, _dtype_code(dtype), px, sx, py, sy)
+        r = _lib.lcsm_q4_matvec(self._ctx, self._layer(layer), rows, _dtype_code(dtype), px, sx, py, sy)
         if r:
             self._check(r, "lcsm_q4_matvec")
         return y
@@ -1060,14 +1072,14 @@ class Q4(_LayerContext):
         """(codes, scales) of fp32 weights [..., N, K] (lcsm_q4_quantize), on torch's current stream."""
         if not (w.is_cuda and w.dtype is _F32 and w.dim() >= 2):
             raise ValueError("w must be a CUDA fp32 tensor [..., N, K]")
-        group = int(group)
+        group = _int(group, "group")
         if group < 1:
             raise ValueError("group must be positive")
         w = w.contiguous()
         K, lead = int(w.shape[-1]), tuple(w.shape[:-1])
         codes = torch.empty(lead + ((K + 1) // 2,), dtype=torch.uint8, device=w.device)
         scales = torch.empty(lead + (-(-K // group),), dtype=scale_dtype, device=w.device)
-        rows = w.numel() // K if K else 0
+        rows = _int(w.numel() // K if K else 0, "the number of rows")
         r = _lib.lcsm_q4_quantize(w.data_ptr(), rows, K, group, _dtype_code(scale_dtype), codes.data_ptr(),
                                   scales.data_ptr(), torch.cuda.current_stream(w.device).cuda_stream)
         if r:
