@@ -96,7 +96,7 @@ template <int NT, bool OUT>
 struct SsmLds {
   typedef SsmBlock<NT> Blk;
   static constexpr int C = OUT ? kSsmParts * Blk::PART : 0, STAGE = C + kSsmParts * Blk::PART;
-  static constexpr bool TWICE = NT > 2;
+  static constexpr bool TWICE = Blk::STAGES > 1;
   static constexpr int G = (TWICE ? 2 : 1) * STAGE, WAVES = G + (OUT ? Blk::GBYTES : 0);
   static constexpr int SCAL = 4 * kSsmQ * (int)sizeof(float);
   static constexpr int bytes(int waves) { return WAVES + (TWICE ? 2 : 1) * waves * SCAL; }

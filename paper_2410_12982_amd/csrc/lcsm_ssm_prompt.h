@@ -565,12 +565,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
     const int r0 = t0 + k * kSsmQ, rows = min(kSsmQ, t1 - r0);
     if (!AHEAD) load_rows(k);
     lds_barrier();  // the stage before has been read (TWICE: this one is there)
-    if (!Lds::TWICE)
-      fetch_stage(k, 0);
-    else if (STAGES > 1)
-      fetch_stage(k, 1);
-    else if (more)
-      fetch_stage(next, 0);
+    fetch_stage(k, Lds::TWICE ? 1 : 0);
     if (OUT) fetch_part(operands_of(k), Blk::G, Lds::G, Blk::GBYTES);
     const double* lq = w.lq + 2 * ((size_t)(block0 + k) * c.H + h);
     const double l0 = lq[0], l1 = lq[1];
@@ -659,10 +654,6 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
       const int a0 = 2 * stage * NB, a1 = a0 + 2 * NB, lds_c = stage_at(k, stage), lds_b = lds_c + Lds::C;
       const bool final = stage == STAGES - 1;
       if (!Lds::TWICE) {
-        if (stage > 0) {
-          lds_barrier();
-          fetch_stage(k, stage);
-        }
         arrived();
         lds_barrier();
       } else if (stage > 0) {
@@ -672,9 +663,6 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
           fetch_stage(k, stage + 1);
         else if (more)
           fetch_stage(next, 0);
-      } else if (OUT && STAGES == 1) {
-        arrived();
-        lds_barrier();  // G is there
       }
       if (final) {
         // under the products: this chunk's gates, the next one's rows
