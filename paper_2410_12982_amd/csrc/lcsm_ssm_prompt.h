@@ -877,7 +877,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
 // one row of heads more moves the windows).
 constexpr int kSsmJoin = 8;  // contributions on their way
 
-inline __device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScratch& w) {
+__device__ __forceinline__ void ssm_join(const SsmCall& c, const SsmScratch& w) {
   const int seq = (int)blockIdx.z, h = (int)blockIdx.y;
   // the segments before this sequence's
   int base = 0;
