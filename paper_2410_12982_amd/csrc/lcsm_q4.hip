@@ -12,10 +12,13 @@
 // with ones gives the sum of x, in the same lanes, for zeros other than 8.
 // fp32 rows are taken apart into three bf16 values that hold all of their bits.
 //
-// One token through 8512 x 2048 weights in groups of 128 takes 5.2 us, 1.7 TB/s of
+// One token through 8512 x 2048 weights in groups of 128 takes 5.4 us, 1.7 TB/s of
 // the 9 MB that are read (1.9 us at the copy rate): a launch, a round trip for
 // the codes and the sum in LDS are most of it.  16 rows of fp16 through 2048 x
-// 4096 in groups of 64 7.5 us, five of fp32 through 1543 x 773 5.7.
+// 4096 in groups of 64 7.6 us, five of fp32 through 1543 x 773 4.8.  Rows of whole
+// prompts take the same kernel, which reads x anew for every 64 outputs and unpacks
+// the codes anew for every 64 rows: 4096 bf16 rows through 8512 x 2048 459 us, 311
+// TFLOP/s, three times what a library product with weights of 16 bits takes.
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -131,7 +134,11 @@ struct Tile {
   float s[NT][GS], z[NT][GS];
 };
 
-// Waves of a workgroup at most: 16 where 128 registers are enough, else 8.
+// Waves of a workgroup at most: 16, with 128 registers each, where few are left
+// over, else 8.  Pieces of four tiles with a scale for all 128 inputs spill 19 of
+// them: one bf16 row through 8512 x 2048 takes 6.0 us, 7.3 by 8 waves, 16 rows 6.7
+// and 8.1.  (With 8 waves, pieces of four tiles of rows and two of outputs with a
+// scale every 32 inputs spill 65 of 256.)
 template <class E, int SPG>
 constexpr int q4_waves(int RT, int NT) {
   return RT == 1 && (NT == 1 || (sizeof(E) == 2 && (NT == 2 || SPG == 4))) ? kMaxWaves : kMaxWaves / 2;
@@ -364,13 +371,19 @@ hipError_t launch(const Q4Call& c, int most, hipStream_t st) {
 // The largest pieces that still are workgroups enough: a piece of NT tiles reads
 // x once for all of them, one of RT tiles of rows unpacks the codes once.  bf16,
 // groups of 128, us (workgroups' pieces as RT NT / waves):
-//   16 rows, 8512 x 2048: 14/16 6.2, 12/8 7.3, 11/8 8.4;  2048 x 4096: 11/16 6.5,
-//   12/16 7.2, 14/16 10.5;  16384 x 8192: 12/8 23.3, 14/16 25.8, 11/8 34.3
-//   (one row 17.1, 23.1, 20.2: long rows are read by fewer waves)
-//   32 rows, 8512 x 2048: 24/8 8.8, 12/8 10.0;  4096 x 1024: 12/8 3.8, 11/16 4.5,
-//   24/8 above 5;  2048 x 4096: 11/16 6.7, 12/16 7.3
-//   64 rows, 8512 x 2048: 44/8 13.6, 22/8 16.0;  4096 x 1024: 14/16 4.9, 22/8 5.1;
-//   2048 x 4096: 12/16 7.5, 11/16 11.7, 14/16 11.5
+//   one row, 8512 x 2048: 11/8 5.4, 12/8 5.9, 14/16 6.0;  2048 x 4096: 11/16 4.4,
+//   12/16 5.9;  16384 x 8192: 12/8 19.1, 11/8 20.6, 14/16 21.6
+//   16 rows, 8512 x 2048: 14/16 6.6, 12/8 7.5, 11/8 8.5;  2048 x 4096: 11/16 6.5,
+//   12/16 7.5, 14/16 10.8;  16384 x 8192: 12/8 23.5, 14/16 24.4, 11/8 34.4
+//   32 rows, 8512 x 2048: 24/8 9.0, 12/8 10.6;  4096 x 1024: 12/8 3.9, 11/16 4.5;
+//   2048 x 4096: 11/16 6.7, 12/16 7.5
+//   64 rows, 8512 x 2048: 44/8 13.6, 22/8 15.9;  4096 x 1024: 12/8 5.1, 14/16 5.3;
+//   2048 x 4096: 12/16 7.7, 11/16 11.6
+// fp16 is the same.  fp32 and shorter groups follow the same thresholds, which were
+// not chosen for them: up to 2048 x 4096 what the rule takes is within 6 % of the
+// best of these pieces (4096 x 1024 with 64 rows in groups of 32 19 %), for more
+// outputs it falls behind by up to a half in fp32 (64 rows 16384 x 8192: 22/8 134,
+// 24/8 90) and three quarters in groups of 32 (64 rows 8512 x 2048: 42/8 41, 22/8 23).
 template <class E, int SPG>
 hipError_t launch_rows(const Q4Call& c, hipStream_t st) {
   const long long tiles = (c.N + 15) / 16, rows = (c.rows + 15) / 16;

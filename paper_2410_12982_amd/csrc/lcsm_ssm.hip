@@ -320,9 +320,12 @@ hipError_t launch_scan(const SsmCall& c, hipStream_t st) {
 }
 
 // Up to so many tokens a prompt call goes through k_ssm_scan: one prompt of 32
-// heads x 64 x 128 takes 14 us for 29 tokens, 37 for 128, 52 for 192, 67 for 256
-// with it (a quarter of a microsecond a token), and in chunks 61 for 257, 63 for
-// 512; one of 24 heads x 64 x 64 in fp32 37 for 192 and 47 for 256, in chunks 37.
+// heads x 64 x 128 in bf16 takes 14 us for 29 tokens, 37 for 128 and 52 for 192
+// with it (a quarter of a microsecond a token), in chunks 61 for 193 and 65 for
+// 512; one of 24 heads x 64 x 64 in fp32 26 for 128 and 36 for 192, in chunks 36
+// for 193 and 37 for 512.  The tokens of all sequences count, since each of many
+// takes a share of the card: 24 of 8 tokens 38 us position by position, 32 of 8 42
+// in chunks.
 constexpr int kSsmScanTokens = 192;
 
 // How a prompt call is cut: segments of `per` chunks so that about as many

@@ -88,10 +88,10 @@ struct SsmBlock {
 // What a workgroup of `waves` keeps in LDS: a stage (C and B; B alone where only
 // the states are wanted), G of the chunk, and what each wave's positions have of
 // its head.  TWICE: two of the first and the last, so that the next ones are
-// fetched while these are used; where they are small, two workgroups a compute
-// unit take turns instead (4 x 2048 tokens of 24 heads x 64 x 64 in fp32 103
-// against 109 us; 16384 tokens of 64 heads x 64 x 128 401 twice, 440 once and four
-// waves).
+// fetched before these have been used; where they are small, two workgroups a
+// compute unit take turns instead (4 x 2048 tokens of 24 heads x 64 x 64 in fp32
+// 103 against 109 us; 16384 tokens of 64 heads x 64 x 128 with two parts a value
+// 401 twice, 440 once and four waves).
 template <int NT, bool OUT>
 struct SsmLds {
   typedef SsmBlock<NT> Blk;

@@ -260,9 +260,9 @@ __global__ __launch_bounds__(256) void k_ssm_window(SsmCall c, SsmScratch w) {
 // B, C and tril(C B^T) of one chunk and group as operands (SsmBlock); and in
 // workgroups of their own, at the same time, what the chunk's positions have of
 // the heads, and the windows (two launches less: 62 -> 56 us for 4198 tokens of 15
-// heads x 48 x 40).  Bound by the latency of a chunk's three steps, so by eight
-// waves: 16384 tokens of 64 heads x 64 x 128 20 us, 26 with four; 11 and 13 for
-// the former.
+// heads x 48 x 40 with two parts a value).  Bound by the latency of a chunk's three
+// steps, so by eight waves: 16384 tokens of 64 heads x 64 x 128 20 us, 26 with four;
+// 11 and 13 for the former.
 template <class E, int NT>
 __global__ __launch_bounds__(64 * kSsmWaves) void k_ssm_bc(SsmCall c, SsmScratch w) {
   constexpr int NP = 32 * NT, LD = NP + 4;
@@ -379,14 +379,19 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
 //
-// 16384 tokens of 64 heads x 64 x 128 in bf16: OUT 265 us, the contributions 120
-// (join 14, operands 20).  What bounds it is issue: 1750 vector instructions (the
-// convolution, two SiLUs, parts of states and operands, decays) and 324 matrix
-// instructions of 16 cycles a wave and chunk keep a SIMD's vector unit 60 % and
-// its matrix unit 35 % of the time, and the two hardly overlap.  Tried: half of
-// the waves a stage behind the others, 412 against 383 us in all; 128 states at
-// once without a second copy, 447; wave priorities, nothing.  4198 tokens of 15
-// heads x 48 x 40 take 24 and 15 us, which is two chunks' latency.
+// 16384 tokens of 64 heads x 64 x 128 in bf16: OUT 360 us, the contributions 121
+// (join 14, operands 21; so traced, one launch at a time.  Passes after one another
+// take 443).  What bounds it is issue: 1960 vector instructions (the convolution,
+// two SiLUs, parts of states and operands, decays) and 456 matrix instructions of
+// 16 cycles a wave and chunk keep a SIMD's vector unit 53 % and its matrix unit 38 %
+// of the time, and the two hardly overlap.  All 256 registers are taken: OUT spills
+// 27 for 65 to 128 states (59 in fp32) and 17 for 33 to 64 (33).  Of a chunk's transfers only the next chunk's first stage is on its way
+// under products: the waits for the chunk's rows and for the decays of its halves,
+// which the compiler cannot count apart from transfers of unknown number, wait for
+// the second stage and G before the first product.  Tried, with two parts a value:
+// half of the waves a stage behind the others, 412 against 383 us in all; 128
+// states at once without a second copy, 447; wave priorities, nothing.  4198 tokens
+// of 15 heads x 48 x 40 take 27 and 15 us, which is two chunks' latency.
 template <class E, int NT, bool OUT, bool PAIR>
 __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chunks(SsmCall c, SsmScratch w) {
   constexpr int PS = kSsmParts;
@@ -665,7 +670,7 @@ __global__ __launch_bounds__(NT == 4 ? 512 : 256, NT > 4 ? 1 : 2) void k_ssm_chu
           fetch_stage(next, 0);
       }
       if (final) {
-        // under the products: this chunk's gates, the next one's rows
+        // under the products: this chunk's gates, or the next one's rows
         if (OUT && c.z) {
           const unsigned from = here(zq);
 #pragma unroll
