@@ -1,0 +1,544 @@
+// Prompts of linear attention in chunks on the matrix units; included by one
+// source per element type.
+//
+// Unrolled over a chunk of C positions, with S the state before it, d the decay
+// and rows counted from 0,
+//
+//   y_t = scale (d^(t+1) q_t S + sum_{j<=t} d^(t-j) (q_t k_j) v_j),
+//   S'  = d^C S + sum_j k_j (d^(C-1-j) v_j)^T,
+//
+// four matrix products.  A workgroup has a state and up to 128 of its values, a
+// wave 32 of them, whose part of the state it keeps in registers as the
+// products' accumulators.  Queries, keys and values of a chunk are in LDS as
+// they are in memory, rows of positions; what a product sums over positions is
+// read from there transposed.  The accumulators of one product are an operand
+// of the next as they stand: the order of a product's K slots is free as long as
+// both operands have it, so that keys are taken in the order that makes S an
+// operand of q S, and the scores are made transposed, which makes them one of
+// (q k) v.  Outputs come out as four values of a position a lane.
+//
+// d^(t-j) is put into the scores and into the values as a factor of its own,
+// never as a quotient: no decay overflows or vanishes before its time.
+//
+// What is not a bf16 value goes into the products as a sum of bf16 parts (which
+// have fp32's range): queries, keys and values of fp16 are two, of fp32 three,
+// exactly.  The scores and S are rounded to two parts (2^-16) where outputs are
+// rounded to 16 bits after it, and to three for fp32; the decayed values are
+// three parts always, since they are what the states are made of.
+//
+// A product with a value v_j that is not finite reaches positions before j as 0 *
+// inf; where there is one, the products of the scores are made without it, and
+// the outputs from j on set to NaN.
+#pragma once
+
+#include "lcsm_lin_internal.h"
+
+namespace lcsm {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
+typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+template <class E>
+struct LinParts {
+  static constexpr int IN = 2;   // of queries, keys and values
+  static constexpr int MID = 2;  // of scores and states
+};
+template <>
+struct LinParts<bf16_t> {
+  static constexpr int IN = 1, MID = 2;
+};
+template <>
+struct LinParts<float> {
+  static constexpr int IN = 3, MID = 3;
+};
+
+// c += a b with both in parts: those products whose parts' numbers add up to at
+// most LAST, the small ones first.
+template <int LAST, int P, int Q>
+__device__ __forceinline__ void lin_mul(const v8bf (&a)[P], const v8bf (&b)[Q], v4f& c) {
+#pragma unroll
+  for (int sum = LAST; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (sum - i >= 0 && sum - i < Q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[sum - i], c, 0, 0, 0);
+}
+
+// Eight values as an operand's parts: each the bf16 nearest to what the parts
+// before it leave.
+template <int P>
+__device__ __forceinline__ void lin_split(float (&v)[8], v8bf (&to)[P]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    v4u w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const v2bf two = {(bf16_t)v[2 * k], (bf16_t)v[2 * k + 1]};
+      w[k] = __builtin_bit_cast(unsigned, two);
+      if (p + 1 < P) {
+        v[2 * k] -= __builtin_bit_cast(float, w[k] << 16);
+        v[2 * k + 1] -= __builtin_bit_cast(float, w[k] & 0xffff0000u);
+      }
+    }
+    to[p] = __builtin_bit_cast(v8bf, w);
+  }
+}
+
+// Rows of bf16 in LDS, `chunks` (a power of two) of eight values a row, placed so
+// that eight rows' chunks of one column lie in different banks.
+__device__ __forceinline__ int lin_at(int row, int chunk, int chunks) {
+  const int turn = chunks >= 8 ? row & 7 : chunks == 4 ? row >> 1 & 3 : 0;
+  return (row * chunks + (chunk ^ turn)) * 16;
+}
+__device__ __forceinline__ v8bf lin_read(const char* lds, int row, int chunk, int chunks) {
+  return *reinterpret_cast<const v8bf*>(lds + lin_at(row, chunk, chunks));
+}
+// Of four rows and the four values from `column` on (a multiple of four) each of
+// 16 lanes reads those of its row (lane / 4); it gets the four rows' values of
+// column lane % 16 of the sixteen that the lanes name.
+__device__ __forceinline__ v4s lin_read_turned(const char* lds, int row, int column, int chunks) {
+  const char* p = lds + lin_at(row, column / 8, chunks) + column % 8 * 2;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+}
+__device__ __forceinline__ v8bf lin_join(v4s a, v4s b) {
+  struct {
+    v4s a, b;
+  } two = {a, b};
+  return __builtin_bit_cast(v8bf, two);
+}
+
+// The piece [*k0, *k1) of `per` chunks (and its sequence, its number in it and
+// the sequence's chunks) that has number `want` when the pieces of all sequences
+// are counted one after another, every sequence having at least one; false past
+// the last one.  All lanes of a wave together.
+template <int C>
+__device__ __forceinline__ bool lin_piece(const LinCall& c, int want, int per, int& seq, int& num, int& chunks) {
+  const int lane = (int)threadIdx.x & 63;
+  int base = 0;
+  for (int i0 = 0; i0 < c.n; i0 += 64) {
+    int mine = 0, ch = 0;
+    if (i0 + lane < c.n) {
+      int t0, t1;
+      lin_rows(c, i0 + lane, t0, t1);
+      ch = (t1 - t0 + C - 1) / C;
+      mine = max((ch + per - 1) / per, 1);
+    }
+    int sum = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+      const int v = __shfl_up(sum, m);
+      if (lane >= m) sum += v;
+    }
+    const int total = __shfl(sum, 63);
+    if (want < base + total) {
+      const unsigned long long past = __ballot(base + sum > want);
+      const int who = __ffsll(past) - 1;
+      seq = __builtin_amdgcn_readfirstlane(i0 + who);
+      num = __builtin_amdgcn_readfirstlane(want - base - __shfl(sum - mine, who));
+      chunks = __builtin_amdgcn_readfirstlane(__shfl(ch, who));
+      return true;
+    }
+    base += total;  // (offsets that do not rise: at most 64 T / C and `want` at a time)
+  }
+  return false;
+}
+
+// Eight elements from p, zeros from `have` on, as parts; wide accesses of global
+// memory may begin at any element.
+template <class E, int P>
+__device__ __forceinline__ void lin_load(const E* p, int have, v8bf (&to)[P]) {
+  struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+    E e[8];
+  };
+  struct Whole {
+    E e[8];
+  };
+  Whole w;
+  if (have >= 8) {
+    const Pack k = *reinterpret_cast<const Pack*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.e[i] = k.e[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.e[i] = i < have ? p[i] : (E)0.f;
+  }
+  if constexpr (P == 1) {
+    to[0] = __builtin_bit_cast(v8bf, w);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)w.e[i];
+    lin_split(v, to);
+  }
+}
+
+// `rows` rows of a chunk into LDS, `width` values of each (zeros past both).
+template <class E, int C, int CHUNKS>
+__device__ __forceinline__ void lin_stage(char* lds, const void* from, size_t stride, int rows, int width) {
+  constexpr int P = LinParts<E>::IN;
+  for (int i = (int)threadIdx.x; i < C * CHUNKS; i += (int)blockDim.x) {
+    const int row = i / CHUNKS, chunk = i % CHUNKS;
+    v8bf v[P];
+    lin_load<E, P>(static_cast<const E*>(from) + (size_t)min(row, rows - 1) * stride + 8 * chunk,
+                   row < rows ? width - 8 * chunk : 0, v);
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<v8bf*>(lds + p * C * CHUNKS * 16 + lin_at(row, chunk, CHUNKS)) = v[p];
+  }
+}
+
+// One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
+// state before it; else its own contribution to the state after it.
+template <class E, int KT, bool OUT>
+__global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(LinCall c, LinCut w) {
+  constexpr int C = lin_chunk<E>(KT), TT = C / 16, PB = C / 32;  // tiles and blocks of positions
+  constexpr int IN = LinParts<E>::IN, MID = LinParts<E>::MID;
+  constexpr int KC = 4 * KT, VC = 4 * kLinWaves;  // chunks of eight a row
+  constexpr int KPART = C * KC * 16, VPART = C * VC * 16;
+  extern __shared__ __align__(16) char lds[];  // keys, values, queries
+  char *const lk = lds, *const lv = lk + IN * KPART, *const lq = lv + IN * VPART;
+  const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int vblocks = (c.V + 32 * kLinWaves - 1) / (32 * kLinWaves);
+  const int g = (int)blockIdx.x / vblocks, v0 = (int)blockIdx.x % vblocks * 32 * kLinWaves;
+  const int segment = (int)blockIdx.y, heads = c.H / c.G;
+  int seq, num, chunks;
+  if (!lin_piece<C>(c, segment, w.per, seq, num, chunks)) return;
+  const bool last = (num + 1) * (long long)w.per >= chunks;
+  if (!OUT && last) return;
+  int t0, t1;
+  lin_rows(c, seq, t0, t1);
+  t0 = __builtin_amdgcn_readfirstlane(t0);
+  t1 = __builtin_amdgcn_readfirstlane(t1);
+  const int src = __builtin_amdgcn_readfirstlane(lin_slot(c.src, seq, c.slots));
+  const int dst = __builtin_amdgcn_readfirstlane(lin_slot(c.dst, seq, c.slots));
+  const int k0 = num * w.per, k1 = last ? chunks : k0 + w.per;
+  const double decay = (double)c.decay[g];
+  const float g2 = (float)(decay * 1.4426950408889634);
+  // d^n for n >= 0, 1 for n = 0 whatever d is
+  auto power = [&](int n) { return n > 0 ? exp2_hw(g2 * (float)n) : 1.f; };
+
+  // the state: S[a][e][i] is key 32 (a / 2) + 8 q + 4 (a % 2) + i, value vc + 16 e + l
+  v4f S[2 * KT][2];
+  const int vc = v0 + 32 * wv;  // this wave's first value
+  const size_t each = (size_t)c.K * c.V;
+  auto key_of = [&](int a, int i) { return a / 2 * 32 + 8 * q + a % 2 * 4 + i; };
+  const float* from = nullptr;
+  if (OUT && chunks > w.per)
+    from = w.states + ((size_t)segment * c.G + g) * each;
+  else if (OUT && src >= 0)
+    from = c.state + ((size_t)src * c.G + g) * each;
+#pragma unroll
+  for (int a = 0; a < 2 * KT; ++a)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = key_of(a, i), v = vc + 16 * e + l;
+        S[a][e][i] = from && k < c.K && v < c.V ? from[(size_t)k * c.V + v] : 0.f;
+      }
+
+  LinDecay whole(decay * C);
+  for (int k = k0; k < k1; ++k) {
+    const int r0 = t0 + k * C, rows = min(C, t1 - r0);
+    __syncthreads();  // the chunk before has been read
+    lin_stage<E, C, KC>(lk, static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride + (size_t)g * c.K, c.k_stride, rows, c.K);
+    lin_stage<E, C, VC>(lv, static_cast<const E*>(c.v) + (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride, rows,
+                        c.V - v0);
+    if (OUT)
+      lin_stage<E, C, KC>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + (size_t)g * heads * c.K, c.q_stride, rows,
+                          c.K);
+    __syncthreads();
+    // values as an operand: 32 positions a block, slots 4 q ..+3 and 16 + 4 q ..+3
+    v8bf vf[PB][2][IN];
+#pragma unroll
+    for (int b = 0; b < PB; ++b)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int p = 0; p < IN; ++p) {
+          const int row = 32 * b + 4 * q + l / 4, column = 32 * wv + 16 * e + l % 4 * 4;
+          vf[b][e][p] = lin_join(lin_read_turned(lv + p * VPART, row, column, VC),
+                                 lin_read_turned(lv + p * VPART, row + 16, column, VC));
+        }
+    if constexpr (OUT) {
+      // values that are not finite: the products of the scores are made without
+      // them, `bad` is the first such position of this lane's value
+      int bad[2] = {C, C};
+      v8bf vp[PB][2][IN];
+      bool odd = false;
+#pragma unroll
+      for (int b = 0; b < PB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const v4u w0 = __builtin_bit_cast(v4u, vf[b][e][0]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            odd |= (w0[j] & 0x7f80u) == 0x7f80u || (w0[j] & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+          for (int p = 0; p < IN; ++p) vp[b][e][p] = vf[b][e][p];
+        }
+      const bool any = __ballot(odd) != 0;
+      if (any) {
+#pragma unroll
+        for (int b = 0; b < PB; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            v4u part[IN];
+#pragma unroll
+            for (int p = 0; p < IN; ++p) part[p] = __builtin_bit_cast(v4u, vf[b][e][p]);
+#pragma unroll
+            for (int j = 7; j >= 0; --j) {
+              const unsigned half = j & 1 ? 0xffff0000u : 0xffffu, top = half & 0x7f807f80u;
+              if ((part[0][j / 2] & top) != top) continue;
+#pragma unroll
+              for (int p = 0; p < IN; ++p) part[p][j / 2] &= ~half;
+              bad[e] = min(bad[e], 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
+            }
+#pragma unroll
+            for (int p = 0; p < IN; ++p) vp[b][e][p] = __builtin_bit_cast(v8bf, part[p]);
+          }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          bad[e] = min(bad[e], __shfl_xor(bad[e], 16));
+          bad[e] = min(bad[e], __shfl_xor(bad[e], 32));
+        }
+      }
+      for (int h = 0; h < heads; ++h) {
+        if (h > 0) {
+          __syncthreads();
+          lin_stage<E, C, KC>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
+                              c.q_stride, rows, c.K);
+          __syncthreads();
+        }
+        // y[tt][e]: values 16 e + 4 q + i of position 16 tt + l
+        v4f y[TT][2];
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < KT; ++kb) {
+          v8bf sp[2][MID];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = S[2 * kb][e][i], v[4 + i] = S[2 * kb + 1][e][i];
+            lin_split(v, sp[e]);
+          }
+#pragma unroll
+          for (int tt = 0; tt < TT; ++tt) {
+            v8bf qf[IN];
+#pragma unroll
+            for (int p = 0; p < IN; ++p) qf[p] = lin_read(lq + p * KPART, 16 * tt + l, 4 * kb + q, KC);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(sp[e], qf, y[tt][e]);
+          }
+        }
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+          const float f = power(16 * tt + l + 1);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) y[tt][e] *= f;
+          v8bf qf[KT][IN];
+#pragma unroll
+          for (int kb = 0; kb < KT; ++kb)
+#pragma unroll
+            for (int p = 0; p < IN; ++p) qf[kb][p] = lin_read(lq + p * KPART, 16 * tt + l, 4 * kb + q, KC);
+          // scores, transposed: positions 16 jt + 4 q + i of the keys for 16 tt + l
+#pragma unroll
+          for (int b = 0; b <= tt / 2; ++b) {
+            float v[8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const int jt = 2 * b + half;
+              v4f s = {0.f, 0.f, 0.f, 0.f};
+              if (jt <= tt) {
+#pragma unroll
+                for (int kb = 0; kb < KT; ++kb) {
+                  v8bf kf[IN];
+#pragma unroll
+                  for (int p = 0; p < IN; ++p) kf[p] = lin_read(lk + p * KPART, 16 * jt + l, 4 * kb + q, KC);
+                  lin_mul<MID - 1>(kf, qf[kb], s);
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int far = 16 * (tt - jt) + l - 4 * q - i;
+                v[4 * half + i] = jt <= tt && far >= 0 ? s[i] * power(far) : 0.f;
+              }
+            }
+            v8bf pf[MID];
+            lin_split(v, pf);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(vp[b][e], pf, y[tt][e]);
+          }
+        }
+        if (any) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int first = __shfl(bad[e], 4 * q + i);
+#pragma unroll
+              for (int tt = 0; tt < TT; ++tt)
+                if (16 * tt + l >= first) y[tt][e][i] = __builtin_nanf("");
+            }
+        }
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+          const int t = 16 * tt + l;
+          if (t >= rows) continue;
+          E* to = static_cast<E*>(c.y) + (size_t)(r0 + t) * c.y_stride + ((size_t)g * heads + h) * c.V + vc + 4 * q;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int have = c.V - (vc + 16 * e + 4 * q);
+            struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+              E e[4];
+            } out;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out.e[i] = (E)(c.scale * y[tt][e][i]);
+            if (have >= 4) {
+              *reinterpret_cast<Pack*>(to + 16 * e) = out;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (i < have) to[16 * e + i] = out.e[i];
+            }
+          }
+        }
+      }
+    }
+    // the state after the chunk
+    const LinDecay d = rows == C ? whole : LinDecay(decay * rows);
+#pragma unroll
+    for (int a = 0; a < 2 * KT; ++a)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[a][e][i] = d(S[a][e][i]);
+#pragma unroll
+    for (int b = 0; b < PB; ++b) {
+      v8bf xf[2][3];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
+          float x = (float)vf[b][e][IN - 1][j];
+#pragma unroll
+          for (int p = IN - 2; p >= 0; --p) x += (float)vf[b][e][p][j];
+          v[j] = x * power(rows - 1 - t);
+        }
+        lin_split(v, xf[e]);
+      }
+#pragma unroll
+      for (int a = 0; a < 2 * KT; ++a) {
+        v8bf kf[IN];
+#pragma unroll
+        for (int p = 0; p < IN; ++p) {
+          const int row = 32 * b + 4 * q + l / 4, column = a / 2 * 32 + l % 4 * 8 + a % 2 * 4;
+          kf[p] = lin_join(lin_read_turned(lk + p * KPART, row, column, KC),
+                           lin_read_turned(lk + p * KPART, row + 16, column, KC));
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) lin_mul<2>(kf, xf[e], S[a][e]);
+      }
+    }
+  }
+  float* to = nullptr;
+  if (!OUT)
+    to = w.states + ((size_t)segment * c.G + g) * each;
+  else if (last && dst >= 0)
+    to = c.state + ((size_t)dst * c.G + g) * each;
+  if (!to) return;
+#pragma unroll
+  for (int a = 0; a < 2 * KT; ++a)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = key_of(a, i), v = vc + 16 * e + l;
+        if (k < c.K && v < c.V) to[(size_t)k * c.V + v] = S[a][e][i];
+      }
+}
+
+// The states before the segments of a cut sequence, in place of the segments'
+// contributions: a thread a value of a state (grid: values, states, sequences).
+constexpr int kLinJoin = 8;  // contributions on their way
+
+template <class E, int KT>
+__global__ __launch_bounds__(256) void k_lin_join(LinCall c, LinCut w) {
+  constexpr int C = lin_chunk<E>(KT);
+  const int seq = (int)blockIdx.z, g = (int)blockIdx.y;
+  // the segments before this sequence's
+  int base = 0;
+  for (int i = (int)threadIdx.x & 63; i < seq; i += 64) {
+    int a, b;
+    lin_rows(c, i, a, b);
+    base = min(base + max(((b - a + C - 1) / C + w.per - 1) / w.per, 1), w.segments);
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) base = min(base + __shfl_xor(base, m), w.segments);
+  int t0, t1;
+  lin_rows(c, seq, t0, t1);
+  const int segments = min(((t1 - t0 + C - 1) / C + w.per - 1) / w.per, w.segments - base);
+  if (segments < 2) return;
+  const size_t each = (size_t)c.K * c.V, at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= each) return;
+  const int src = lin_slot(c.src, seq, c.slots);
+  float s = src >= 0 ? c.state[((size_t)src * c.G + g) * each + at] : 0.f;
+  const LinDecay d((double)c.decay[g] * C * w.per);
+  const size_t step = (size_t)c.G * each;
+  float* p = w.states + ((size_t)base * c.G + g) * each + at;
+  for (int k = 0; k < segments; k += kLinJoin) {
+    float v[kLinJoin];
+#pragma unroll
+    for (int j = 0; j < kLinJoin; ++j) v[j] = k + j < segments - 1 ? p[(k + j) * step] : 0.f;
+#pragma unroll
+    for (int j = 0; j < kLinJoin; ++j) {
+      if (k + j >= segments) break;
+      p[(k + j) * step] = s;
+      s = d(s) + v[j];
+    }
+  }
+}
+
+template <class E, int KT>
+hipError_t lin_prompt_kt(const LinCall& c, const LinCut& w, hipStream_t st) {
+  constexpr int C = lin_chunk<E>(KT), IN = LinParts<E>::IN, KPART = C * KT * 64, VPART = C * kLinWaves * 64;
+  constexpr int lds_sum = IN * (KPART + VPART), lds_out = lds_sum + IN * KPART;
+  const unsigned vblocks = (unsigned)((c.V + 32 * kLinWaves - 1) / (32 * kLinWaves));
+  const dim3 grid((unsigned)c.G * vblocks, (unsigned)w.segments), threads(64 * kLinWaves);
+  auto out = k_lin_chunks<E, KT, true>;
+  auto sum = k_lin_chunks<E, KT, false>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(out), hipFuncAttributeMaxDynamicSharedMemorySize, lds_out);
+  if (e == hipSuccess && w.segments > c.n) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(sum), hipFuncAttributeMaxDynamicSharedMemorySize, lds_sum);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(sum, grid, threads, lds_sum, st, c, w);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_lin_join<E, KT>), dim3((unsigned)(((size_t)c.K * c.V + 255) / 256), (unsigned)c.G, (unsigned)c.n),
+                       dim3(256), 0, st, c, w);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(out, grid, threads, lds_out, st, c, w);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t lin_prompt(const LinCall& c, const LinCut& w, hipStream_t st) {
+  switch (lin_blocks_of(c.K)) {
+    case 1: return lin_prompt_kt<E, 1>(c, w, st);
+    case 2: return lin_prompt_kt<E, 2>(c, w, st);
+    case 4: return lin_prompt_kt<E, 4>(c, w, st);
+    default: return lin_prompt_kt<E, 8>(c, w, st);
+  }
+}
+
+}  // namespace lcsm

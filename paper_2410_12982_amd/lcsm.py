@@ -1,5 +1,6 @@
 """Python binding of the C ABI in ``include/lcsm.h``, ``lcsm_base.h``, ``lcsm_dd.h``, ``lcsm_synth.h``, ``lcsm_ssm.h``,
-``lcsm_norm.h`` and ``lcsm_q4.h`` (ctypes).
+``lcsm_norm.h``, ``lcsm_q4.h``, ``lcsm_q8.h``, ``lcsm_lin.h`` and ``lcsm_rot.h``
+(ctypes).
 
 Argument marshalling only: every step of the computation runs in the HIP
 kernels of ``liblcsm.so``.  PyTorch supplies device memory (the workspace and
@@ -95,6 +96,37 @@ class Q4Shape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int) for k in ("M", "N", "K", "group", "scale_dtype")] + [("reserved", ctypes.c_int * 3)]
 
 
+class Q8Shape(ctypes.Structure):
+    """``lcsm_q8_shape``."""
+    _fields_ = [(k, ctypes.c_int) for k in ("M", "N", "K", "max_rows")] + [("reserved", ctypes.c_int * 4)]
+
+
+class LinShape(ctypes.Structure):
+    """``lcsm_lin_shape``."""
+    _fields_ = [(k, ctypes.c_int) for k in ("M", "slots", "H", "G", "K", "V", "dtype", "max_tokens")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int * 3)]
+
+
+class LinIo(ctypes.Structure):
+    """``lcsm_lin_io``."""
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("q", "k", "v", "y")]
+                + [(k, ctypes.c_size_t) for k in ("q_stride", "k_stride", "v_stride", "y_stride")]
+                + [(k, ctypes.c_void_p) for k in ("src", "dst")])
+
+
+class RotShape(ctypes.Structure):
+    """``lcsm_rot_shape``."""
+    _fields_ = ([(k, ctypes.c_int) for k in ("M", "P", "q_heads", "k_heads", "rotary", "pairs", "norm", "dtype")]
+                + [("eps", ctypes.c_float), ("reserved", ctypes.c_int * 3)])
+
+
+class RotIo(ctypes.Structure):
+    """``lcsm_rot_io``."""
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("q", "k", "q_out", "k_out")]
+                + [(k, ctypes.c_size_t) for k in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")]
+                + [("positions", ctypes.c_void_p)])
+
+
 _c_int_p = ctypes.POINTER(ctypes.c_int)
 _vp = ctypes.c_void_p
 
@@ -183,6 +215,32 @@ _SIGS = {
     "lcsm_q4_reset": (ctypes.c_int, [_vp]),
     "lcsm_q4_destroy": (None, [_vp]),
     "lcsm_q4_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_q8.h
+    "lcsm_q8_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(Q8Shape), ctypes.POINTER(ctypes.c_size_t)]),
+    "lcsm_q8_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(Q8Shape)] + [_vp] * 5 + [ctypes.c_size_t]),
+    "lcsm_q8_matmul": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, ctypes.c_size_t,
+                                      _vp, ctypes.c_size_t]),
+    "lcsm_q8_quantize": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int] + [_vp] * 3),
+    "lcsm_q8_reset": (ctypes.c_int, [_vp]),
+    "lcsm_q8_destroy": (None, [_vp]),
+    "lcsm_q8_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_lin.h
+    "lcsm_lin_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(LinShape), ctypes.POINTER(ctypes.c_size_t)]),
+    "lcsm_lin_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(LinShape)] + [_vp] * 3 + [ctypes.c_size_t]),
+    "lcsm_lin_step_layer": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.POINTER(LinIo)]),
+    "lcsm_lin_prompt_layer": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp,
+                                             ctypes.POINTER(LinIo)]),
+    "lcsm_lin_state": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.POINTER(_vp)]),
+    "lcsm_lin_reset": (ctypes.c_int, [_vp]),
+    "lcsm_lin_destroy": (None, [_vp]),
+    "lcsm_lin_last_error": (ctypes.c_char_p, [_vp]),
+    # include/lcsm_rot.h
+    "lcsm_rot_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(RotShape), ctypes.POINTER(ctypes.c_size_t)]),
+    "lcsm_rot_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(RotShape)] + [_vp] * 5 + [ctypes.c_size_t]),
+    "lcsm_rot_apply": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, ctypes.POINTER(RotIo)]),
+    "lcsm_rot_reset": (ctypes.c_int, [_vp]),
+    "lcsm_rot_destroy": (None, [_vp]),
+    "lcsm_rot_last_error": (ctypes.c_char_p, [_vp]),
 }
 
 for _name, (_res, _args) in _SIGS.items():
@@ -763,6 +821,7 @@ F32, BF16, F16 = 0, 1, 2
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 ACTS = {"none": 0, "silu": 1, "sigmoid": 2}
+PAIRS = {"half": 0, "adjacent": 1}
 
 
 def _dtype_code(dtype):
@@ -822,6 +881,29 @@ class _LayerContext:
         self._last_error = getattr(_lib, f"lcsm_{self._kind}_last_error")
         self._destroy = getattr(_lib, f"lcsm_{self._kind}_destroy")
         self._reset = getattr(_lib, f"lcsm_{self._kind}_reset")
+
+    def _create(self, shape, params, device, stream):
+        """The context over a workspace of its own, from parameters (None: not given) that are laid out anew."""
+        nbytes = ctypes.c_size_t(0)
+        r = getattr(_lib, f"lcsm_{self._kind}_workspace_bytes")(ctypes.byref(shape), ctypes.byref(nbytes))
+        if r:
+            raise LcsmError(r, f"lcsm_{self._kind}_workspace_bytes")
+        self._open(device, stream)
+        self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+        self._order()
+        r = self._on_device(getattr(_lib, f"lcsm_{self._kind}_init"), ctypes.byref(self._ctx), ctypes.byref(shape),
+                            *(t.data_ptr() if t is not None else None for t in params), self.stream.cuda_stream,
+                            self.workspace.data_ptr(), nbytes.value)
+        if r:
+            raise LcsmError(r, f"lcsm_{self._kind}_init")
+        _handed_over(self.stream, device, params)
+
+    def _on_device(self, call, *args):
+        """A call of the library, which queues work and allocates on the current device, on the context's."""
+        if torch.cuda.current_device() == self.device.index:
+            return call(*args)
+        with torch.cuda.device(self.device):
+            return call(*args)
 
     def _check(self, r, where):
         if r:
@@ -1085,3 +1167,206 @@ class Q4(_LayerContext):
         if r:
             raise LcsmError(r, "lcsm_q4_quantize")
         return codes, scales
+
+
+class Q8(_LayerContext):
+    """Matrices of 8-bit weights with a scale for each output, times rows that are quantized to 8 bits on the way with a
+    scale for each row (``include/lcsm_q8.h``): ``codes`` int8 [M, N, K], ``scales`` fp32 [M, N], ``bias`` fp32 [M, N] or
+    None.  They are laid out anew and need not be kept.  ``max_rows``: rows of the largest call."""
+    _kind = "q8"
+
+    def __init__(self, codes, scales, max_rows, bias=None, stream=None):
+        if not (codes.is_cuda and codes.dim() == 3):
+            raise ValueError("codes must be a CUDA tensor [M, N, K]")
+        self.M, self.N, self.K = (int(v) for v in codes.shape)
+        self.max_rows, dev = _int(max_rows, "max_rows"), codes.device
+        params = [_weight(codes, (self.M, self.N, self.K), "codes", dev, torch.int8),
+                  _weight(scales, (self.M, self.N), "scales", dev), _weight(bias, (self.M, self.N), "bias", dev)]
+        shape = Q8Shape(*(_int(v, "a size") for v in (self.M, self.N, self.K)), self.max_rows)
+        self._create(shape, params, dev, stream)
+
+    def matmul(self, layer, x, y=None):
+        """y [rows, N] = x [rows, K] times the layer's matrix, in x's type."""
+        rows, dtype = x.shape[0], x.dtype
+        px, sx = self._rows(x, rows, self.K, dtype, "x")
+        if y is None:
+            y = x.new_empty(rows, self.N)
+            py, sy = y.data_ptr(), self.N
+        else:
+            py, sy = self._rows(y, rows, self.N, dtype, "y")
+        if self._order():
+            _used_on(self.stream, (x, y))
+        r = self._on_device(_lib.lcsm_q8_matmul, self._ctx, self._layer(layer), _int(rows, "rows"), _dtype_code(dtype), px, sx,
+                            py, sy)
+        if r:
+            self._check(r, "lcsm_q8_matmul")
+        return y
+
+    @staticmethod
+    def quantize(w):
+        """(codes, scales) of fp32 weights [..., N, K] (lcsm_q8_quantize), on torch's current stream."""
+        if not (w.is_cuda and w.dtype is _F32 and w.dim() >= 2):
+            raise ValueError("w must be a CUDA fp32 tensor [..., N, K]")
+        w = w.contiguous()
+        K, lead = int(w.shape[-1]), tuple(w.shape[:-1])
+        codes = torch.empty(lead + (K,), dtype=torch.int8, device=w.device)
+        scales = torch.empty(lead, dtype=torch.float32, device=w.device)
+        rows = _int(w.numel() // K if K else 0, "the number of rows")
+        with torch.cuda.device(w.device):
+            r = _lib.lcsm_q8_quantize(w.data_ptr(), rows, _int(K, "K"), codes.data_ptr(), scales.data_ptr(),
+                                      torch.cuda.current_stream(w.device).cuda_stream)
+        if r:
+            raise LcsmError(r, "lcsm_q8_quantize")
+        return codes, scales
+
+
+class Lin(_LayerContext):
+    """Linear attention of M layers with a decay for each state (``include/lcsm_lin.h``), for prompts and for single
+    tokens.
+
+    ``decay`` [M, G], fp32 CUDA tensor: the natural logarithms of the G states' decays.  ``heads`` heads of queries,
+    heads / G neighbouring ones of which read one state of ``keys`` x ``values``; outputs are multiplied by ``scale``.
+    ``slots`` sequences' states are held (``state(layer)`` [slots, G, keys, values] fp32).  ``max_tokens``: tokens of the
+    largest prompt call.
+    """
+    _kind = "lin"
+
+    def __init__(self, decay, slots, heads, keys, values, scale=1.0, dtype=torch.bfloat16, max_tokens=0, stream=None):
+        if not (decay.is_cuda and decay.dim() == 2):
+            raise ValueError("decay must be a CUDA tensor [M, G]")
+        self.M, self.G = (int(v) for v in decay.shape)
+        self.H, self.K, self.V = _int(heads, "heads"), _int(keys, "keys"), _int(values, "values")
+        self.slots, self.dtype, self.max_tokens = _int(slots, "slots"), dtype, _int(max_tokens, "max_tokens")
+        dev = decay.device
+        shape = LinShape(_int(self.M, "the layers"), self.slots, self.H, _int(self.G, "the states"), self.K, self.V,
+                         _dtype_code(dtype), self.max_tokens, float(scale))
+        self._create(shape, [_weight(decay, (self.M, self.G), "decay", dev)], dev, stream)
+        self._widths = self.H * self.K, self.G * self.K, self.G * self.V, self.H * self.V
+        self._io = LinIo()
+        self._io_ref = ctypes.byref(self._io)
+        self._states = []
+        for m in range(self.M):
+            p = _vp()
+            self._check(_lib.lcsm_lin_state(self._ctx, m, ctypes.byref(p)), "lcsm_lin_state")
+            at = p.value - self.workspace.data_ptr()
+            size = 4 * self.slots * self.G * self.K * self.V
+            self._states.append(self.workspace[at:at + size].view(torch.float32).view(self.slots, self.G, self.K, self.V))
+
+    def _list(self, t, n, name):
+        if t is None:
+            return None
+        if t.dtype is torch.int32 and t.shape == (n,) and t.device == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
+
+    def _fill(self, rows, n, q, k, v, y, src, dst, offsets=None):
+        io, dtype = self._io, self.dtype
+        wq, wk, wv, wy = self._widths
+        io.q, io.q_stride = self._rows(q, rows, wq, dtype, "q")
+        io.k, io.k_stride = self._rows(k, rows, wk, dtype, "k")
+        io.v, io.v_stride = self._rows(v, rows, wv, dtype, "v")
+        if y is None:
+            y = q.new_empty(rows, wy)
+            io.y, io.y_stride = y.data_ptr(), wy
+        else:
+            io.y, io.y_stride = self._rows(y, rows, wy, dtype, "y")
+        io.src, io.dst = self._list(src, n, "src"), self._list(dst, n, "dst")
+        if self._order():
+            _used_on(self.stream, (q, k, v, y, src, dst, offsets))
+        return y
+
+    def step(self, layer, q, k, v, y=None, src=None, dst=None):
+        """One token of each of n sequences: q [n, heads keys], k [n, G keys], v [n, G values], y [n, heads values].
+        ``src``, ``dst``: int32 [n], the slots that states are read from (-1: zero) and written to (-1: not kept); None:
+        slot i for sequence i."""
+        n = q.shape[0]
+        y = self._fill(n, n, q, k, v, y, src, dst)
+        r = self._on_device(_lib.lcsm_lin_step_layer, self._ctx, self._layer(layer), _int(n, "rows"), self._io_ref)
+        if r:
+            self._check(r, "lcsm_lin_step_layer")
+        return y
+
+    def prompt(self, layer, q, k, v, y=None, offsets=None, src=None, dst=None):
+        """The tokens of n sequences one after another, q [T, heads keys] and so on: sequence i is rows offsets[i] ..
+        offsets[i+1] (int32 [n + 1]; None: one sequence of all rows)."""
+        T, n, at = q.shape[0], 1, None
+        if offsets is not None:
+            n = offsets.shape[0] - 1
+            at = self._list(offsets, n + 1, "offsets")
+        y = self._fill(T, n, q, k, v, y, src, dst, offsets)
+        r = self._on_device(_lib.lcsm_lin_prompt_layer, self._ctx, self._layer(layer), _int(T, "rows"), _int(n, "sequences"), at,
+                            self._io_ref)
+        if r:
+            self._check(r, "lcsm_lin_prompt_layer")
+        return y
+
+    def state(self, layer):
+        """The states of a layer, a view [slots, G, keys, values] of the workspace."""
+        return self._states[layer]
+
+
+class Rot(_LayerContext):
+    """The norms of queries and keys for each head, with the rotation by their positions in the same pass
+    (``include/lcsm_rot.h``).  Heads of P values; ``norm``: "none", "rms" or "layer" with the weights ``q_weight`` and
+    ``k_weight``, fp32 CUDA tensors [M, P] or None (ones); M layers if one is given, else ``layers``.  The first
+    ``rotary`` values of a head are turned (None: all, of an odd P all but one) by position times base^(-2 j / rotary),
+    or by the frequencies ``freqs``, fp64 CUDA tensor [rotary / 2]; ``pairs``: "half" (j and j + rotary / 2) or
+    "adjacent" (2 j and 2 j + 1)."""
+    _kind = "rot"
+
+    def __init__(self, P, q_heads, k_heads, rotary=None, base=10000.0, freqs=None, pairs="half", norm="rms", eps=1e-5,
+                 q_weight=None, k_weight=None, dtype=torch.bfloat16, layers=1, device="cuda:0", stream=None):
+        given = [t for t in (q_weight, k_weight) if t is not None]
+        dev = _cuda_device(given[0].device if given else freqs.device if freqs is not None else device)
+        self.M, self.P = _int(given[0].shape[0] if given else layers, "layers"), _int(P, "P")
+        self.q_heads, self.k_heads, self.dtype = _int(q_heads, "q_heads"), _int(k_heads, "k_heads"), dtype
+        if rotary is None:
+            rotary = self.P // 2 * 2 if freqs is None else 2 * freqs.shape[0]
+        self.rotary = _int(rotary, "rotary")
+        if freqs is None and self.rotary > 0:
+            freqs = torch.tensor([float(base) ** (-2.0 * j / self.rotary) for j in range(min(self.rotary, self.P) // 2)],
+                                 dtype=torch.float64, device=dev)
+        ws = [_weight(t, (self.M, self.P), n, dev) for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
+        freqs = _weight(freqs, (min(self.rotary, self.P) // 2,), "freqs", dev, torch.float64) if self.rotary > 0 else None
+        shape = RotShape(self.M, self.P, self.q_heads, self.k_heads, self.rotary, PAIRS[pairs], NORMS[norm], _dtype_code(dtype),
+                         float(eps))
+        self._create(shape, [freqs] + ws, dev, stream)
+        self._io = RotIo()
+        self._io_ref = ctypes.byref(self._io)
+
+    def apply(self, layer, q, k, positions, q_out=None, k_out=None):
+        """(q, k) normed and turned: q [rows, q_heads P] and k [rows, k_heads P] (None without heads of keys), positions
+        int32 [rows] (None where nothing is turned).  ``q_out`` and ``k_out`` receive them where given (q and k themselves
+        may)."""
+        rows, P, io = q.shape[0], self.P, self._io
+        qw, kw = self.q_heads * P, self.k_heads * P
+        io.q, io.q_stride = self._rows(q, rows, qw, self.dtype, "q")
+        if q_out is None:
+            q_out = q.new_empty(rows, qw)
+            io.q_out, io.q_out_stride = q_out.data_ptr(), qw
+        else:
+            io.q_out, io.q_out_stride = self._rows(q_out, rows, qw, self.dtype, "q_out")
+        if kw == 0:
+            if k is not None or k_out is not None:
+                raise ValueError("the context has no heads of keys")
+            io.k, io.k_stride, io.k_out, io.k_out_stride = None, 0, None, 0
+        else:
+            io.k, io.k_stride = self._rows(k, rows, kw, self.dtype, "k")
+            if k_out is None:
+                k_out = k.new_empty(rows, kw)
+                io.k_out, io.k_out_stride = k_out.data_ptr(), kw
+            else:
+                io.k_out, io.k_out_stride = self._rows(k_out, rows, kw, self.dtype, "k_out")
+        if positions is None:
+            io.positions = None
+        elif (positions.dtype is torch.int32 and positions.shape == (rows,) and positions.device == self.device
+              and positions.is_contiguous()):
+            io.positions = positions.data_ptr()
+        else:
+            raise ValueError(f"positions must be a contiguous int32 tensor of shape {(rows,)} on {self.device}")
+        if self._order():
+            _used_on(self.stream, (q, k, q_out, k_out, positions))
+        r = self._on_device(_lib.lcsm_rot_apply, self._ctx, self._layer(layer), rows, self._io_ref)
+        if r:
+            self._check(r, "lcsm_rot_apply")
+        return q_out, k_out
