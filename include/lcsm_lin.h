@@ -72,7 +72,8 @@ int lcsm_lin_init(lcsm_lin** out, const lcsm_lin_shape* shape, const float* deca
 
 /* What a call reads and writes, rows of tokens in the context's type.  A row
  * is contiguous, rows are `_stride` elements apart (at least the row's
- * length): slices of one wide projection's rows can be handed in as they are.
+ * length, at most 2^24): slices of one wide projection's rows can be handed in
+ * as they are.
  *   q [rows][H K], k [rows][G K], v [rows][G V], y [rows][H V]
  *   y receives the outputs and overlaps nothing else.
  *   src  device int[n]: the slot that sequence i's state is read from, -1:

@@ -26,6 +26,28 @@ auto with_dtype(int t, F&& f) {
   }
 }
 
+constexpr size_t kMaxStride = (size_t)1 << 24;  // elements between rows
+
+// A buffer that is the same for all lanes (which the compiler does not always
+// see, and then loops over the lanes' values at every access).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_buffer(const void* p, unsigned bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)at), hi = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0,
+                                           __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
+}
+
+// Rows as a buffer of whole rows from a base row on: what lies past its end
+// reads as zero and is not stored.  `rows` of them, `width` elements in the
+// last; kMaxStride keeps the offsets of 40 rows of fp32, and of 64 of 16 bits,
+// below 2^32.
+template <class E>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size_t row, size_t stride, int rows,
+                                                             int width) {
+  const unsigned bytes = rows > 0 ? (unsigned)((rows - 1) * stride + width) * (unsigned)sizeof(E) : 0u;
+  return uniform_buffer(static_cast<const E*>(p) + row * stride, bytes);
+}
+
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 // The reciprocal is good to an ulp.
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + exp2_hw(-1.44269504f * v)); }

@@ -133,6 +133,12 @@ hipError_t launch_prompt(const LinCall& c, int dtype, float* states, hipStream_t
   w.states = states;
   w.per = cut ? (blocks + want - 1) / want : blocks;
   w.segments = cut ? blocks / w.per + c.n : c.n;
+  const size_t e = dtype_size(dtype);
+  auto aligned = [&](const void* p, size_t stride, int width, int n) {
+    return (uintptr_t)p % (n * e) == 0 && stride % n == 0 && width % n == 0;
+  };
+  w.direct = e == 2 && aligned(c.q, c.q_stride, c.K, 8) && aligned(c.k, c.k_stride, c.K, 8) && aligned(c.v, c.v_stride, c.V, 8);
+  w.quads = aligned(c.y, c.y_stride, c.V, 4);
   return dtype == LCSM_F32 ? lin_prompt_f32(c, w, st) : dtype == LCSM_BF16 ? lin_prompt_bf16(c, w, st) : lin_prompt_f16(c, w, st);
 }
 
@@ -206,6 +212,8 @@ int lin_call(lcsm_lin* c, int layer, int T, int n, const lcsm_lin_io* io, lcsm::
     if (io->q_stride < (size_t)s.H * s.K || io->k_stride < (size_t)s.G * s.K || io->v_stride < (size_t)s.G * s.V ||
         io->y_stride < (size_t)s.H * s.V)
       return lin_fail(c, LCSM_EINVAL, "a row stride is shorter than the row");
+    for (size_t stride : {io->q_stride, io->k_stride, io->v_stride, io->y_stride})
+      if (stride > lcsm::kMaxStride) return lin_fail(c, LCSM_EINVAL, "a row stride is above 2^24 elements");
   }
   if (c->faulted) return LCSM_ESTATE;
   const size_t m = (size_t)layer;

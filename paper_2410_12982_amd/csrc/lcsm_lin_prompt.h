@@ -17,6 +17,10 @@
 // operand of q S, and the scores are made transposed, which makes them one of
 // (q k) v.  Outputs come out as four values of a position a lane.
 //
+// Chunks are counted from a sequence's end, so that the one that is not full is
+// its first, and begins with rows of zeros that are nowhere in memory: what the
+// factors depend on is then the same for all chunks.
+//
 // d^(t-j) is put into the scores and into the values as a factor of its own,
 // never as a quotient: no decay overflows or vanishes before its time.
 //
@@ -92,21 +96,36 @@ __device__ __forceinline__ int lin_at(int row, int chunk, int chunks) {
   const int turn = chunks >= 8 ? row & 7 : chunks == 4 ? row >> 1 & 3 : 0;
   return (row * chunks + (chunk ^ turn)) * 16;
 }
-__device__ __forceinline__ v8bf lin_read(const char* lds, int row, int chunk, int chunks) {
-  return *reinterpret_cast<const v8bf*>(lds + lin_at(row, chunk, chunks));
-}
-// Of four rows and the four values from `column` on (a multiple of four) each of
-// 16 lanes reads those of its row (lane / 4); it gets the four rows' values of
-// column lane % 16 of the sixteen that the lanes name.
-__device__ __forceinline__ v4s lin_read_turned(const char* lds, int row, int column, int chunks) {
-  const char* p = lds + lin_at(row, column / 8, chunks) + column % 8 * 2;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+// Where rows that are the same modulo 8 have the chunks 4 m + low: two places of
+// a lane and what is the same for all lanes.
+struct LinPlace {
+  int at[2];
+  __device__ LinPlace(int row, int low, int chunks) {
+    at[0] = lin_at(row, low, chunks);
+    at[1] = chunks >= 8 ? at[0] ^ 64 : at[0];
+  }
+  __device__ int operator()(int rows, int m, int chunks) const { return at[m & 1] + rows * chunks * 16 + (m >> 1) * 128; }
+};
+__device__ __forceinline__ v8bf lin_read(const char* lds, int at) { return *reinterpret_cast<const v8bf*>(lds + at); }
+// Each of 16 lanes names four values of one of four rows (of row lane / 4); it
+// gets the four rows' values of column lane % 16 of the sixteen that they name.
+__device__ __forceinline__ v4s lin_read_turned(const char* lds, int at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds + at));
 }
 __device__ __forceinline__ v8bf lin_join(v4s a, v4s b) {
   struct {
     v4s a, b;
   } two = {a, b};
   return __builtin_bit_cast(v8bf, two);
+}
+
+constexpr unsigned kLinNowhere = 0xC0000000u;  // past every buffer here
+
+// v, with what is made of it made here: sums of it and of what is the same in
+// every turn of a loop are not kept in registers from one turn to the next.
+__device__ __forceinline__ unsigned lin_here(unsigned v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // The piece [*k0, *k1) of `per` chunks (and its sequence, its number in it and
@@ -174,23 +193,74 @@ __device__ __forceinline__ void lin_load(const E* p, int have, v8bf (&to)[P]) {
   }
 }
 
-// `rows` rows of a chunk into LDS, `width` values of each (zeros past both).
-template <class E, int C, int CHUNKS>
-__device__ __forceinline__ void lin_stage(char* lds, const void* from, size_t stride, int rows, int width) {
-  constexpr int P = LinParts<E>::IN;
-  for (int i = (int)threadIdx.x; i < C * CHUNKS; i += (int)blockDim.x) {
-    const int row = i / CHUNKS, chunk = i % CHUNKS;
-    v8bf v[P];
-    lin_load<E, P>(static_cast<const E*>(from) + (size_t)min(row, rows - 1) * stride + 8 * chunk,
-                   row < rows ? width - 8 * chunk : 0, v);
+// 16 bytes a lane from a buffer into LDS, one lane after another.  The compiler does
+// not wait for these where LDS is read.
+__device__ __forceinline__ void lin_fetch(__amdgpu_buffer_rsrc_t r, unsigned at, char* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, (int)at, 0, 0, 0);
+}
+
+// A chunk's rows into LDS, `width` values of each (zeros past them): `pad` rows of
+// zeros, then those of `from`.  DIRECT: straight from memory (bf16 rows of whole
+// and aligned eights); the caller waits for them.
+template <class E, int C, int CHUNKS, bool DIRECT>
+__device__ __forceinline__ void lin_stage(char* lds, const E* from, size_t stride, int pad, int width) {
+  constexpr int P = LinParts<E>::IN, THREADS = 64 * kLinWaves;
+  if constexpr (DIRECT) {
+    const auto r = row_buffer<E>(from, 0, stride, C - pad, width);
+    const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    constexpr int STEP = THREADS / CHUNKS;  // rows a turn: a multiple of 8, so that a lane has one chunk of all its rows
+    static_assert(C % STEP == 0 && STEP % 8 == 0, "whole turns");
+    const int row = (int)threadIdx.x / CHUNKS, chunk = lin_at(row, (int)threadIdx.x % CHUNKS, CHUNKS) / 16 - row * CHUNKS;
+    // (rows before the first wrap around to past the buffer's end)
+    const unsigned each = (unsigned)stride * 2u;
+    const unsigned at = lin_here((unsigned)(row - pad) * each + 16u * (unsigned)chunk);
 #pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<v8bf*>(lds + p * C * CHUNKS * 16 + lin_at(row, chunk, CHUNKS)) = v[p];
+    for (int i = 0; i < C / STEP; ++i)
+      lin_fetch(r, 8 * chunk < width ? at + (unsigned)(i * STEP) * each : kLinNowhere, lds + (i * THREADS + 64 * wv) * 16);
+  } else {
+#pragma unroll 2
+    for (int i = 0; i < C * CHUNKS; i += THREADS) {
+      const int at = i + (int)threadIdx.x, row = at / CHUNKS, chunk = at % CHUNKS;
+      if (at >= C * CHUNKS) break;
+      v8bf v[P];
+      lin_load<E, P>(from + (size_t)max(row - pad, 0) * stride + 8 * chunk, row >= pad ? width - 8 * chunk : 0, v);
+#pragma unroll
+      for (int p = 0; p < P; ++p) *reinterpret_cast<v8bf*>(lds + p * C * CHUNKS * 16 + lin_at(row, chunk, CHUNKS)) = v[p];
+    }
+  }
+}
+
+// Four outputs from column `at` of `width` on, of the row that begins at `row` of
+// a buffer.  quads: four are whole and aligned as one.
+template <class E>
+__device__ __forceinline__ void lin_store(__amdgpu_buffer_rsrc_t r, unsigned row, int at, int width, v4f v, bool quads) {
+  typedef unsigned v2u __attribute__((ext_vector_type(2)));
+  struct {
+    E e[4];
+  } out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out.e[i] = (E)v[i];
+  if (quads) {
+    const unsigned to = at < width ? row + (unsigned)at * (unsigned)sizeof(E) : kLinNowhere;
+    if constexpr (sizeof(E) == 4)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, out), r, (int)to, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), r, (int)to, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned to = at + i < width ? row + (unsigned)(at + i) * (unsigned)sizeof(E) : kLinNowhere;
+      if constexpr (sizeof(E) == 4)
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, out.e[i]), r, (int)to, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, out.e[i]), r, (int)to, 0, 0);
+    }
   }
 }
 
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
-template <class E, int KT, bool OUT>
+template <class E, int KT, bool OUT, bool DIRECT>
 __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(LinCall c, LinCut w) {
   constexpr int C = lin_chunk<E>(KT), TT = C / 16, PB = C / 32;  // tiles and blocks of positions
   constexpr int IN = LinParts<E>::IN, MID = LinParts<E>::MID;
@@ -215,58 +285,91 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   const int dst = __builtin_amdgcn_readfirstlane(lin_slot(c.dst, seq, c.slots));
   const int k0 = num * w.per, k1 = last ? chunks : k0 + w.per;
   const double decay = (double)c.decay[g];
-  const float g2 = (float)(decay * 1.4426950408889634);
-  // d^n for n >= 0, 1 for n = 0 whatever d is
-  auto power = [&](int n) { return n > 0 ? exp2_hw(g2 * (float)n) : 1.f; };
+  float g2 = (float)(decay * 1.4426950408889634);
+  if (g2 < -1e30f) g2 = -1e30f;  // (d = 0: finite, so that d^0 is 1; NaN stays)
+  // d^n, 1 for n <= 0
+  auto power = [&](int n) { return exp2_hw(g2 * (float)max(n, 0)); };
+  // the same of distances 16 m + n as d^(16 m) d^n: m is the same for all lanes
+  float tile[TT], near[4], far[4], back[4];
+#pragma unroll
+  for (int m = 0; m < TT; ++m) tile[m] = power(16 * m);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    near[i] = power(l - 4 * q - i);       // in a tile (where it is not negative)
+    far[i] = power(16 + l - 4 * q - i);   // from the tile before
+    back[i] = power(15 - 4 * q - i);      // to the end of the tile
+  }
 
   // the state: S[a][e][i] is key 32 (a / 2) + 8 q + 4 (a % 2) + i, value vc + 16 e + l
   v4f S[2 * KT][2];
   const int vc = v0 + 32 * wv;  // this wave's first value
   const size_t each = (size_t)c.K * c.V;
-  auto key_of = [&](int a, int i) { return a / 2 * 32 + 8 * q + a % 2 * 4 + i; };
+  // a state as a buffer: keys past the last one are past its end
+  unsigned column[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    column[e] = vc + 16 * e + l < c.V ? (unsigned)(8 * q * c.V + vc + 16 * e + l) * 4u : kLinNowhere;
+  auto state_at = [&](unsigned from, int a, int i) { return from + (unsigned)((a / 2 * 32 + a % 2 * 4 + i) * c.V) * 4u; };
   const float* from = nullptr;
   if (OUT && chunks > w.per)
     from = w.states + ((size_t)segment * c.G + g) * each;
   else if (OUT && src >= 0)
     from = c.state + ((size_t)src * c.G + g) * each;
+  const auto before = uniform_buffer(from, from ? (unsigned)(each * 4) : 0u);
 #pragma unroll
-  for (int a = 0; a < 2 * KT; ++a)
+  for (int e = 0; e < 2; ++e) {
+    const unsigned at = lin_here(column[e]);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = key_of(a, i), v = vc + 16 * e + l;
-        S[a][e][i] = from && k < c.K && v < c.V ? from[(size_t)k * c.V + v] : 0.f;
-      }
+      for (int i = 0; i < 4; ++i)
+        S[a][e][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(before, state_at(at, a, i), 0, 0));
+  }
+
+  // keys and queries as they are, rows 16 n + l, eights 4 m + q; keys turned, rows
+  // 16 n + 4 q ..+3, eights 4 m + 0 ..+3; values turned, eights 4 wv + 2 e + 0 ..+1
+  const LinPlace plain(l, q, KC), turned(4 * q + l / 4, l % 4, KC);
+  const int value_at[2] = {lin_at(4 * q + l / 4, 4 * wv + l % 4 / 2, VC) + l % 2 * 8,
+                           lin_at(4 * q + l / 4, 4 * wv + 2 + l % 4 / 2, VC) + l % 2 * 8};
 
   LinDecay whole(decay * C);
+  const unsigned out_row = (unsigned)c.y_stride * (unsigned)sizeof(E);
   for (int k = k0; k < k1; ++k) {
-    const int r0 = t0 + k * C, rows = min(C, t1 - r0);
+    const int end = t1 - (chunks - 1 - k) * C, r0 = max(end - C, t0), pad = C - (end - r0);
     __syncthreads();  // the chunk before has been read
-    lin_stage<E, C, KC>(lk, static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride + (size_t)g * c.K, c.k_stride, rows, c.K);
-    lin_stage<E, C, VC>(lv, static_cast<const E*>(c.v) + (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride, rows,
-                        c.V - v0);
-    if (OUT)
-      lin_stage<E, C, KC>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + (size_t)g * heads * c.K, c.q_stride, rows,
-                          c.K);
-    __syncthreads();
+    lin_stage<E, C, KC, DIRECT>(lk, static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride + (size_t)g * c.K, c.k_stride, pad,
+                                c.K);
+    lin_stage<E, C, VC, DIRECT>(lv, static_cast<const E*>(c.v) + (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride,
+                                pad, c.V - v0);
+    auto stage_queries = [&](int h) {
+      lin_stage<E, C, KC, DIRECT>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
+                                  c.q_stride, pad, c.K);
+    };
+    // (the compiler does not wait for transfers straight into LDS)
+    auto arrived = [&]() {
+      if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    };
+    if (OUT) stage_queries(0);
+    arrived();
     // values as an operand: 32 positions a block, slots 4 q ..+3 and 16 + 4 q ..+3
     v8bf vf[PB][2][IN];
+    auto read_values = [&]() {
 #pragma unroll
-    for (int b = 0; b < PB; ++b)
+      for (int b = 0; b < PB; ++b)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int p = 0; p < IN; ++p) {
-          const int row = 32 * b + 4 * q + l / 4, column = 32 * wv + 16 * e + l % 4 * 4;
-          vf[b][e][p] = lin_join(lin_read_turned(lv + p * VPART, row, column, VC),
-                                 lin_read_turned(lv + p * VPART, row + 16, column, VC));
-        }
+          for (int p = 0; p < IN; ++p) {
+            const int at = value_at[e] + p * VPART + 32 * b * VC * 16;
+            vf[b][e][p] = lin_join(lin_read_turned(lv, at), lin_read_turned(lv, at + 16 * VC * 16));
+          }
+    };
+    read_values();
     if constexpr (OUT) {
       // values that are not finite: the products of the scores are made without
       // them, `bad` is the first such position of this lane's value
       int bad[2] = {C, C};
-      v8bf vp[PB][2][IN];
       bool odd = false;
 #pragma unroll
       for (int b = 0; b < PB; ++b)
@@ -276,8 +379,6 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             odd |= (w0[j] & 0x7f80u) == 0x7f80u || (w0[j] & 0x7f800000u) == 0x7f800000u;
-#pragma unroll
-          for (int p = 0; p < IN; ++p) vp[b][e][p] = vf[b][e][p];
         }
       const bool any = __ballot(odd) != 0;
       if (any) {
@@ -297,7 +398,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
               bad[e] = min(bad[e], 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
             }
 #pragma unroll
-            for (int p = 0; p < IN; ++p) vp[b][e][p] = __builtin_bit_cast(v8bf, part[p]);
+            for (int p = 0; p < IN; ++p) vf[b][e][p] = __builtin_bit_cast(v8bf, part[p]);
           }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -308,9 +409,8 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
       for (int h = 0; h < heads; ++h) {
         if (h > 0) {
           __syncthreads();
-          lin_stage<E, C, KC>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
-                              c.q_stride, rows, c.K);
-          __syncthreads();
+          stage_queries(h);
+          arrived();
         }
         // y[tt][e]: values 16 e + 4 q + i of position 16 tt + l
         v4f y[TT][2];
@@ -324,29 +424,37 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float v[8];
+            // (the parts of all states, made before the loop over the heads, would take
+            // more registers than there are)
+            asm volatile("" : "+v"(S[2 * kb][e]), "+v"(S[2 * kb + 1][e]));
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = S[2 * kb][e][i], v[4 + i] = S[2 * kb + 1][e][i];
             lin_split(v, sp[e]);
           }
 #pragma unroll
           for (int tt = 0; tt < TT; ++tt) {
+            __builtin_amdgcn_sched_barrier(0);
             v8bf qf[IN];
 #pragma unroll
-            for (int p = 0; p < IN; ++p) qf[p] = lin_read(lq + p * KPART, 16 * tt + l, 4 * kb + q, KC);
+            for (int p = 0; p < IN; ++p) qf[p] = lin_read(lq, p * KPART + plain(16 * tt, kb, KC));
 #pragma unroll
             for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(sp[e], qf, y[tt][e]);
           }
         }
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt) {
-          const float f = power(16 * tt + l + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          const float f = power(16 * tt + l + 1 - pad);
+          // queries and keys are read again for every tile of positions: kept, they
+          // would take more registers than there are
+          const int again = KT >= 4 ? (int)lin_here(0u) : 0;
 #pragma unroll
           for (int e = 0; e < 2; ++e) y[tt][e] *= f;
           v8bf qf[KT][IN];
 #pragma unroll
           for (int kb = 0; kb < KT; ++kb)
 #pragma unroll
-            for (int p = 0; p < IN; ++p) qf[kb][p] = lin_read(lq + p * KPART, 16 * tt + l, 4 * kb + q, KC);
+            for (int p = 0; p < IN; ++p) qf[kb][p] = lin_read(lq, again + p * KPART + plain(16 * tt, kb, KC));
           // scores, transposed: positions 16 jt + 4 q + i of the keys for 16 tt + l
 #pragma unroll
           for (int b = 0; b <= tt / 2; ++b) {
@@ -354,26 +462,29 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const int jt = 2 * b + half;
+              __builtin_amdgcn_sched_barrier(0);
               v4f s = {0.f, 0.f, 0.f, 0.f};
               if (jt <= tt) {
 #pragma unroll
                 for (int kb = 0; kb < KT; ++kb) {
                   v8bf kf[IN];
 #pragma unroll
-                  for (int p = 0; p < IN; ++p) kf[p] = lin_read(lk + p * KPART, 16 * jt + l, 4 * kb + q, KC);
+                  for (int p = 0; p < IN; ++p) kf[p] = lin_read(lk, again + p * KPART + plain(16 * jt, kb, KC));
                   lin_mul<MID - 1>(kf, qf[kb], s);
                 }
               }
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int far = 16 * (tt - jt) + l - 4 * q - i;
-                v[4 * half + i] = jt <= tt && far >= 0 ? s[i] * power(far) : 0.f;
+                if (jt < tt)
+                  v[4 * half + i] = s[i] * far[i] * tile[tt - jt - 1];
+                else
+                  v[4 * half + i] = jt == tt && l >= 4 * q + i ? s[i] * near[i] : 0.f;
               }
             }
             v8bf pf[MID];
             lin_split(v, pf);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(vp[b][e], pf, y[tt][e]);
+            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(vf[b][e], pf, y[tt][e]);
           }
         }
         if (any) {
@@ -387,32 +498,18 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
                 if (16 * tt + l >= first) y[tt][e][i] = __builtin_nanf("");
             }
         }
+        const auto r = row_buffer<E>(static_cast<E*>(c.y) + ((size_t)g * heads + h) * c.V, (size_t)r0, c.y_stride, C - pad, c.V);
+        const unsigned to = lin_here((unsigned)(l - pad) * out_row);
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt) {
-          const int t = 16 * tt + l;
-          if (t >= rows) continue;
-          E* to = static_cast<E*>(c.y) + (size_t)(r0 + t) * c.y_stride + ((size_t)g * heads + h) * c.V + vc + 4 * q;
+        for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int have = c.V - (vc + 16 * e + 4 * q);
-            struct __attribute__((packed, aligned(sizeof(E)))) Pack {
-              E e[4];
-            } out;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) out.e[i] = (E)(c.scale * y[tt][e][i]);
-            if (have >= 4) {
-              *reinterpret_cast<Pack*>(to + 16 * e) = out;
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (i < have) to[16 * e + i] = out.e[i];
-            }
-          }
-        }
+          for (int e = 0; e < 2; ++e)
+            lin_store<E>(r, to + 16 * tt * out_row, vc + 16 * e + 4 * q, c.V, c.scale * y[tt][e], w.quads);
       }
+      if (any) read_values();
     }
     // the state after the chunk
-    const LinDecay d = rows == C ? whole : LinDecay(decay * rows);
+    const LinDecay d = pad == 0 ? whole : LinDecay(decay * (C - pad));
 #pragma unroll
     for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
@@ -427,22 +524,21 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int t = 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j);
           float x = (float)vf[b][e][IN - 1][j];
 #pragma unroll
           for (int p = IN - 2; p >= 0; --p) x += (float)vf[b][e][p][j];
-          v[j] = x * power(rows - 1 - t);
+          v[j] = x * back[j % 4] * tile[TT - 1 - 2 * b - j / 4];
         }
         lin_split(v, xf[e]);
       }
 #pragma unroll
       for (int a = 0; a < 2 * KT; ++a) {
+        __builtin_amdgcn_sched_barrier(0);
         v8bf kf[IN];
 #pragma unroll
         for (int p = 0; p < IN; ++p) {
-          const int row = 32 * b + 4 * q + l / 4, column = a / 2 * 32 + l % 4 * 8 + a % 2 * 4;
-          kf[p] = lin_join(lin_read_turned(lk + p * KPART, row, column, KC),
-                           lin_read_turned(lk + p * KPART, row + 16, column, KC));
+          const int at = p * KPART + turned(32 * b, a / 2, KC) + a % 2 * 8;
+          kf[p] = lin_join(lin_read_turned(lk, at), lin_read_turned(lk, at + 16 * KC * 16));
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) lin_mul<2>(kf, xf[e], S[a][e]);
@@ -455,15 +551,18 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   else if (last && dst >= 0)
     to = c.state + ((size_t)dst * c.G + g) * each;
   if (!to) return;
+  const auto after = uniform_buffer(to, (unsigned)(each * 4));
 #pragma unroll
-  for (int a = 0; a < 2 * KT; ++a)
+  for (int e = 0; e < 2; ++e) {
+    const unsigned at = lin_here(column[e]);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int k = key_of(a, i), v = vc + 16 * e + l;
-        if (k < c.K && v < c.V) to[(size_t)k * c.V + v] = S[a][e][i];
+        const float v = S[a][e][i];  // (a bit cast of the element itself takes the first one)
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), after, (int)state_at(at, a, i), 0, 0);
       }
+  }
 }
 
 // The states before the segments of a cut sequence, in place of the segments'
@@ -491,7 +590,9 @@ __global__ __launch_bounds__(256) void k_lin_join(LinCall c, LinCut w) {
   if (at >= each) return;
   const int src = lin_slot(c.src, seq, c.slots);
   float s = src >= 0 ? c.state[((size_t)src * c.G + g) * each + at] : 0.f;
-  const LinDecay d((double)c.decay[g] * C * w.per);
+  // (the first segment's first chunk may not be full)
+  const double decay = (double)c.decay[g], whole = (double)C * w.per;
+  const LinDecay first(decay * (whole - ((t1 - t0 + C - 1) / C * C - (t1 - t0)))), d(decay * whole);
   const size_t step = (size_t)c.G * each;
   float* p = w.states + ((size_t)base * c.G + g) * each + at;
   for (int k = 0; k < segments; k += kLinJoin) {
@@ -502,7 +603,7 @@ __global__ __launch_bounds__(256) void k_lin_join(LinCall c, LinCut w) {
     for (int j = 0; j < kLinJoin; ++j) {
       if (k + j >= segments) break;
       p[(k + j) * step] = s;
-      s = d(s) + v[j];
+      s = (k + j == 0 ? first(s) : d(s)) + v[j];
     }
   }
 }
@@ -513,8 +614,9 @@ hipError_t lin_prompt_kt(const LinCall& c, const LinCut& w, hipStream_t st) {
   constexpr int lds_sum = IN * (KPART + VPART), lds_out = lds_sum + IN * KPART;
   const unsigned vblocks = (unsigned)((c.V + 32 * kLinWaves - 1) / (32 * kLinWaves));
   const dim3 grid((unsigned)c.G * vblocks, (unsigned)w.segments), threads(64 * kLinWaves);
-  auto out = k_lin_chunks<E, KT, true>;
-  auto sum = k_lin_chunks<E, KT, false>;
+  constexpr bool DIRECT = IN == 1;
+  auto out = DIRECT && w.direct ? k_lin_chunks<E, KT, true, DIRECT> : k_lin_chunks<E, KT, true, false>;
+  auto sum = DIRECT && w.direct ? k_lin_chunks<E, KT, false, DIRECT> : k_lin_chunks<E, KT, false, false>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(out), hipFuncAttributeMaxDynamicSharedMemorySize, lds_out);
   if (e == hipSuccess && w.segments > c.n) {
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(sum), hipFuncAttributeMaxDynamicSharedMemorySize, lds_sum);
