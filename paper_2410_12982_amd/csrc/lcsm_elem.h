@@ -48,6 +48,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, size
   return uniform_buffer(static_cast<const E*>(p) + row * stride, bytes);
 }
 
+// 16 bytes a lane from `lane_at` + `at` of a buffer into LDS, one lane after
+// another.  The compiler does not wait for these where LDS is read.
+__device__ __forceinline__ void fetch_to_lds(__amdgpu_buffer_rsrc_t r, unsigned lane_at, unsigned at, char* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, (int)lane_at, (int)at, 0, 0);
+}
+
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 // The reciprocal is good to an ulp.
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + exp2_hw(-1.44269504f * v)); }

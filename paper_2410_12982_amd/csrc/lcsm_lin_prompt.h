@@ -193,12 +193,6 @@ __device__ __forceinline__ void lin_load(const E* p, int have, v8bf (&to)[P]) {
   }
 }
 
-// 16 bytes a lane from a buffer into LDS, one lane after another.  The compiler does
-// not wait for these where LDS is read.
-__device__ __forceinline__ void lin_fetch(__amdgpu_buffer_rsrc_t r, unsigned at, char* to) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, (int)at, 0, 0, 0);
-}
-
 // A chunk's rows into LDS, `width` values of each (zeros past them): `pad` rows of
 // zeros, then those of `from`.  DIRECT: straight from memory (bf16 rows of whole
 // and aligned eights); the caller waits for them.
@@ -216,7 +210,7 @@ __device__ __forceinline__ void lin_stage(char* lds, const E* from, size_t strid
     const unsigned at = lin_here((unsigned)(row - pad) * each + 16u * (unsigned)chunk);
 #pragma unroll
     for (int i = 0; i < C / STEP; ++i)
-      lin_fetch(r, 8 * chunk < width ? at + (unsigned)(i * STEP) * each : kLinNowhere, lds + (i * THREADS + 64 * wv) * 16);
+      fetch_to_lds(r, 8 * chunk < width ? at + (unsigned)(i * STEP) * each : kLinNowhere, 0, lds + (i * THREADS + 64 * wv) * 16);
   } else {
 #pragma unroll 2
     for (int i = 0; i < C * CHUNKS; i += THREADS) {

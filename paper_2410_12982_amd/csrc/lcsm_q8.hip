@@ -200,6 +200,117 @@ hipError_t launch_few(const Q8Call& c, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Many rows.  A workgroup of WN x WX waves takes WN NT tiles of outputs and WX RT
+// of rows, a wave NT x RT of them, in registers.  The tiles of 64 inputs go from
+// memory straight into one of four stages in LDS, three stages ahead of the one
+// that is multiplied.
+constexpr int kStages = 4;
+
+// All waves past their LDS reads; transfers into LDS stay on their way, which
+// __syncthreads would wait for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <class E, int WN, int WX, int NT, int RT>
+__global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
+  constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // tiles a wave fetches
+  constexpr int STAGE = (TN + TX) * 1024;
+  static_assert((TN + TX) % WAVES == 0 && EACH == 4, "the waits below count four transfers a stage");
+  extern __shared__ __align__(16) char lds[];
+  const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wn = wv / WX, wx = wv % WX;
+  const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16;
+  const int gn = (nts + TN - 1) / TN, gx = (rts + TX - 1) / TX;
+  // Workgroup b runs on XCD b % 8: each XCD (and its L2) takes a contiguous range
+  // of the tiles, ordered so that those at work together share rows and outputs.
+  constexpr int GROUP = 4;  // row pieces that go through the outputs together
+  const int total = gn * gx, per = total / 8, rest = total % 8, xcd = (int)blockIdx.x % 8;
+  const int id = xcd * per + min(xcd, rest) + (int)blockIdx.x / 8;
+  const int group = id / (GROUP * gn), first = group * GROUP, have = min(GROUP, gx - first);
+  const int pn = (id - first * gn) / have, px = first + (id - first * gn) % have;
+  // what this wave fetches: tiles of outputs first, then of rows (past the last
+  // one the last one again: what is made of it is not stored)
+  __amdgpu_buffer_rsrc_t from[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int t = wv * EACH + i;
+    const char* p = t < TN ? c.codes + (size_t)min(pn * TN + t, nts - 1) * c.kb * 1024
+                           : c.row_codes + (size_t)min(px * TX + t - TN, rts - 1) * c.kb * 1024;
+    from[i] = uniform_buffer(p, (unsigned)c.kb * 1024u);
+  }
+  auto fetch = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      fetch_to_lds(from[i], lane * 16u, k * 1024u, lds + k % kStages * STAGE + (wv * EACH + i) * 1024);
+  };
+  v4i acc[NT][RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kStages - 1; ++k)
+    if (k < c.kb) fetch(k);
+  for (int k = 0; k < c.kb; ++k) {
+    // this wave's transfers of stage k have arrived, those of the next two may be on
+    // their way; then all waves' have, and stage k - 1 has been read
+    if (k + kStages - 1 <= c.kb)
+      asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    if (k + kStages - 1 < c.kb) fetch(k + kStages - 1);
+    const v4i* at = reinterpret_cast<const v4i*>(lds + k % kStages * STAGE) + lane;
+    v4i a[NT], b[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) b[r] = at[(TN + wx * RT + r) * 64];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) a[t] = at[(wn * NT + t) * 64];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t], b[r], acc[t][r], 0, 0, 0);
+  }
+  // outputs 4 q ..+3 of tile t, row l of tile r
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = (px * TX + wx * RT + r) * 16 + l;
+    if (row >= c.rows) continue;
+    const float s = c.row_scales[row];
+    E* y = static_cast<E*>(c.y) + (size_t)row * c.y_stride;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int n = (pn * TN + wn * NT + t) * 16 + 4 * q;
+      struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+        E e[4];
+      } out;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = min(n + i, c.N - 1);
+        const float v = (float)acc[t][r][i] * c.scales[at] * s;
+        out.e[i] = (E)(c.bias ? v + c.bias[at] : v);
+      }
+      if (n + 4 <= c.N) {
+        *reinterpret_cast<Pack*>(y + n) = out;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < c.N) y[n + i] = out.e[i];
+      }
+    }
+  }
+}
+
+template <class E, int WN, int WX, int NT, int RT>
+hipError_t launch_many(const Q8Call& c, hipStream_t st) {
+  constexpr int TN = WN * NT, TX = WX * RT, LDS = kStages * (TN + TX) * 1024;
+  const long long gn = ((c.N + 15) / 16 + TN - 1) / TN, gx = ((c.rows + 15) / 16 + TX - 1) / TX;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q8_many<E, WN, WX, NT, RT>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_q8_many<E, WN, WX, NT, RT>), dim3((unsigned)(gn * gx)), dim3(64 * WN * WX), LDS, st, c);
+  return hipGetLastError();
+}
+
 template <class E>
 hipError_t launch_q8(const Q8Call& c, hipStream_t st) {
   hipLaunchKernelGGL((k_q8_rows<E, true>), dim3((unsigned)((c.rows + 3) / 4)), dim3(256), 0, st, c.x, c.x_stride, c.rows,
@@ -207,7 +318,10 @@ hipError_t launch_q8(const Q8Call& c, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (c.rows <= 16) return launch_few<E, 1, 1>(c, st);
-  return launch_few<E, 2, 2>(c, st);
+  if (c.rows <= 64) return launch_few<E, 2, 2>(c, st);
+  const long long n = c.N, r = c.rows;
+  if (((n + 255) / 256) * ((r + 255) / 256) >= 192) return launch_many<E, 2, 4, 8, 4>(c, st);
+  return launch_many<E, 2, 2, 4, 4>(c, st);
 }
 
 unsigned blocks(size_t n) {
