@@ -17,6 +17,7 @@ namespace lcsm {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kTileK = 64;   // inputs of a tile, of 16 rows
 constexpr int kPadK = 128;   // inputs are padded to whole pairs of tiles
@@ -31,6 +32,7 @@ struct Q8Call {
   const float *scales, *bias;  // bias NULL: none
   char* row_codes;
   float* row_scales;
+  int quads;  // four outputs are aligned as one, rows of them reach less than 2^32 bytes
 };
 
 // ---- quantizing
@@ -53,64 +55,228 @@ struct Codes {
     if (fabsf(r) > sf || (fabsf(r) == sf && (c & 1))) c += r > 0.f ? 1 : -1;
     return inv > 0.f ? min(max(c, -127), 127) : 0;
   }
+  // Four codes a word.  x inv is within 2^-17 of x / s, so that its nearest integer
+  // is the code where it is not that close to a border; where one value of a wave
+  // is, all are made as above (a quarter of the instructions without).
+  template <int N>
+  __device__ void words(const float (&x)[N], int (&to)[N / 4]) const {
+    constexpr float M = 12582912.f;  // 1.5 2^23: an integer added to it is in its low bits
+    float b[N], worst = f == 1.f && inv > 0.f ? 0.f : 1.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      b[i] = fmaf(x[i], inv, M);
+      worst = fmaxf(worst, fabsf(fmaf(x[i], inv, M - b[i])));
+    }
+    if (__any(!(worst < 0.4999f))) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i)
+        to[i] = ((*this)(x[4 * i]) & 255) | ((*this)(x[4 * i + 1]) & 255) << 8 | ((*this)(x[4 * i + 2]) & 255) << 16 |
+                (int)((unsigned)(*this)(x[4 * i + 3]) << 24);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const unsigned lo = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b[4 * i + 1]), __builtin_bit_cast(unsigned, b[4 * i]), 0x0c0c0400u);
+        const unsigned hi = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b[4 * i + 3]), __builtin_bit_cast(unsigned, b[4 * i + 2]), 0x04000c0cu);
+        to[i] = (int)(lo | hi);
+      }
+    }
+  }
 };
 
-__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }
-
-// 16 elements from p, zeros from `have` on; wide accesses of global memory may
+// N elements as they come, zeros from `have` on; wide accesses of global memory may
 // begin at any element.
+template <class E, int N>
+struct Raw {
+  typedef unsigned short v2h __attribute__((ext_vector_type(2)));
+  static constexpr int WORDS = N * (int)sizeof(E) / 4;
+  unsigned w[WORDS];
+  __device__ void load(const E* p, int have) {
+    struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+      unsigned w[WORDS];
+    };
+    if (have >= N) {
+      const Pack k = *reinterpret_cast<const Pack*>(p);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) w[i] = k.w[i];
+    } else {
+      struct {
+        E e[N];
+      } k;
+#pragma unroll
+      for (int i = 0; i < N; ++i) k.e[i] = i < have ? p[i] : (E)0.f;
+      struct All {
+        unsigned w[WORDS];
+      };
+      const All all = __builtin_bit_cast(All, k);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) w[i] = all.w[i];
+    }
+  }
+  __device__ void values(float (&v)[N]) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (sizeof(E) == 4) {
+        v[i] = __builtin_bit_cast(float, w[i]);
+      } else {
+        v[2 * i] = (float)__builtin_bit_cast(E, (unsigned short)w[i]);
+        v[2 * i + 1] = (float)__builtin_bit_cast(E, (unsigned short)(w[i] >> 16));
+      }
+    }
+  }
+  // The larger of `most` and the magnitudes, as their bits, whose order is theirs
+  // (NaN above all); two of them a word where elements have 16 bits.
+  __device__ unsigned larger(unsigned most) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (sizeof(E) == 4) {
+        const unsigned m = w[i] & 0x7fffffffu;
+        most = m > most ? m : most;
+      } else {
+        most = both(most, w[i] & 0x7fff7fffu);
+      }
+    }
+    return most;
+  }
+  static __device__ unsigned both(unsigned a, unsigned b) {
+    if constexpr (sizeof(E) == 4)
+      return b > a ? b : a;
+    else
+      return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b)));
+  }
+  // The magnitude that `most` stands for.
+  static __device__ float magnitude(unsigned most) {
+    if constexpr (sizeof(E) == 4) {
+      return __builtin_bit_cast(float, most);
+    } else {
+      const unsigned a = most & 0xffffu, b = most >> 16;
+      return (float)__builtin_bit_cast(E, (unsigned short)(b > a ? b : a));
+    }
+  }
+};
+
+// Rows into tiles, 16 rows a workgroup; a wave takes every so many'th tile, of which
+// the first HELD stay in its registers while the rows' largest magnitudes are
+// found (the others are read again).
 template <class E>
-__device__ __forceinline__ void load16(const E* p, int have, float (&v)[16]) {
-  struct __attribute__((packed, aligned(sizeof(E)))) Pack {
-    E e[16];
+__global__ __launch_bounds__(256) void k_q8_rows(const void* x, size_t x_stride, int rows, int K, int kb,
+                                                 char* __restrict__ codes, float* __restrict__ scales) {
+  constexpr int HELD = 8;
+  typedef Raw<E, 16> R;
+  __shared__ unsigned part[4][16];  // [waves][rows]
+  const int lane = (int)threadIdx.x & 63, nw = (int)blockDim.x >> 6;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int q = lane >> 4, l = lane & 15;
+  const size_t row = (size_t)blockIdx.x * 16 + l;
+  // (rows past the last one are the last one again, and not stored)
+  const E* p = static_cast<const E*>(x) + (row < (size_t)rows ? row : (size_t)rows - 1) * x_stride;
+  auto load = [&](int t, R& to) {
+    const int k = t * kTileK + 16 * q;
+    to.load(p + min(k, K - 1), K - k);
   };
-  if (have >= 16) {
-    const Pack k = *reinterpret_cast<const Pack*>(p);
+  R held[HELD];
+  unsigned most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = (float)k.e[i];
-  } else {
+  for (int i = 0; i < HELD; ++i)
+    if (wv + i * nw < kb) load(wv + i * nw, held[i]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = i < have ? (float)p[i] : 0.f;
+  for (int i = 0; i < HELD; ++i)
+    if (wv + i * nw < kb) most = held[i].larger(most);
+  for (int t = wv + HELD * nw; t < kb; t += nw) {
+    R v;
+    load(t, v);
+    most = v.larger(most);
+  }
+  most = R::both(most, __shfl_xor(most, 16));
+  most = R::both(most, __shfl_xor(most, 32));
+  if (q == 0) part[wv][l] = most;
+  __syncthreads();
+  for (int w = 0; w < nw; ++w) most = R::both(most, part[w][l]);
+  const Codes code(R::magnitude(most));
+  if (threadIdx.x < 16 && row < (size_t)rows) scales[row] = code.s;
+  v4i* to = reinterpret_cast<v4i*>(codes) + (size_t)blockIdx.x * kb * 64 + lane;
+  auto store = [&](int t, const R& raw) {
+    float v[16];
+    raw.values(v);
+    int w[4];
+    code.words(v, w);
+    to[(size_t)t * 64] = v4i{w[0], w[1], w[2], w[3]};
+  };
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (wv + i * nw < kb) store(wv + i * nw, held[i]);
+  for (int t = wv + HELD * nw; t < kb; t += nw) {
+    R v;
+    load(t, v);
+    store(t, v);
   }
 }
 
-// A wave a row.  TILES: into tiles (padded with zeros to whole tiles), else the
-// codes one after another.
-template <class E, bool TILES>
-__global__ __launch_bounds__(256) void k_q8_rows(const void* x, size_t x_stride, int rows, int K, int kb,
-                                                 char* __restrict__ codes, float* __restrict__ scales) {
+// The same where there are few rows: a workgroup a row, four inputs a thread.
+template <class E>
+__global__ __launch_bounds__(512) void k_q8_row(const void* x, size_t x_stride, int K, int kb,
+                                                char* __restrict__ codes, float* __restrict__ scales) {
+  constexpr int HELD = 4, THREADS = 512;
+  typedef Raw<E, 4> R;
+  __shared__ unsigned part[THREADS / 64];
+  const size_t row = blockIdx.x;
+  const E* p = static_cast<const E*>(x) + row * x_stride;
+  const int first = 4 * (int)threadIdx.x, end = kb * kTileK;
+  R held[HELD];
+  unsigned most = 0;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int k = first + i * 4 * THREADS;
+    if (k < end) held[i].load(p + min(k, K - 1), K - k);
+  }
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (first + i * 4 * THREADS < end) most = held[i].larger(most);
+  for (int k = first + HELD * 4 * THREADS; k < end; k += 4 * THREADS) {
+    R v;
+    v.load(p + min(k, K - 1), K - k);
+    most = v.larger(most);
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) most = R::both(most, __shfl_xor(most, m));
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) most = R::both(most, part[w]);
+  const Codes code(R::magnitude(most));
+  if (threadIdx.x == 0) scales[row] = code.s;
+  char* to = codes + row / 16 * kb * 1024 + row % 16 * 16;
+  auto store = [&](int k, const R& raw) {
+    float v[4];
+    raw.values(v);
+    int w[1];
+    code.words(v, w);
+    *reinterpret_cast<int*>(to + (size_t)(k / kTileK) * 1024 + k % kTileK / 16 * 256 + k % 16) = w[0];
+  };
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (first + i * 4 * THREADS < end) store(first + i * 4 * THREADS, held[i]);
+  for (int k = first + HELD * 4 * THREADS; k < end; k += 4 * THREADS) {
+    R v;
+    v.load(p + min(k, K - 1), K - k);
+    store(k, v);
+  }
+}
+
+// Weights: a wave a row, the codes one after another.
+__global__ __launch_bounds__(256) void k_q8_quantize(const float* __restrict__ w, int rows, int K,
+                                                     char* __restrict__ codes, float* __restrict__ scales) {
   const int lane = (int)threadIdx.x & 63;
   const long long row = (long long)blockIdx.x * 4 + threadIdx.x / 64;
   if (row >= rows) return;
-  const E* p = static_cast<const E*>(x) + (size_t)row * x_stride;
-  float most = 0.f;
-  for (int k = 16 * lane; k < K; k += 1024) {
-    float v[16];
-    load16(p + k, K - k, v);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) most = larger(most, fabsf(v[i]));
-  }
+  const float* p = w + (size_t)row * K;
+  unsigned most = 0;
+  auto larger = [](unsigned a, unsigned b) { return b > a ? b : a; };
+  for (int k = lane; k < K; k += 64) most = larger(most, __builtin_bit_cast(unsigned, fabsf(p[k])));
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
-  const Codes code(most);
+  const Codes code(__builtin_bit_cast(float, most));
   if (lane == 0) scales[row] = code.s;
-  const int end = TILES ? kb * kTileK : K;
-  for (int k = 16 * lane; k < end; k += 1024) {
-    float v[16];
-    load16(p + k, K - k, v);
-    v4i w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = (code(v[4 * i]) & 255) | (code(v[4 * i + 1]) & 255) << 8 | (code(v[4 * i + 2]) & 255) << 16 |
-             (int)((unsigned)code(v[4 * i + 3]) << 24);
-    if constexpr (TILES) {
-      const size_t tile = (size_t)(row / 16) * kb + k / kTileK;
-      *reinterpret_cast<v4i*>(codes + tile * 1024 + (k % kTileK / 16 * 16 + row % 16) * 16) = w;
-    } else {
-      char* to = codes + (size_t)row * K + k;
-      for (int i = 0; i < 16 && k + i < K; ++i) to[i] = (char)(w[i / 4] >> (8 * (i % 4)));
-    }
-  }
+  for (int k = lane; k < K; k += 64) codes[(size_t)row * K + k] = (char)code(p[k]);
 }
 
 // Weights [M][N][K] as tiles [M][nts][kb][64][16], zeros past N and K.
@@ -134,13 +300,30 @@ __global__ __launch_bounds__(256) void k_q8_codes(const int8_t* __restrict__ src
 
 // ---- products
 
-// A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
-// every so many'th tile along K, and their sums meet in LDS.
-constexpr int kAhead = 4;  // tiles along K on their way
+// Four outputs as one.
+template <class T>
+__device__ __forceinline__ void store_quad(__amdgpu_buffer_rsrc_t r, unsigned at, const T& out) {
+  typedef unsigned v2u __attribute__((ext_vector_type(2)));
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  if constexpr (sizeof(T) == 16)
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, out), r, (int)at, 0, 0);
+  else
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), r, (int)at, 0, 0);
+}
 
-template <class E, int RT, int NT>
-__global__ __launch_bounds__(1024) void k_q8_few(Q8Call c) {
-  extern __shared__ __align__(16) v4i part[];  // [waves][NT][RT][64]
+// A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
+// every so many'th tile along K, and their sums meet in LDS.  OWN: the workgroup
+// quantizes the rows itself, into LDS, under the weights' loads: as long as they
+// are few, that is less than a launch of its own.
+constexpr int kAhead = 4;   // tiles along K on their way
+constexpr int kPiece = 256;  // inputs of a row that a wave quantizes at once
+constexpr int kPieces = 4;   // and how many of them
+
+template <class E, int RT, int NT, bool OWN>
+__global__ __launch_bounds__(512) void k_q8_few(Q8Call c) {
+  static_assert(!OWN || RT == 1, "up to 16 rows");
+  extern __shared__ __align__(16) v4i part[];  // [waves][NT][RT][64]; OWN: codes [rows][kb][4] before
+  __shared__ unsigned most[16];                // of the rows, as the bits of magnitudes
   const int lane = (int)threadIdx.x & 63, nw = (int)blockDim.x >> 6;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16;
@@ -150,20 +333,67 @@ __global__ __launch_bounds__(1024) void k_q8_few(Q8Call c) {
   for (int t = 0; t < NT; ++t) w[t] = reinterpret_cast<const v4i*>(c.codes) + (size_t)min(nt0 + t, nts - 1) * c.kb * 64 + lane;
 #pragma unroll
   for (int r = 0; r < RT; ++r) x[r] = reinterpret_cast<const v4i*>(c.row_codes) + (size_t)min(rt0 + r, rts - 1) * c.kb * 64 + lane;
-  v4i acc[NT][RT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
-  for (int k0 = wv; k0 < c.kb; k0 += kAhead * nw) {
-    v4i a[kAhead][NT], b[kAhead][RT];
+  v4i a[kAhead][NT], b[kAhead][RT], acc[NT][RT];
+  auto load = [&](int k0) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int k = min(k0 + u * nw, c.kb - 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) a[u][t] = w[t][(size_t)k * 64];
+      if (!OWN) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) b[u][r] = x[r][(size_t)k * 64];
+        for (int r = 0; r < RT; ++r) b[u][r] = x[r][(size_t)k * 64];
+      }
+    }
+  };
+  load(wv);
+  if constexpr (OWN) {
+    const int pieces = (c.K + kPiece - 1) / kPiece, all = c.rows * pieces;
+    typedef Raw<E, 4> R;
+    R v[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int id = wv + j * nw, row = id / pieces, k = id % pieces * kPiece + 4 * lane;
+      if (id < all) v[j].load(static_cast<const E*>(c.x) + (size_t)row * c.x_stride + min(k, c.K - 1), c.K - k);
+    }
+    if (threadIdx.x < 16) most[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int id = wv + j * nw;
+      if (id >= all) break;
+      unsigned m = v[j].larger(0);
+#pragma unroll
+      for (int e = 1; e < 64; e *= 2) m = R::both(m, __shfl_xor(m, e));
+      // (the order of these changes nothing)
+      if (lane == 0) atomicMax(&most[id / pieces], __builtin_bit_cast(unsigned, R::magnitude(m)));
+    }
+    __syncthreads();
+    int* codes = reinterpret_cast<int*>(part);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int id = wv + j * nw, row = id / pieces, k = id % pieces * kPiece + 4 * lane;
+      if (id >= all) break;
+      const Codes code(__builtin_bit_cast(float, most[row]));
+      float x[4];
+      v[j].values(x);
+      int word[1];
+      code.words(x, word);
+      if (k < c.kb * kTileK) codes[(row * c.kb * kTileK + k) / 4] = word[0];
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
+  for (int k0 = wv; k0 < c.kb; k0 += kAhead * nw) {
+    if (k0 > wv) load(k0);
+    if constexpr (OWN) {
+      const int row = lane & 15, q = lane >> 4;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)  // rows past the last one: what is made of them is not stored
+        b[u][0] = part[(min(row, c.rows - 1) * c.kb + min(k0 + u * nw, c.kb - 1)) * 4 + q];
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -174,6 +404,7 @@ __global__ __launch_bounds__(1024) void k_q8_few(Q8Call c) {
         for (int r = 0; r < RT; ++r) acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][t], b[u][r], acc[t][r], 0, 0, 0);
     }
   }
+  if (OWN) __syncthreads();  // the codes have been read
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -187,141 +418,253 @@ __global__ __launch_bounds__(1024) void k_q8_few(Q8Call c) {
     const int i = (t * RT + r / 16) * 256 + (o % 16 / 4 * 16 + r % 16) * 4 + o % 4;
     int v = 0;
     for (int k = 0; k < nw; ++k) v += sum[k * NT * RT * 256 + i];
-    const float y = (float)v * c.scales[n] * c.row_scales[at];
-    static_cast<E*>(c.y)[(size_t)at * c.y_stride + n] = (E)(c.bias ? y + c.bias[n] : y);
+    const float s = OWN ? Codes(__builtin_bit_cast(float, most[at])).s : c.row_scales[at];
+    static_cast<E*>(c.y)[(size_t)at * c.y_stride + n] = (E)fmaf((float)v * c.scales[n], s, c.bias ? c.bias[n] : 0.f);
   }
 }
 
-template <class E, int RT, int NT>
-hipError_t launch_few(const Q8Call& c, hipStream_t st) {
-  const int waves = c.kb < 8 ? c.kb : 8;
+template <class E, int RT, int NT, bool OWN>
+hipError_t launch_few(const Q8Call& c, int waves, hipStream_t st) {
+  if (waves > c.kb) waves = c.kb;
   const dim3 grid((unsigned)(((c.N + 15) / 16 + NT - 1) / NT), (unsigned)((c.rows + 16 * RT - 1) / (16 * RT)));
-  hipLaunchKernelGGL((k_q8_few<E, RT, NT>), grid, dim3(64 * waves), (size_t)waves * NT * RT * 1024, st, c);
+  size_t lds = (size_t)waves * NT * RT * 1024;
+  if (OWN && lds < (size_t)c.rows * c.kb * kTileK) lds = (size_t)c.rows * c.kb * kTileK;
+  hipLaunchKernelGGL((k_q8_few<E, RT, NT, OWN>), grid, dim3(64 * waves), lds, st, c);
   return hipGetLastError();
 }
 
-// Many rows.  A workgroup of WN x WX waves takes WN NT tiles of outputs and WX RT
-// of rows, a wave NT x RT of them, in registers.  The tiles of 64 inputs go from
-// memory straight into one of four stages in LDS, three stages ahead of the one
-// that is multiplied.
-constexpr int kStages = 4;
+// Many rows.  A workgroup of WN x WX waves takes pieces of WN NT tiles of outputs and
+// WX RT of rows, one after another, a wave NT x RT of them, in registers.  Stages
+// of 64 inputs go from memory straight into LDS, three ahead of the one whose
+// operands are read, which are read a stage ahead of their products; this goes on
+// from one piece to the next, whose first stages arrive while the last piece's
+// outputs are made and stored.
 
-// All waves past their LDS reads; transfers into LDS stay on their way, which
-// __syncthreads would wait for.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All waves past their LDS reads; transfers stay on their way, which __syncthreads
+// would wait for.  (The wait is one that the compiler sees, so that it does not
+// wait again, for later reads too.)
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// At most N memory instructions of this wave on their way, the oldest done.
+template <int N>
+__device__ __forceinline__ void wait_but() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
-template <class E, int WN, int WX, int NT, int RT>
+template <class E, int WN, int WX, int NT, int RT, int STAGES>
 __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
-  constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // tiles a wave fetches
+  constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // tiles a wave fetches of a stage
   constexpr int STAGE = (TN + TX) * 1024;
-  static_assert((TN + TX) % WAVES == 0 && EACH == 4, "the waits below count four transfers a stage");
+  static_assert((TN + TX) % WAVES == 0, "the waits below count the transfers of a stage");
   extern __shared__ __align__(16) char lds[];
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wn = wv / WX, wx = wv % WX;
-  const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16;
+  const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16, kb = c.kb;
   const int gn = (nts + TN - 1) / TN, gx = (rts + TX - 1) / TX;
   // Workgroup b runs on XCD b % 8: each XCD (and its L2) takes a contiguous range
-  // of the tiles, ordered so that those at work together share rows and outputs.
-  constexpr int GROUP = 4;  // row pieces that go through the outputs together
+  // of the pieces, ordered so that those at work together share rows and outputs.
+  constexpr int GROUP = 4;  // rows of pieces that go through the outputs together
   const int total = gn * gx, per = total / 8, rest = total % 8, xcd = (int)blockIdx.x % 8;
-  const int id = xcd * per + min(xcd, rest) + (int)blockIdx.x / 8;
-  const int group = id / (GROUP * gn), first = group * GROUP, have = min(GROUP, gx - first);
-  const int pn = (id - first * gn) / have, px = first + (id - first * gn) % have;
+  const int begin = xcd * per + min(xcd, rest), end = begin + per + (xcd < rest ? 1 : 0);
+  const int step = (int)gridDim.x / 8, mine = begin + (int)blockIdx.x / 8;
+  if (mine >= end) return;
+  const int turns = ((end - mine + step - 1) / step) * kb;
+  auto place = [&](int id, int& pn, int& px) {
+    const int first = id / (GROUP * gn) * GROUP, have = min(GROUP, gx - first), at = id - first * gn;
+    pn = at / have;
+    px = first + at % have;
+  };
   // what this wave fetches: tiles of outputs first, then of rows (past the last
   // one the last one again: what is made of it is not stored)
   __amdgpu_buffer_rsrc_t from[EACH];
+  int fetch_id = mine, fetch_k = 0;
+  auto locate = [&]() {
+    int pn, px;
+    place(fetch_id, pn, px);
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    const int t = wv * EACH + i;
-    const char* p = t < TN ? c.codes + (size_t)min(pn * TN + t, nts - 1) * c.kb * 1024
-                           : c.row_codes + (size_t)min(px * TX + t - TN, rts - 1) * c.kb * 1024;
-    from[i] = uniform_buffer(p, (unsigned)c.kb * 1024u);
-  }
-  auto fetch = [&](int k) {
+    for (int i = 0; i < EACH; ++i) {
+      const int t = wv * EACH + i;
+      const char* p = t < TN ? c.codes + (size_t)min(pn * TN + t, nts - 1) * kb * 1024
+                             : c.row_codes + (size_t)min(px * TX + t - TN, rts - 1) * kb * 1024;
+      from[i] = uniform_buffer(p, (unsigned)kb * 1024u);
+    }
+  };
+  auto fetch = [&](int stage) {
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      fetch_to_lds(from[i], lane * 16u, k * 1024u, lds + k % kStages * STAGE + (wv * EACH + i) * 1024);
+      fetch_to_lds(from[i], lane * 16u, fetch_k * 1024u, lds + stage % STAGES * STAGE + (wv * EACH + i) * 1024);
+    if (++fetch_k == kb) {
+      fetch_k = 0;
+      fetch_id += step;
+      if (fetch_id < end) locate();
+    }
+  };
+  struct Operands {
+    v4i a[NT], b[RT];
+  };
+  auto read = [&](int stage, Operands& to) {
+    const v4i* at = reinterpret_cast<const v4i*>(lds + stage % STAGES * STAGE) + lane;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) to.b[r] = at[(TN + wx * RT + r) * 64];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) to.a[t] = at[(wn * NT + t) * 64];
   };
   v4i acc[NT][RT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
-#pragma unroll
-  for (int k = 0; k < kStages - 1; ++k)
-    if (k < c.kb) fetch(k);
-  for (int k = 0; k < c.kb; ++k) {
-    // this wave's transfers of stage k have arrived, those of the next two may be on
-    // their way; then all waves' have, and stage k - 1 has been read
-    if (k + kStages - 1 <= c.kb)
-      asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  // the products of stage g, whose operands are in registers, while those of the
+  // next one are read
+  auto turn = [&](int g, const Operands& now, Operands& next) {
+    // this wave's transfers of stage g + 1 have arrived, those of two more may be on
+    // their way; then all waves' have, and stage g has been read
+    if (g + STAGES > turns)
+      wait_but<0>();
     else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      wait_but<(STAGES - 2) * EACH>();
     lds_barrier();
-    if (k + kStages - 1 < c.kb) fetch(k + kStages - 1);
-    const v4i* at = reinterpret_cast<const v4i*>(lds + k % kStages * STAGE) + lane;
-    v4i a[NT], b[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) b[r] = at[(TN + wx * RT + r) * 64];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) a[t] = at[(wn * NT + t) * 64];
+    if (g + STAGES < turns) fetch(g + STAGES);
+    read(g + 1, next);  // (after the last stage: what is not used)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t], b[r], acc[t][r], 0, 0, 0);
-  }
-  // outputs 4 q ..+3 of tile t, row l of tile r
+      for (int r = 0; r < RT; ++r) acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now.a[t], now.b[r], acc[t][r], 0, 0, 0);
+  };
+  locate();
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = (px * TX + wx * RT + r) * 16 + l;
-    if (row >= c.rows) continue;
-    const float s = c.row_scales[row];
-    E* y = static_cast<E*>(c.y) + (size_t)row * c.y_stride;
+  for (int g = 0; g < STAGES; ++g)
+    if (g < turns) fetch(g);
+  if (turns >= STAGES)
+    wait_but<(STAGES - 1) * EACH>();
+  else
+    wait_but<0>();
+  lds_barrier();
+  Operands even, odd;
+  read(0, even);
+  for (int id = mine, g = 0; id < end; id += step) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int n = (pn * TN + wn * NT + t) * 16 + 4 * q;
-      struct __attribute__((packed, aligned(sizeof(E)))) Pack {
-        E e[4];
-      } out;
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = min(n + i, c.N - 1);
-        const float v = (float)acc[t][r][i] * c.scales[at] * s;
-        out.e[i] = (E)(c.bias ? v + c.bias[at] : v);
-      }
-      if (n + 4 <= c.N) {
-        *reinterpret_cast<Pack*>(y + n) = out;
+      for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
+    for (int k = 0; k < kb; k += 2, g += 2) {  // (an even number of tiles)
+      turn(g, even, odd);
+      turn(g + 1, odd, even);
+    }
+    // outputs 4 q ..+3 of tile t, row l of tile r; all scales are on their way before
+    // the first is used
+    int pn, px;
+    place(id, pn, px);
+    const int row0 = (px * TX + wx * RT) * 16 + l, n0 = (pn * TN + wn * NT) * 16 + 4 * q;
+    const bool whole = (pn * TN + wn * NT + NT) * 16 <= c.N;  // the same for all lanes
+    v4f scale[NT];
+    float by[RT];
+    auto four = [&](const float* p, int n) {
+      struct __attribute__((packed, aligned(4))) Pack {
+        float f[4];
+      };
+      v4f v;
+      if (whole) {
+        const Pack k = *reinterpret_cast<const Pack*>(p + n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = k.f[i];
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (n + i < c.N) y[n + i] = out.e[i];
+        for (int i = 0; i < 4; ++i) v[i] = p[min(n + i, c.N - 1)];
+      }
+      return v;
+    };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) scale[t] = four(c.scales, n0 + 16 * t);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) by[r] = c.row_scales[min(row0 + 16 * r, c.rows - 1)];
+    struct Out {
+      E e[4];
+    };
+    auto make = [&](int t, int r) {
+      Out out;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out.e[i] = (E)((float)acc[t][r][i] * scale[t][i] * by[r]);
+      return out;
+    };
+    if (whole && !c.bias && c.quads && (px * TX + wx * RT + RT) * 16 <= c.rows) {
+      const unsigned each = (unsigned)c.y_stride * (unsigned)sizeof(E);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const auto y = uniform_buffer(static_cast<E*>(c.y) + (size_t)(px * TX + wx * RT + r) * 16 * c.y_stride +
+                                          (pn * TN + wn * NT) * 16, 15 * each + NT * 16 * (unsigned)sizeof(E));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) store_quad(y, l * each + (16 * t + 4 * q) * (unsigned)sizeof(E), make(t, r));
+      }
+    } else {
+      E* y = static_cast<E*>(c.y) + (size_t)row0 * c.y_stride + n0;
+#pragma unroll
+      for (int r = 0; r < RT; ++r, y += 16 * c.y_stride) {
+        if (row0 + 16 * r >= c.rows) break;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int n = n0 + 16 * t;
+          struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+            E e[4];
+          } out;
+          if (c.bias) {
+            const v4f bias = four(c.bias, n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out.e[i] = (E)fmaf((float)acc[t][r][i] * scale[t][i], by[r], bias[i]);
+          } else {
+            const Out o = make(t, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out.e[i] = o.e[i];
+          }
+          if (whole || n + 4 <= c.N) {
+            *reinterpret_cast<Pack*>(y + 16 * t) = out;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (n + i < c.N) y[16 * t + i] = out.e[i];
+          }
+        }
       }
     }
+    // (stores count among the transfers that the turns wait for; to count them in
+    // there, and leave them on their way, takes the same time)
+    wait_but<0>();
   }
 }
 
-template <class E, int WN, int WX, int NT, int RT>
+template <class E, int WN, int WX, int NT, int RT, int STAGES>
 hipError_t launch_many(const Q8Call& c, hipStream_t st) {
-  constexpr int TN = WN * NT, TX = WX * RT, LDS = kStages * (TN + TX) * 1024;
+  constexpr int TN = WN * NT, TX = WX * RT, LDS = STAGES * (TN + TX) * 1024;
   const long long gn = ((c.N + 15) / 16 + TN - 1) / TN, gx = ((c.rows + 15) / 16 + TX - 1) / TX;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q8_many<E, WN, WX, NT, RT>),
+  const long long room = WN * WX > 4 ? 256 : 512;  // workgroups that fit the card
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q8_many<E, WN, WX, NT, RT, STAGES>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_q8_many<E, WN, WX, NT, RT>), dim3((unsigned)(gn * gx)), dim3(64 * WN * WX), LDS, st, c);
+  const unsigned grid = (unsigned)(gn * gx < room ? (gn * gx + 7) / 8 * 8 : room);
+  hipLaunchKernelGGL((k_q8_many<E, WN, WX, NT, RT, STAGES>), dim3(grid), dim3(64 * WN * WX), LDS, st, c);
   return hipGetLastError();
 }
 
+constexpr int kRowsAlone = 2048;
+
 template <class E>
 hipError_t launch_q8(const Q8Call& c, hipStream_t st) {
-  hipLaunchKernelGGL((k_q8_rows<E, true>), dim3((unsigned)((c.rows + 3) / 4)), dim3(256), 0, st, c.x, c.x_stride, c.rows,
-                     c.K, c.kb, c.row_codes, c.row_scales);
+  const int few = c.kb < 8 ? c.kb : 8;  // waves
+  if (c.rows <= 16 && (long long)c.rows * ((c.K + kPiece - 1) / kPiece) <= kPieces * few)
+    return launch_few<E, 1, 1, true>(c, few, st);
+  if (c.rows < kRowsAlone)
+    hipLaunchKernelGGL((k_q8_row<E>), dim3((unsigned)c.rows), dim3(512), 0, st, c.x, c.x_stride, c.K, c.kb, c.row_codes,
+                       c.row_scales);
+  else
+    hipLaunchKernelGGL((k_q8_rows<E>), dim3((unsigned)((c.rows + 15) / 16)), dim3(64 * (c.kb < 4 ? c.kb : 4)), 0, st, c.x,
+                       c.x_stride, c.rows, c.K, c.kb, c.row_codes, c.row_scales);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (c.rows <= 16) return launch_few<E, 1, 1>(c, st);
-  if (c.rows <= 64) return launch_few<E, 2, 2>(c, st);
+  if (c.rows <= 16) return launch_few<E, 1, 1, false>(c, few, st);
+  if (c.rows <= 64) return launch_few<E, 2, 2, false>(c, few, st);
   const long long n = c.N, r = c.rows;
-  if (((n + 255) / 256) * ((r + 255) / 256) >= 192) return launch_many<E, 2, 4, 8, 4>(c, st);
-  return launch_many<E, 2, 2, 4, 4>(c, st);
+  if (((n + 255) / 256) * ((r + 255) / 256) >= 192) return launch_many<E, 2, 4, 8, 4, 4>(c, st);
+  return launch_many<E, 2, 2, 4, 4, 4>(c, st);
 }
 
 unsigned blocks(size_t n) {
@@ -456,7 +799,8 @@ int lcsm_q8_matmul(lcsm_q8* ctx, int layer, int rows, int dtype, const void* x, 
   const size_t m = (size_t)layer;
   const lcsm::Q8Call c{rows, s.N, s.K, ctx->kb, x, y, x_stride, y_stride, ctx->codes + m * ctx->nts * ctx->kb * 1024,
                        ctx->scales + m * s.N, ctx->bias ? ctx->bias + m * s.N : nullptr, ctx->row_codes,
-                       ctx->row_scales};
+                       ctx->row_scales,
+                       (uintptr_t)y % (4 * lcsm::dtype_size(dtype)) == 0 && y_stride % 4 == 0 && y_stride <= lcsm::kMaxStride};
   const hipError_t e = lcsm::with_dtype(dtype, [&](auto v) { return lcsm::launch_q8<decltype(v)>(c, ctx->stream); });
   return e == hipSuccess ? LCSM_OK : q8_fail(ctx, LCSM_EDEVICE, "product launch", e);
 }
@@ -465,8 +809,8 @@ int lcsm_q8_quantize(const float* w, int rows, int K, void* codes, float* scales
   if (rows < 0 || K < 1 || K > (1 << 24)) return LCSM_EINVAL;
   if (!rows) return LCSM_OK;
   if (!w || !codes || !scales) return LCSM_EINVAL;
-  hipLaunchKernelGGL((lcsm::k_q8_rows<float, false>), dim3((unsigned)(((long long)rows + 3) / 4)), dim3(256), 0,
-                     (hipStream_t)stream, w, (size_t)K, rows, K, 0, (char*)codes, scales);
+  hipLaunchKernelGGL(lcsm::k_q8_quantize, dim3((unsigned)(((long long)rows + 3) / 4)), dim3(256), 0, (hipStream_t)stream, w,
+                     rows, K, (char*)codes, scales);
   return hipGetLastError() == hipSuccess ? LCSM_OK : LCSM_EDEVICE;
 }
 
