@@ -62,8 +62,8 @@ int lcsm_q8_init(lcsm_q8** out, const lcsm_q8_shape* shape, const void* codes, c
 /* y [rows][N] from x [rows][K], both of type dtype; a row is contiguous, rows
  * are `_stride` elements apart.  x and y do not overlap.  rows = 0 queues
  * nothing.  Errors: LCSM_EINVAL (null pointers, layer, dtype or strides out of
- * range, rows below zero or above max_rows), LCSM_ESTATE after a fault (until
- * lcsm_q8_reset), LCSM_EDEVICE. */
+ * range, rows below zero or above max_rows, more than 2^42 outputs),
+ * LCSM_ESTATE after a fault (until lcsm_q8_reset), LCSM_EDEVICE. */
 int lcsm_q8_matmul(lcsm_q8* ctx, int layer, int rows, int dtype, const void* x, size_t x_stride,
                    void* y, size_t y_stride);
 

@@ -435,8 +435,8 @@ hipError_t launch_few(const Q8Call& c, int waves, hipStream_t st) {
 
 // Many rows.  A workgroup of WN x WX waves takes pieces of WN NT tiles of outputs and
 // WX RT of rows, one after another, a wave NT x RT of them, in registers.  Stages
-// of 64 inputs go from memory straight into LDS, three ahead of the one whose
-// operands are read, which are read a stage ahead of their products; this goes on
+// of KT tiles of inputs go from memory straight into LDS, STAGES - 1 ahead of the
+// one whose operands are read, which are read a stage ahead of their products; this goes on
 // from one piece to the next, whose first stages arrive while the last piece's
 // outputs are made and stored.
 
@@ -455,15 +455,15 @@ __device__ __forceinline__ void wait_but() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <class E, int WN, int WX, int NT, int RT, int STAGES>
+template <class E, int WN, int WX, int NT, int RT, int KT, int STAGES>
 __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
-  constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // tiles a wave fetches of a stage
-  constexpr int STAGE = (TN + TX) * 1024;
-  static_assert((TN + TX) % WAVES == 0, "the waits below count the transfers of a stage");
+  constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // rows of tiles that a wave fetches
+  constexpr int STAGE = (TN + TX) * KT * 1024;
+  static_assert((TN + TX) % WAVES == 0 && (STAGES - 1) * EACH * KT < 64, "the waits below count the transfers of a stage");
   extern __shared__ __align__(16) char lds[];
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wn = wv / WX, wx = wv % WX;
-  const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16, kb = c.kb;
+  const int nts = (c.N + 15) / 16, rts = (c.rows + 15) / 16, kb = c.kb, ns = kb / KT;
   const int gn = (nts + TN - 1) / TN, gx = (rts + TX - 1) / TX;
   // Workgroup b runs on XCD b % 8: each XCD (and its L2) takes a contiguous range
   // of the pieces, ordered so that those at work together share rows and outputs.
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
   const int begin = xcd * per + min(xcd, rest), end = begin + per + (xcd < rest ? 1 : 0);
   const int step = (int)gridDim.x / 8, mine = begin + (int)blockIdx.x / 8;
   if (mine >= end) return;
-  const int turns = ((end - mine + step - 1) / step) * kb;
+  const int turns = ((end - mine + step - 1) / step) * ns;
   auto place = [&](int id, int& pn, int& px) {
     const int first = id / (GROUP * gn) * GROUP, have = min(GROUP, gx - first), at = id - first * gn;
     pn = at / have;
@@ -493,63 +493,79 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
       from[i] = uniform_buffer(p, (unsigned)kb * 1024u);
     }
   };
-  auto fetch = [&](int stage) {
+  int fetch_to = 0, read_at = 0;  // places in LDS
+  auto fetch = [&]() {
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      fetch_to_lds(from[i], lane * 16u, fetch_k * 1024u, lds + stage % STAGES * STAGE + (wv * EACH + i) * 1024);
-    if (++fetch_k == kb) {
+#pragma unroll
+      for (int j = 0; j < KT; ++j)
+        fetch_to_lds(from[i], lane * 16u, (unsigned)(fetch_k + j) * 1024u, lds + fetch_to + ((wv * EACH + i) * KT + j) * 1024);
+    fetch_to = fetch_to + STAGE < STAGES * STAGE ? fetch_to + STAGE : 0;
+    fetch_k += KT;
+    if (fetch_k == kb) {
       fetch_k = 0;
       fetch_id += step;
       if (fetch_id < end) locate();
     }
   };
   struct Operands {
-    v4i a[NT], b[RT];
+    v4i a[KT][NT], b[KT][RT];
   };
-  auto read = [&](int stage, Operands& to) {
-    const v4i* at = reinterpret_cast<const v4i*>(lds + stage % STAGES * STAGE) + lane;
+  auto read = [&](Operands& to) {
+    const v4i* at = reinterpret_cast<const v4i*>(lds + read_at) + lane;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) to.b[r] = at[(TN + wx * RT + r) * 64];
+    for (int j = 0; j < KT; ++j) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) to.a[t] = at[(wn * NT + t) * 64];
+      for (int r = 0; r < RT; ++r) to.b[j][r] = at[((TN + wx * RT + r) * KT + j) * 64];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) to.a[j][t] = at[((wn * NT + t) * KT + j) * 64];
+    }
+    read_at = read_at + STAGE < STAGES * STAGE ? read_at + STAGE : 0;
   };
   v4i acc[NT][RT];
   // the products of stage g, whose operands are in registers, while those of the
   // next one are read
   auto turn = [&](int g, const Operands& now, Operands& next) {
-    // this wave's transfers of stage g + 1 have arrived, those of two more may be on
-    // their way; then all waves' have, and stage g has been read
+    // this wave's transfers of stage g + 1 have arrived, those of the stages after it
+    // may be on their way; then all waves' have, and stage g has been read
     if (g + STAGES > turns)
       wait_but<0>();
     else
-      wait_but<(STAGES - 2) * EACH>();
+      wait_but<(STAGES - 2) * EACH * KT>();
     lds_barrier();
-    if (g + STAGES < turns) fetch(g + STAGES);
-    read(g + 1, next);  // (after the last stage: what is not used)
+    read(next);  // (after the last stage: what is not used)
+    if (g + STAGES < turns) fetch();
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int j = 0; j < KT; ++j)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now.a[t], now.b[r], acc[t][r], 0, 0, 0);
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          acc[t][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now.a[j][t], now.b[j][r], acc[t][r], 0, 0, 0);
   };
   locate();
 #pragma unroll
   for (int g = 0; g < STAGES; ++g)
-    if (g < turns) fetch(g);
+    if (g < turns) fetch();
   if (turns >= STAGES)
-    wait_but<(STAGES - 1) * EACH>();
+    wait_but<(STAGES - 1) * EACH * KT>();
   else
     wait_but<0>();
   lds_barrier();
   Operands even, odd;
-  read(0, even);
+  read(even);
   for (int id = mine, g = 0; id < end; id += step) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < RT; ++r) acc[t][r] = v4i{0, 0, 0, 0};
-    for (int k = 0; k < kb; k += 2, g += 2) {  // (an even number of tiles)
+    for (int k = 0; k + 1 < ns; k += 2, g += 2) {
       turn(g, even, odd);
       turn(g + 1, odd, even);
+    }
+    if (KT > 1 && ns % 2) {  // (tiles come in pairs)
+      turn(g++, even, odd);
+      even = odd;
     }
     // outputs 4 q ..+3 of tile t, row l of tile r; all scales are on their way before
     // the first is used
@@ -632,16 +648,16 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
   }
 }
 
-template <class E, int WN, int WX, int NT, int RT, int STAGES>
+template <class E, int WN, int WX, int NT, int RT, int KT, int STAGES>
 hipError_t launch_many(const Q8Call& c, hipStream_t st) {
-  constexpr int TN = WN * NT, TX = WX * RT, LDS = STAGES * (TN + TX) * 1024;
+  constexpr int TN = WN * NT, TX = WX * RT, LDS = STAGES * (TN + TX) * KT * 1024;
   const long long gn = ((c.N + 15) / 16 + TN - 1) / TN, gx = ((c.rows + 15) / 16 + TX - 1) / TX;
-  const long long room = WN * WX > 4 ? 256 : 512;  // workgroups that fit the card
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q8_many<E, WN, WX, NT, RT, STAGES>),
+  const long long room = LDS > 81920 ? 256 : 512;  // workgroups that fit the card
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_q8_many<E, WN, WX, NT, RT, KT, STAGES>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (e != hipSuccess) return e;
   const unsigned grid = (unsigned)(gn * gx < room ? (gn * gx + 7) / 8 * 8 : room);
-  hipLaunchKernelGGL((k_q8_many<E, WN, WX, NT, RT, STAGES>), dim3(grid), dim3(64 * WN * WX), LDS, st, c);
+  hipLaunchKernelGGL((k_q8_many<E, WN, WX, NT, RT, KT, STAGES>), dim3(grid), dim3(64 * WN * WX), LDS, st, c);
   return hipGetLastError();
 }
 
@@ -660,11 +676,22 @@ hipError_t launch_q8(const Q8Call& c, hipStream_t st) {
                        c.x_stride, c.rows, c.K, c.kb, c.row_codes, c.row_scales);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (c.rows <= 16) return launch_few<E, 1, 1, false>(c, few, st);
-  if (c.rows <= 64) return launch_few<E, 2, 2, false>(c, few, st);
-  const long long n = c.N, r = c.rows;
-  if (((n + 255) / 256) * ((r + 255) / 256) >= 192) return launch_many<E, 2, 4, 8, 4, 4>(c, st);
-  return launch_many<E, 2, 2, 4, 4, 4>(c, st);
+  // Pieces of outputs and rows: the largest that still are workgroups enough, in tiles of 16.  us for
+  // rows x inputs -> outputs, bf16, both launches, as few<RT, NT> 1,1 2,1 2,2, many 64 x 64, 128 x 64, 128 x 128, 256 x 256:
+  //   32 x 2048 -> 2048     6.7  7.0  8.1  11.3   64 x 2048 -> 2048    7.3   7.2   8.2  11.3  13.4   17
+  //   64 x 2048 -> 8192     11   10.5 10.3 11.4  128 x 2048 -> 8192   16    14.6  14.8 11.9  13.9   18
+  //   256 x 8192 -> 2048    31   26   21   30    512 x 2048 -> 2048               16   13    15     20   37
+  //   512 x 2048 -> 8192              42   24   21   22   38   1024 x 2048 -> 8192     80   42   36   31   43
+  //   512 x 4096 -> 16384             150  69   53   45   64   2048 x 2048 -> 8192     158  83   69   60   56
+  const long long n = (c.N + 15) / 16, r = (c.rows + 15) / 16;
+  auto pieces = [&](int tn, int tr) { return ((n + tn - 1) / tn) * ((r + tr - 1) / tr); };
+  if (r == 1 || pieces(1, 1) <= 512) return launch_few<E, 1, 1, false>(c, few, st);
+  if (pieces(1, 2) <= 512) return launch_few<E, 2, 1, false>(c, few, st);
+  if (pieces(2, 2) <= 640) return launch_few<E, 2, 2, false>(c, few, st);
+  if (pieces(16, 16) >= 192) return launch_many<E, 2, 4, 8, 4, 1, 4>(c, st);
+  if (pieces(8, 8) >= 384) return launch_many<E, 2, 2, 4, 4, 1, 5>(c, st);
+  if (pieces(8, 4) >= 384) return launch_many<E, 2, 2, 4, 2, 2, 3>(c, st);
+  return launch_many<E, 2, 2, 2, 2, 2, 5>(c, st);
 }
 
 unsigned blocks(size_t n) {
@@ -790,6 +817,7 @@ int lcsm_q8_matmul(lcsm_q8* ctx, int layer, int rows, int dtype, const void* x, 
   if (rows < 0 || rows > s.max_rows) return q8_fail(ctx, LCSM_EINVAL, "rows below zero or above max_rows");
   if (!lcsm::dtype_ok(dtype)) return q8_fail(ctx, LCSM_EINVAL, "unknown type");
   if (rows > 0) {
+    if ((double)rows * s.N > 4398046511104.0) return q8_fail(ctx, LCSM_EINVAL, "more than 2^42 outputs");
     if (!x || !y) return q8_fail(ctx, LCSM_EINVAL, "null input or output pointer");
     if (x_stride < (size_t)s.K || y_stride < (size_t)s.N)
       return q8_fail(ctx, LCSM_EINVAL, "a row stride is shorter than the row");

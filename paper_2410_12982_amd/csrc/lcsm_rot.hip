@@ -11,6 +11,7 @@
 #include <string.h>
 
 #include <new>
+#include <type_traits>
 
 #include "lcsm_elem.h"
 #include "lcsm_rot.h"
@@ -22,8 +23,8 @@ constexpr int kRotMaxP = 512;
 constexpr int kRotMaxHeads = 65536;
 
 struct RotCall {
-  int rows, P, q_heads, heads, rotary, norm;  // heads: of queries and keys
-  int team, teams;                            // lanes a head; teams a row
+  int rows, P, q_heads, k_heads, rotary, norm;
+  int team, teams, q_teams;  // lanes a head; teams a row, and how many of them have queries
   float eps;
   const void *q, *k;
   void *q_out, *k_out;
@@ -40,29 +41,49 @@ struct __attribute__((packed, aligned(sizeof(E)))) Pack {
   E e[V];
 };
 
+// Sum over the L lanes of a team (a power of two), in a fixed order; every lane
+// gets it.  Once quads have their sums, lanes that lie mirrored in a row of 8 or 16
+// have the other half's.
+__device__ __forceinline__ float team_sum(float v, int L) {
+  auto add = [&](auto dpp) {
+    const int x = __builtin_bit_cast(int, v);
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, x, decltype(dpp)::value, 0xf, 0xf, false));
+  };
+  if (L > 1) add(std::integral_constant<int, 0xB1>());   // quad_perm 1 0 3 2
+  if (L > 2) add(std::integral_constant<int, 0x4E>());   // quad_perm 2 3 0 1
+  if (L > 4) add(std::integral_constant<int, 0x141>());  // row_half_mirror
+  if (L > 8) add(std::integral_constant<int, 0x140>());  // row_mirror
+  if (L > 16) v += __shfl_xor(v, 16);
+  if (L > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
 // A lane has up to CNT items of a head: V pairs, or V values that are not
-// turned; pairs first.
+// turned; pairs first.  A team takes `each` heads of queries, or of keys.
 template <class E, int V, bool HALF, int CNT>
 __global__ __launch_bounds__(256) void k_rot(RotCall c) {
   const int L = c.team, lane = (int)threadIdx.x % L;
   const size_t unit = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / L) + threadIdx.x / L;
   const size_t row = unit / c.teams;
   if (row >= (size_t)c.rows) return;  // whole teams: no lane waits for them
-  const int first = (int)(unit % c.teams), half = c.rotary / 2;
+  const int mine = (int)(unit % c.teams), half = c.rotary / 2;
   const int pairs = half / V, items = pairs + (c.P - c.rotary) / V;
+  const bool key = mine >= c.q_teams;
+  const int first = key ? mine - c.q_teams : mine, step = key ? c.teams - c.q_teams : c.q_teams;
+  const int heads = key ? c.k_heads : c.q_heads;
+  const E* x = key ? static_cast<const E*>(c.k) + row * c.k_stride : static_cast<const E*>(c.q) + row * c.q_stride;
+  E* y = key ? static_cast<E*>(c.k_out) + row * c.k_out_stride : static_cast<E*>(c.q_out) + row * c.q_out_stride;
+  const float* w = key ? c.k_w : c.q_w;
 
-  // of item i: its kind, and where its values are
   auto item = [&](int i) { return i * L + lane; };
   auto at_a = [&](int j) { return j < pairs ? (HALF ? j * V : 2 * j * V) : c.rotary + (j - pairs) * V; };
   Pack<E, V> a[CNT], b[CNT];
   auto load = [&](int h) {
-    const E* x = h < c.q_heads ? static_cast<const E*>(c.q) + row * c.q_stride + (size_t)h * c.P
-                               : static_cast<const E*>(c.k) + row * c.k_stride + (size_t)(h - c.q_heads) * c.P;
 #pragma unroll
     for (int i = 0; i < CNT; ++i) {
       const int j = item(i);
       if (j >= items) continue;
-      const E* p = x + at_a(j);
+      const E* p = x + (size_t)h * c.P + at_a(j);
       if (HALF || j >= pairs) {
         a[i] = *reinterpret_cast<const Pack<E, V>*>(p);
         if (j < pairs) b[i] = *reinterpret_cast<const Pack<E, V>*>(p + half);
@@ -75,27 +96,24 @@ __global__ __launch_bounds__(256) void k_rot(RotCall c) {
   };
   load(first);
 
-  float cs[CNT][V], sn[CNT][V];
-  if (pairs > 0) {
-    const double t = (double)c.positions[row];
+  float wa[CNT][V], wb[CNT][V], cs[CNT][V], sn[CNT][V];
+  const double t = pairs > 0 ? (double)c.positions[row] : 0.0;
 #pragma unroll
-    for (int i = 0; i < CNT; ++i)
+  for (int i = 0; i < CNT; ++i) {
+    const int j = item(i);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int j = item(i);
-        cs[i][e] = 1.f;
-        sn[i][e] = 0.f;
-        if (j >= pairs) continue;
-        const double r = t * c.turns[j * V + e];
-        sincospif((float)(2.0 * (r - rint(r))), &sn[i][e], &cs[i][e]);
-      }
+    for (int e = 0; e < V; ++e) {
+      wa[i][e] = w && j < items ? w[at_a(j) + (HALF || j >= pairs ? e : 2 * e)] : 1.f;
+      wb[i][e] = w && j < pairs ? w[at_a(j) + (HALF ? half + e : 2 * e + 1)] : 1.f;
+      cs[i][e] = 1.f;
+      sn[i][e] = 0.f;
+      if (j >= pairs) continue;
+      const double r = t * c.turns[j * V + e];
+      sincospif((float)(2.0 * (r - rint(r))), &sn[i][e], &cs[i][e]);
+    }
   }
-  auto sum = [&](float v) {
-    for (int m = 1; m < L; m *= 2) v += __shfl_xor(v, m);
-    return v;
-  };
   const float inv = 1.f / (float)c.P;
-  for (int h = first; h < c.heads; h += c.teams) {
+  for (int h = first; h < heads; h += step) {
     float va[CNT][V], vb[CNT][V];
 #pragma unroll
     for (int i = 0; i < CNT; ++i)
@@ -104,7 +122,7 @@ __global__ __launch_bounds__(256) void k_rot(RotCall c) {
         va[i][e] = item(i) < items ? (float)a[i].e[e] : 0.f;
         vb[i][e] = item(i) < pairs ? (float)b[i].e[e] : 0.f;
       }
-    if (h + c.teams < c.heads) load(h + c.teams);
+    if (h + step < heads) load(h + step);
     if (c.norm != LCSM_NORM_NONE) {
       if (c.norm == LCSM_NORM_LAYER) {
         float s = 0.f;
@@ -112,7 +130,7 @@ __global__ __launch_bounds__(256) void k_rot(RotCall c) {
         for (int i = 0; i < CNT; ++i)
 #pragma unroll
           for (int e = 0; e < V; ++e) s += va[i][e] + vb[i][e];
-        const float mean = sum(s) * inv;
+        const float mean = team_sum(s, L) * inv;
 #pragma unroll
         for (int i = 0; i < CNT; ++i)
 #pragma unroll
@@ -126,29 +144,18 @@ __global__ __launch_bounds__(256) void k_rot(RotCall c) {
       for (int i = 0; i < CNT; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) s = fmaf(va[i][e], va[i][e], fmaf(vb[i][e], vb[i][e], s));
-      const float f = 1.f / sqrtf(fmaf(sum(s), inv, c.eps));
-      const float* w = h < c.q_heads ? c.q_w : c.k_w;
+      const float f = 1.f / sqrtf(fmaf(team_sum(s, L), inv, c.eps));
 #pragma unroll
-      for (int i = 0; i < CNT; ++i) {
-        const int j = item(i);
+      for (int i = 0; i < CNT; ++i)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          va[i][e] *= f;
-          vb[i][e] *= f;
-          if (w && j < items) {
-            va[i][e] *= w[at_a(j) + (HALF || j >= pairs ? e : 2 * e)];
-            if (j < pairs) vb[i][e] *= w[at_a(j) + (HALF ? half + e : 2 * e + 1)];
-          }
-        }
-      }
+        for (int e = 0; e < V; ++e) va[i][e] *= f * wa[i][e], vb[i][e] *= f * wb[i][e];
     }
-    E* y = h < c.q_heads ? static_cast<E*>(c.q_out) + row * c.q_out_stride + (size_t)h * c.P
-                         : static_cast<E*>(c.k_out) + row * c.k_out_stride + (size_t)(h - c.q_heads) * c.P;
+    E* to = y + (size_t)h * c.P;
 #pragma unroll
     for (int i = 0; i < CNT; ++i) {
       const int j = item(i);
       if (j >= items) continue;
-      E* p = y + at_a(j);
+      E* p = to + at_a(j);
       Pack<E, V> ra, rb;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
@@ -169,19 +176,20 @@ __global__ __launch_bounds__(256) void k_rot(RotCall c) {
   }
 }
 
-// Heads that a team goes through where there are rows enough to fill the card
-// without: the lanes' sines and cosines are made once for them.
-constexpr int kRotHeads = 8;
-constexpr long long kRotTeams = 1 << 16;
+// Heads that a team goes through at most, and the waves that have to be left: the
+// lanes' weights, sines and cosines are made once for them.
+constexpr int kRotHeads = 16;
+constexpr long long kRotWaves = 8192;
 
 template <class E, int V, bool HALF, int CNT>
 hipError_t launch_rot_of(RotCall c, hipStream_t st) {
   const int items = c.rotary / 2 / V + (c.P - c.rotary) / V;
   c.team = 1;
   while (c.team < items && c.team < 64) c.team *= 2;
-  const long long lanes = (long long)c.rows * c.heads * c.team;
-  const int each = lanes / 64 > kRotTeams ? kRotHeads : 1;
-  c.teams = (c.heads + each - 1) / each;
+  const long long waves = (long long)c.rows * (c.q_heads + c.k_heads) * c.team / 64;
+  const int each = waves < 2 * kRotWaves ? 1 : waves >= kRotHeads * kRotWaves ? kRotHeads : (int)(waves / kRotWaves);
+  c.q_teams = (c.q_heads + each - 1) / each;
+  c.teams = c.q_teams + (c.k_heads + each - 1) / each;
   const long long per = 256 / c.team, groups = ((long long)c.rows * c.teams + per - 1) / per;
   const long long x = groups < (1 << 20) ? groups : 1 << 20;
   hipLaunchKernelGGL((k_rot<E, V, HALF, CNT>), dim3((unsigned)x, (unsigned)((groups + x - 1) / x)), dim3(256), 0, st, c);
@@ -193,7 +201,7 @@ template <class E, bool HALF>
 hipError_t launch_rot_pairs(const RotCall& c, hipStream_t st) {
   const int half = c.rotary / 2, rest = c.P - c.rotary;
   constexpr int W = 16 / (int)sizeof(E);
-  if (half % W == 0 && rest % W == 0) return launch_rot_of<E, W, HALF, kRotMaxP / W / 64 < 1 ? 1 : kRotMaxP / W / 64>(c, st);
+  if (half % W == 0 && rest % W == 0) return launch_rot_of<E, W, HALF, kRotMaxP / W / 64>(c, st);
   if (half % 2 == 0 && rest % 2 == 0) return launch_rot_of<E, 2, HALF, kRotMaxP / 2 / 64>(c, st);
   if (half + rest <= 64) return launch_rot_of<E, 1, HALF, 1>(c, st);
   return launch_rot_of<E, 1, HALF, kRotMaxP / 64>(c, st);
@@ -334,7 +342,7 @@ int lcsm_rot_apply(lcsm_rot* ctx, int layer, int rows, const lcsm_rot_io* io) {
   if (!rows) return LCSM_OK;
   const size_t at = (size_t)layer * s.P;
   lcsm::RotCall c{};
-  c.rows = rows, c.P = s.P, c.q_heads = s.q_heads, c.heads = s.q_heads + s.k_heads;
+  c.rows = rows, c.P = s.P, c.q_heads = s.q_heads, c.k_heads = s.k_heads;
   c.rotary = s.rotary, c.norm = s.norm, c.eps = s.eps;
   c.q = io->q, c.k = io->k, c.q_out = io->q_out, c.k_out = io->k_out;
   c.q_stride = io->q_stride, c.k_stride = io->k_stride, c.q_out_stride = io->q_out_stride, c.k_out_stride = io->k_out_stride;

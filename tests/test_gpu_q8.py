@@ -67,6 +67,17 @@ def test_large(R, N, K):
         m.check(m.ctx.matmul(0, x), x, dtype)
 
 
+@pytest.mark.parametrize("R,N", [(3500, 3600), (2500, 2600), (1300, 2600), (700, 1500), (90, 2400), (40, 4500)])
+@pytest.mark.parametrize("K", [70, 300])
+def test_every_size_of_pieces(R, N, K):
+    """Pieces of each size, whole ones and such that end inside, with and without a bias, an odd and an even number of stages."""
+    for dtype, bias in (("f16", True), ("f32", False)):
+        say(f"[q8] {R} x {K} -> {N} {dtype}")
+        m = Matrix(N, K, R, bias=bias, seed=R + K)
+        x = m.rows(R, dtype)
+        m.check(m.ctx.matmul(0, x), x, dtype)
+
+
 def test_longest_sums():
     """Every code at its end, over the longest rows: the sums reach 2^31."""
     K = 1 << 17
