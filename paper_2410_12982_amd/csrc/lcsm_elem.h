@@ -54,6 +54,21 @@ __device__ __forceinline__ void fetch_to_lds(__amdgpu_buffer_rsrc_t r, unsigned 
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, (int)lane_at, (int)at, 0, 0);
 }
 
+// All waves past their LDS accesses; transfers and stores of global memory stay on
+// their way, which __syncthreads may wait for.  (The wait is one that the compiler
+// sees, so that it does not wait again, for later reads too.)
+__device__ __forceinline__ void barrier_for_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// At most N memory instructions of this wave on their way, the older ones done.
+template <int N>
+__device__ __forceinline__ void wait_memory_but() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 // The reciprocal is good to an ulp.
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + exp2_hw(-1.44269504f * v)); }

@@ -14,8 +14,10 @@
 // read from there transposed.  The accumulators of one product are an operand
 // of the next as they stand: the order of a product's K slots is free as long as
 // both operands have it, so that keys are taken in the order that makes S an
-// operand of q S, and the scores are made transposed, which makes them one of
-// (q k) v.  Outputs come out as four values of a position a lane.
+// operand of q S.  The scores, which all waves need, are made by all of them, a
+// tile of 16 x 16 positions at a time, and handed on through LDS as operands:
+// made transposed, a lane's accumulators are its share of them.  Outputs come out
+// as four values of a position a lane.
 //
 // Chunks are counted from a sequence's end, so that the one that is not full is
 // its first, and begins with rows of zeros that are nowhere in memory: what the
@@ -70,24 +72,28 @@ __device__ __forceinline__ void lin_mul(const v8bf (&a)[P], const v8bf (&b)[Q], 
       if (sum - i >= 0 && sum - i < Q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[sum - i], c, 0, 0, 0);
 }
 
-// Eight values as an operand's parts: each the bf16 nearest to what the parts
-// before it leave.
-template <int P>
-__device__ __forceinline__ void lin_split(float (&v)[8], v8bf (&to)[P]) {
+// Values as parts: each the bf16 nearest to what the parts before it leave.
+template <int P, int N>
+__device__ __forceinline__ void lin_parts(float (&v)[N], unsigned (&to)[P][N / 2]) {
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    v4u w;
+  for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 2; ++k) {
       const v2bf two = {(bf16_t)v[2 * k], (bf16_t)v[2 * k + 1]};
-      w[k] = __builtin_bit_cast(unsigned, two);
+      to[p][k] = __builtin_bit_cast(unsigned, two);
       if (p + 1 < P) {
-        v[2 * k] -= __builtin_bit_cast(float, w[k] << 16);
-        v[2 * k + 1] -= __builtin_bit_cast(float, w[k] & 0xffff0000u);
+        v[2 * k] -= __builtin_bit_cast(float, to[p][k] << 16);
+        v[2 * k + 1] -= __builtin_bit_cast(float, to[p][k] & 0xffff0000u);
       }
     }
-    to[p] = __builtin_bit_cast(v8bf, w);
-  }
+}
+// Eight values as an operand's.
+template <int P>
+__device__ __forceinline__ void lin_split(float (&v)[8], v8bf (&to)[P]) {
+  unsigned w[P][4];
+  lin_parts(v, w);
+#pragma unroll
+  for (int p = 0; p < P; ++p) to[p] = __builtin_bit_cast(v8bf, (v4u){w[p][0], w[p][1], w[p][2], w[p][3]});
 }
 
 // Rows of bf16 in LDS, `chunks` (a power of two) of eight values a row, placed so
@@ -204,10 +210,11 @@ __device__ __forceinline__ void lin_stage(char* lds, const E* from, size_t strid
     const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     constexpr int STEP = THREADS / CHUNKS;  // rows a turn: a multiple of 8, so that a lane has one chunk of all its rows
     static_assert(C % STEP == 0 && STEP % 8 == 0, "whole turns");
-    const int row = (int)threadIdx.x / CHUNKS, chunk = lin_at(row, (int)threadIdx.x % CHUNKS, CHUNKS) / 16 - row * CHUNKS;
+    const int tid = (int)lin_here(threadIdx.x);
+    const int row = tid / CHUNKS, chunk = lin_at(row, tid % CHUNKS, CHUNKS) / 16 - row * CHUNKS;
     // (rows before the first wrap around to past the buffer's end)
     const unsigned each = (unsigned)stride * 2u;
-    const unsigned at = lin_here((unsigned)(row - pad) * each + 16u * (unsigned)chunk);
+    const unsigned at = (unsigned)(row - pad) * each + 16u * (unsigned)chunk;
 #pragma unroll
     for (int i = 0; i < C / STEP; ++i)
       fetch_to_lds(r, 8 * chunk < width ? at + (unsigned)(i * STEP) * each : kLinNowhere, 0, lds + (i * THREADS + 64 * wv) * 16);
@@ -252,6 +259,18 @@ __device__ __forceinline__ void lin_store(__amdgpu_buffer_rsrc_t r, unsigned row
   }
 }
 
+// What a workgroup has in LDS: keys (DIRECT: this chunk's and the next one's),
+// values (the same where there are no outputs), queries, and the scores of the
+// tiles of 16 x 32 positions that are not above the diagonal.
+template <class E, int KT, bool OUT, bool DIRECT>
+struct LinLds {
+  static constexpr int C = lin_chunk<E>(KT), IN = LinParts<E>::IN;
+  static constexpr int KEYS = IN * C * KT * 64, VALUES = IN * C * kLinWaves * 64;
+  static constexpr int V = (DIRECT ? 2 : 1) * KEYS, Q = V + (DIRECT && !OUT ? 2 : 1) * VALUES;
+  static constexpr int FRAGS = C == 64 ? 6 : 2, P = Q + (OUT ? KEYS : 0);
+  static constexpr int BYTES = P + (OUT ? LinParts<E>::MID * FRAGS * 1024 : 0);
+};
+
 // One segment (w.per chunks) of a sequence: OUT, with its outputs and from the
 // state before it; else its own contribution to the state after it.
 template <class E, int KT, bool OUT, bool DIRECT>
@@ -260,8 +279,9 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   constexpr int IN = LinParts<E>::IN, MID = LinParts<E>::MID;
   constexpr int KC = 4 * KT, VC = 4 * kLinWaves;  // chunks of eight a row
   constexpr int KPART = C * KC * 16, VPART = C * VC * 16;
-  extern __shared__ __align__(16) char lds[];  // keys, values, queries
-  char *const lk = lds, *const lv = lk + IN * KPART, *const lq = lv + IN * VPART;
+  typedef LinLds<E, KT, OUT, DIRECT> Lds;
+  extern __shared__ __align__(16) char lds[];
+  char *const lv = lds + Lds::V, *const lq = lds + Lds::Q, *const lp = lds + Lds::P;
   const int lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int vblocks = (c.V + 32 * kLinWaves - 1) / (32 * kLinWaves);
@@ -289,9 +309,9 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   for (int m = 0; m < TT; ++m) tile[m] = power(16 * m);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    near[i] = power(l - 4 * q - i);       // in a tile (where it is not negative)
-    far[i] = power(16 + l - 4 * q - i);   // from the tile before
-    back[i] = power(15 - 4 * q - i);      // to the end of the tile
+    near[i] = c.scale * power(l - 4 * q - i);      // in a tile (where it is not negative)
+    far[i] = c.scale * power(16 + l - 4 * q - i);  // from the tile before
+    back[i] = power(15 - 4 * q - i);               // to the end of the tile
   }
 
   // the state: S[a][e][i] is key 32 (a / 2) + 8 q + 4 (a % 2) + i, value vc + 16 e + l
@@ -328,83 +348,118 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 
   LinDecay whole(decay * C);
   const unsigned out_row = (unsigned)c.y_stride * (unsigned)sizeof(E);
+  // rows of chunk k, counted from the sequence's end
+  int r0 = 0, pad = 0;
+  auto locate = [&](int k) {
+    const int end = t1 - (chunks - 1 - k) * C;
+    r0 = max(end - C, t0);
+    pad = C - (end - r0);
+  };
+  auto stage_keys = [&](int k) {
+    locate(k);
+    lin_stage<E, C, KC, DIRECT>(lds + (DIRECT ? k % 2 * Lds::KEYS : 0), static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride +
+                                (size_t)g * c.K, c.k_stride, pad, c.K);
+  };
+  auto stage_values = [&](int k) {
+    locate(k);
+    lin_stage<E, C, VC, DIRECT>(lv + (DIRECT && !OUT ? k % 2 * Lds::VALUES : 0), static_cast<const E*>(c.v) +
+                                (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride, pad, c.V - v0);
+  };
+  auto stage_queries = [&](int k, int h) {
+    locate(k);
+    lin_stage<E, C, KC, DIRECT>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
+                                c.q_stride, pad, c.K);
+  };
+  // (the compiler does not wait for transfers straight into LDS)
+  auto arrived = [&]() {
+    if (DIRECT) wait_memory_but<0>();
+    barrier_for_lds();
+  };
+  if (OUT) {  // halves of scores above the diagonal stay zero
+    for (int i = (int)threadIdx.x; i < MID * Lds::FRAGS * 64; i += 64 * kLinWaves)
+      reinterpret_cast<v4u*>(lp)[i] = v4u{0, 0, 0, 0};
+  }
+  if (DIRECT && k0 < k1) {
+    stage_keys(k0);
+    stage_values(k0);
+    if (OUT) stage_queries(k0, 0);
+  }
   for (int k = k0; k < k1; ++k) {
-    const int end = t1 - (chunks - 1 - k) * C, r0 = max(end - C, t0), pad = C - (end - r0);
-    __syncthreads();  // the chunk before has been read
-    lin_stage<E, C, KC, DIRECT>(lk, static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride + (size_t)g * c.K, c.k_stride, pad,
-                                c.K);
-    lin_stage<E, C, VC, DIRECT>(lv, static_cast<const E*>(c.v) + (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride,
-                                pad, c.V - v0);
-    auto stage_queries = [&](int h) {
-      lin_stage<E, C, KC, DIRECT>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
-                                  c.q_stride, pad, c.K);
-    };
-    // (the compiler does not wait for transfers straight into LDS)
-    auto arrived = [&]() {
-      if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-    };
-    if (OUT) stage_queries(0);
+    const char* lk = lds + (DIRECT ? k % 2 * Lds::KEYS : 0);
+    const char* values = lv + (DIRECT && !OUT ? k % 2 * Lds::VALUES : 0);
+    if (!DIRECT) {
+      barrier_for_lds();  // the chunk before has been read
+      stage_keys(k);
+      stage_values(k);
+      if (OUT) stage_queries(k, 0);
+    }
     arrived();
+    // DIRECT: the next chunk's keys (and values) go where those before these were,
+    // which all waves have passed
+    if (DIRECT && k + 1 < k1) {
+      stage_keys(k + 1);
+      if (!OUT) stage_values(k + 1);
+    }
+    locate(k);
     // values as an operand: 32 positions a block, slots 4 q ..+3 and 16 + 4 q ..+3
     v8bf vf[PB][2][IN];
-    auto read_values = [&]() {
 #pragma unroll
-      for (int b = 0; b < PB; ++b)
+    for (int b = 0; b < PB; ++b)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int p = 0; p < IN; ++p) {
-            const int at = value_at[e] + p * VPART + 32 * b * VC * 16;
-            vf[b][e][p] = lin_join(lin_read_turned(lv, at), lin_read_turned(lv, at + 16 * VC * 16));
-          }
-    };
-    read_values();
+        for (int p = 0; p < IN; ++p) {
+          const int at = value_at[e] + p * VPART + 32 * b * VC * 16;
+          vf[b][e][p] = lin_join(lin_read_turned(values, at), lin_read_turned(values, at + 16 * VC * 16));
+        }
     if constexpr (OUT) {
-      // values that are not finite: the products of the scores are made without
-      // them, `bad` is the first such position of this lane's value
-      int bad[2] = {C, C};
-      bool odd = false;
+      // a value that is not finite: the first such position of this lane's value is `bad`
+      typedef unsigned short v2h __attribute__((ext_vector_type(2)));
+      v2h most = {0, 0};
 #pragma unroll
       for (int b = 0; b < PB; ++b)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const v4u w0 = __builtin_bit_cast(v4u, vf[b][e][0]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            odd |= (w0[j] & 0x7f80u) == 0x7f80u || (w0[j] & 0x7f800000u) == 0x7f800000u;
+          for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(v2h, w0[j] & 0x7fff7fffu));
         }
-      const bool any = __ballot(odd) != 0;
-      if (any) {
-#pragma unroll
-        for (int b = 0; b < PB; ++b)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            v4u part[IN];
-#pragma unroll
-            for (int p = 0; p < IN; ++p) part[p] = __builtin_bit_cast(v4u, vf[b][e][p]);
-#pragma unroll
-            for (int j = 7; j >= 0; --j) {
-              const unsigned half = j & 1 ? 0xffff0000u : 0xffffu, top = half & 0x7f807f80u;
-              if ((part[0][j / 2] & top) != top) continue;
-#pragma unroll
-              for (int p = 0; p < IN; ++p) part[p][j / 2] &= ~half;
-              bad[e] = min(bad[e], 32 * b + (j < 4 ? 4 * q + j : 12 + 4 * q + j));
-            }
-#pragma unroll
-            for (int p = 0; p < IN; ++p) vf[b][e][p] = __builtin_bit_cast(v8bf, part[p]);
-          }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          bad[e] = min(bad[e], __shfl_xor(bad[e], 16));
-          bad[e] = min(bad[e], __shfl_xor(bad[e], 32));
-        }
-      }
+      const bool any = __ballot(most[0] >= 0x7f80 || most[1] >= 0x7f80) != 0;
       for (int h = 0; h < heads; ++h) {
         if (h > 0) {
-          __syncthreads();
-          stage_queries(h);
+          if (!DIRECT) {
+            barrier_for_lds();
+            stage_queries(k, h);
+          }
           arrived();
+        }
+        // scores, transposed: positions 16 jt + 4 q + i of the keys for 16 tt + l
+#pragma unroll 1
+        for (int n = wv; n < TT * (TT + 1) / 2; n += kLinWaves) {
+          const int tt = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3, jt = n - tt * (tt + 1) / 2, apart = tt - jt;
+          v4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kb = 0; kb < KT; ++kb) {
+            v8bf qf[IN], kf[IN];
+#pragma unroll
+            for (int p = 0; p < IN; ++p) {
+              qf[p] = lin_read(lq, p * KPART + plain(16 * tt, kb, KC));
+              kf[p] = lin_read(lk, p * KPART + plain(16 * jt, kb, KC));
+            }
+            lin_mul<MID - 1>(kf, qf, s);
+          }
+          const float between = apart < 2 ? 1.f : apart == 2 ? tile[1] : tile[TT - 2];
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] = apart ? s[i] * far[i] * between : l >= 4 * q + i ? s[i] * near[i] : 0.f;
+          unsigned parts[MID][2];
+          lin_parts(v, parts);
+          typedef unsigned v2u __attribute__((ext_vector_type(2)));
+          const int at = (tt < 2 ? tt : 2 * tt - 2 + jt / 2) * 1024 + lane * 16 + jt % 2 * 8;
+#pragma unroll
+          for (int p = 0; p < MID; ++p)
+            *reinterpret_cast<v2u*>(lp + p * Lds::FRAGS * 1024 + at) = v2u{parts[p][0], parts[p][1]};
         }
         // y[tt][e]: values 16 e + 4 q + i of position 16 tt + l
         v4f y[TT][2];
@@ -437,79 +492,101 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
         }
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt) {
-          __builtin_amdgcn_sched_barrier(0);
-          const float f = power(16 * tt + l + 1 - pad);
-          // queries and keys are read again for every tile of positions: kept, they
-          // would take more registers than there are
-          const int again = KT >= 4 ? (int)lin_here(0u) : 0;
+          const float f = c.scale * power((int)lin_here((unsigned)(16 * tt + l + 1 - pad)));
 #pragma unroll
           for (int e = 0; e < 2; ++e) y[tt][e] *= f;
-          v8bf qf[KT][IN];
-#pragma unroll
-          for (int kb = 0; kb < KT; ++kb)
-#pragma unroll
-            for (int p = 0; p < IN; ++p) qf[kb][p] = lin_read(lq, again + p * KPART + plain(16 * tt, kb, KC));
-          // scores, transposed: positions 16 jt + 4 q + i of the keys for 16 tt + l
-#pragma unroll
-          for (int b = 0; b <= tt / 2; ++b) {
-            float v[8];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const int jt = 2 * b + half;
-              __builtin_amdgcn_sched_barrier(0);
-              v4f s = {0.f, 0.f, 0.f, 0.f};
-              if (jt <= tt) {
-#pragma unroll
-                for (int kb = 0; kb < KT; ++kb) {
-                  v8bf kf[IN];
-#pragma unroll
-                  for (int p = 0; p < IN; ++p) kf[p] = lin_read(lk, again + p * KPART + plain(16 * jt, kb, KC));
-                  lin_mul<MID - 1>(kf, qf[kb], s);
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (jt < tt)
-                  v[4 * half + i] = s[i] * far[i] * tile[tt - jt - 1];
-                else
-                  v[4 * half + i] = jt == tt && l >= 4 * q + i ? s[i] * near[i] : 0.f;
-              }
-            }
-            v8bf pf[MID];
-            lin_split(v, pf);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(vf[b][e], pf, y[tt][e]);
-          }
         }
-        if (any) {
+        barrier_for_lds();  // the scores are there; queries and values have been read
+        if (DIRECT) {
+          if (h + 1 < heads)
+            stage_queries(k, h + 1);
+          else if (k + 1 < k1)
+            stage_queries(k + 1, 0);
+          if (h == 0 && k + 1 < k1) stage_values(k + 1);
+          locate(k);
+        }
+        auto scores_times = [&](const v8bf (&x)[2][IN], int b) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
+          for (int tt = 2 * b; tt < TT; ++tt) {
+            __builtin_amdgcn_sched_barrier(0);
+            v8bf pf[MID];
+#pragma unroll
+            for (int p = 0; p < MID; ++p)
+              pf[p] = *reinterpret_cast<const v8bf*>(lp + (p * Lds::FRAGS + (tt < 2 ? tt : 2 * tt - 2 + b)) * 1024 + lane * 16);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(x[e], pf, y[tt][e]);
+          }
+        };
+        if (!any) {
+#pragma unroll
+          for (int b = 0; b < PB; ++b) scores_times(vf[b], b);
+        } else {
+          // without the values that are not finite, and from the first of them on NaN
+          unsigned bad[2] = {0, 0};  // slots 8 b + 0 ..+7 that have such a value
+#pragma unroll
+          for (int b = 0; b < PB; ++b) {
+            v8bf fine[2][IN];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              v4u part[IN];
+#pragma unroll
+              for (int p = 0; p < IN; ++p) {
+                part[p] = __builtin_bit_cast(v4u, vf[b][e][p]);
+                asm volatile("" : "+v"(part[p]));  // (made here, not before the loop over the heads)
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                // of each half one where it is finite, and so the half's mask
+                const v2h one = __builtin_elementwise_min(__builtin_bit_cast(v2h, (part[0][j] & 0x7f807f80u) ^ 0x7f807f80u), (v2h){1, 1});
+                const unsigned mask = __builtin_bit_cast(unsigned, (v2h){0, 0} - one), none = ~mask;
+                bad[e] |= ((none & 1) | (none >> 30 & 2)) << (8 * b + 2 * j);
+#pragma unroll
+                for (int p = 0; p < IN; ++p) part[p][j] &= mask;
+              }
+#pragma unroll
+              for (int p = 0; p < IN; ++p) fine[e][p] = __builtin_bit_cast(v8bf, part[p]);
+            }
+            scores_times(fine, b);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int slot = __ffs(bad[e]) - 1;
+            int at = slot < 0 ? C : slot / 8 * 32 + 4 * q + slot % 8 + (slot % 8 < 4 ? 0 : 12);
+            at = min(at, __shfl_xor(at, 16));
+            at = min(at, __shfl_xor(at, 32));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int first = __shfl(bad[e], 4 * q + i);
+              const int first = __shfl(at, 4 * q + i);
 #pragma unroll
               for (int tt = 0; tt < TT; ++tt)
                 if (16 * tt + l >= first) y[tt][e][i] = __builtin_nanf("");
             }
+          }
         }
         const auto r = row_buffer<E>(static_cast<E*>(c.y) + ((size_t)g * heads + h) * c.V, (size_t)r0, c.y_stride, C - pad, c.V);
         const unsigned to = lin_here((unsigned)(l - pad) * out_row);
+        const int column = (int)lin_here((unsigned)(vc + 4 * q));
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            lin_store<E>(r, to + 16 * tt * out_row, vc + 16 * e + 4 * q, c.V, c.scale * y[tt][e], w.quads);
+          for (int e = 0; e < 2; ++e) lin_store<E>(r, to + 16 * tt * out_row, column + 16 * e, c.V, y[tt][e], w.quads);
       }
-      if (any) read_values();
     }
     // the state after the chunk
     const LinDecay d = pad == 0 ? whole : LinDecay(decay * (C - pad));
+    if (d.keep != 0.f) {
 #pragma unroll
-    for (int a = 0; a < 2 * KT; ++a)
+      for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[a][e][i] = d(S[a][e][i]);
+          for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], d.by, S[a][e][i]);
+    } else {
+#pragma unroll
+      for (int a = 0; a < 2 * KT; ++a)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) S[a][e] *= d.by;
+    }
 #pragma unroll
     for (int b = 0; b < PB; ++b) {
       v8bf xf[2][3];
@@ -604,13 +681,14 @@ __global__ __launch_bounds__(256) void k_lin_join(LinCall c, LinCut w) {
 
 template <class E, int KT>
 hipError_t lin_prompt_kt(const LinCall& c, const LinCut& w, hipStream_t st) {
-  constexpr int C = lin_chunk<E>(KT), IN = LinParts<E>::IN, KPART = C * KT * 64, VPART = C * kLinWaves * 64;
-  constexpr int lds_sum = IN * (KPART + VPART), lds_out = lds_sum + IN * KPART;
+  constexpr bool CAN = LinParts<E>::IN == 1;
+  const bool direct = CAN && w.direct;
+  const int lds_out = direct ? LinLds<E, KT, true, CAN>::BYTES : LinLds<E, KT, true, false>::BYTES;
+  const int lds_sum = direct ? LinLds<E, KT, false, CAN>::BYTES : LinLds<E, KT, false, false>::BYTES;
   const unsigned vblocks = (unsigned)((c.V + 32 * kLinWaves - 1) / (32 * kLinWaves));
   const dim3 grid((unsigned)c.G * vblocks, (unsigned)w.segments), threads(64 * kLinWaves);
-  constexpr bool DIRECT = IN == 1;
-  auto out = DIRECT && w.direct ? k_lin_chunks<E, KT, true, DIRECT> : k_lin_chunks<E, KT, true, false>;
-  auto sum = DIRECT && w.direct ? k_lin_chunks<E, KT, false, DIRECT> : k_lin_chunks<E, KT, false, false>;
+  auto out = direct ? k_lin_chunks<E, KT, true, CAN> : k_lin_chunks<E, KT, true, false>;
+  auto sum = direct ? k_lin_chunks<E, KT, false, CAN> : k_lin_chunks<E, KT, false, false>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(out), hipFuncAttributeMaxDynamicSharedMemorySize, lds_out);
   if (e == hipSuccess && w.segments > c.n) {
     e = hipFuncSetAttribute(reinterpret_cast<const void*>(sum), hipFuncAttributeMaxDynamicSharedMemorySize, lds_sum);

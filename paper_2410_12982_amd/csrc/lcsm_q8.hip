@@ -440,21 +440,6 @@ hipError_t launch_few(const Q8Call& c, int waves, hipStream_t st) {
 // from one piece to the next, whose first stages arrive while the last piece's
 // outputs are made and stored.
 
-// All waves past their LDS reads; transfers stay on their way, which __syncthreads
-// would wait for.  (The wait is one that the compiler sees, so that it does not
-// wait again, for later reads too.)
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-// At most N memory instructions of this wave on their way, the oldest done.
-template <int N>
-__device__ __forceinline__ void wait_but() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
 template <class E, int WN, int WX, int NT, int RT, int KT, int STAGES>
 __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
   constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // rows of tiles that a wave fetches
@@ -529,10 +514,10 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
     // this wave's transfers of stage g + 1 have arrived, those of the stages after it
     // may be on their way; then all waves' have, and stage g has been read
     if (g + STAGES > turns)
-      wait_but<0>();
+      wait_memory_but<0>();
     else
-      wait_but<(STAGES - 2) * EACH * KT>();
-    lds_barrier();
+      wait_memory_but<(STAGES - 2) * EACH * KT>();
+    barrier_for_lds();
     read(next);  // (after the last stage: what is not used)
     if (g + STAGES < turns) fetch();
 #pragma unroll
@@ -548,10 +533,10 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
   for (int g = 0; g < STAGES; ++g)
     if (g < turns) fetch();
   if (turns >= STAGES)
-    wait_but<(STAGES - 1) * EACH * KT>();
+    wait_memory_but<(STAGES - 1) * EACH * KT>();
   else
-    wait_but<0>();
-  lds_barrier();
+    wait_memory_but<0>();
+  barrier_for_lds();
   Operands even, odd;
   read(even);
   for (int id = mine, g = 0; id < end; id += step) {
@@ -644,7 +629,7 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
     }
     // (stores count among the transfers that the turns wait for; to count them in
     // there, and leave them on their way, takes the same time)
-    wait_but<0>();
+    wait_memory_but<0>();
   }
 }
 
