@@ -45,6 +45,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
 typedef bf16_t v2bf __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
 template <class E>
@@ -79,7 +80,8 @@ __device__ __forceinline__ void lin_parts(float (&v)[N], unsigned (&to)[P][N / 2
   for (int p = 0; p < P; ++p)
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) {
-      const v2bf two = {(bf16_t)v[2 * k], (bf16_t)v[2 * k + 1]};
+      // (one conversion of two: as two conversions they are three instructions)
+      const v2bf two = __builtin_convertvector((v2f){v[2 * k], v[2 * k + 1]}, v2bf);
       to[p][k] = __builtin_bit_cast(unsigned, two);
       if (p + 1 < P) {
         v[2 * k] -= __builtin_bit_cast(float, to[p][k] << 16);
@@ -170,65 +172,86 @@ __device__ __forceinline__ bool lin_piece(const LinCall& c, int want, int per, i
   return false;
 }
 
-// Eight elements from p, zeros from `have` on, as parts; wide accesses of global
-// memory may begin at any element.
-template <class E, int P>
-__device__ __forceinline__ void lin_load(const E* p, int have, v8bf (&to)[P]) {
-  struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+// What a thread loads of a chunk's rows, eight elements at a time: all loads are on
+// their way before the first is used.
+template <class E, int C, int CHUNKS>
+struct LinRaw {
+  static constexpr int P = LinParts<E>::IN, THREADS = 64 * kLinWaves, N = (C * CHUNKS + THREADS - 1) / THREADS;
+  struct Eight {
     E e[8];
-  };
-  struct Whole {
-    E e[8];
-  };
-  Whole w;
-  if (have >= 8) {
-    const Pack k = *reinterpret_cast<const Pack*>(p);
+  } v[N];
+  // Rows of `from` after `pad` rows of zeros, `width` values of each; wide accesses
+  // of global memory may begin at any element.
+  __device__ __forceinline__ void load(const E* from, size_t stride, int pad, int width) {
+    struct __attribute__((packed, aligned(sizeof(E)))) Pack {
+      E e[8];
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.e[i] = k.e[i];
-  } else {
+    for (int n = 0; n < N; ++n) {
+      const int at = n * THREADS + (int)threadIdx.x, row = at / CHUNKS, chunk = at % CHUNKS;
+      const int have = row >= pad && row < C ? width - 8 * chunk : 0;
+      const E* p = from + (size_t)max(row - pad, 0) * stride + 8 * chunk;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.e[i] = i < have ? p[i] : (E)0.f;
-  }
-  if constexpr (P == 1) {
-    to[0] = __builtin_bit_cast(v8bf, w);
-  } else {
-    float v[8];
+      for (int i = 0; i < 8; ++i) v[n].e[i] = (E)0.f;
+      if (have >= 8) {
+        const Pack k = *reinterpret_cast<const Pack*>(p);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)w.e[i];
-    lin_split(v, to);
-  }
-}
-
-// A chunk's rows into LDS, `width` values of each (zeros past them): `pad` rows of
-// zeros, then those of `from`.  DIRECT: straight from memory (bf16 rows of whole
-// and aligned eights); the caller waits for them.
-template <class E, int C, int CHUNKS, bool DIRECT>
-__device__ __forceinline__ void lin_stage(char* lds, const E* from, size_t stride, int pad, int width) {
-  constexpr int P = LinParts<E>::IN, THREADS = 64 * kLinWaves;
-  if constexpr (DIRECT) {
-    const auto r = row_buffer<E>(from, 0, stride, C - pad, width);
-    const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    constexpr int STEP = THREADS / CHUNKS;  // rows a turn: a multiple of 8, so that a lane has one chunk of all its rows
-    static_assert(C % STEP == 0 && STEP % 8 == 0, "whole turns");
-    const int tid = (int)lin_here(threadIdx.x);
-    const int row = tid / CHUNKS, chunk = lin_at(row, tid % CHUNKS, CHUNKS) / 16 - row * CHUNKS;
-    // (rows before the first wrap around to past the buffer's end)
-    const unsigned each = (unsigned)stride * 2u;
-    const unsigned at = (unsigned)(row - pad) * each + 16u * (unsigned)chunk;
+        for (int i = 0; i < 8; ++i) v[n].e[i] = k.e[i];
+      } else if (have > 0) {
 #pragma unroll
-    for (int i = 0; i < C / STEP; ++i)
-      fetch_to_lds(r, 8 * chunk < width ? at + (unsigned)(i * STEP) * each : kLinNowhere, 0, lds + (i * THREADS + 64 * wv) * 16);
-  } else {
-#pragma unroll 2
-    for (int i = 0; i < C * CHUNKS; i += THREADS) {
-      const int at = i + (int)threadIdx.x, row = at / CHUNKS, chunk = at % CHUNKS;
-      if (at >= C * CHUNKS) break;
-      v8bf v[P];
-      lin_load<E, P>(from + (size_t)max(row - pad, 0) * stride + 8 * chunk, row >= pad ? width - 8 * chunk : 0, v);
-#pragma unroll
-      for (int p = 0; p < P; ++p) *reinterpret_cast<v8bf*>(lds + p * C * CHUNKS * 16 + lin_at(row, chunk, CHUNKS)) = v[p];
+        for (int i = 0; i < 8; ++i)
+          if (i < have) v[n].e[i] = p[i];
+      }
     }
   }
+  // As parts into LDS.
+  __device__ __forceinline__ void put(char* lds) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = n * THREADS + (int)threadIdx.x, row = at / CHUNKS, chunk = at % CHUNKS;
+      if (at >= C * CHUNKS) break;
+      v8bf w[P];
+      if constexpr (P == 1) {
+        w[0] = __builtin_bit_cast(v8bf, v[n]);
+      } else {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)v[n].e[i];
+        lin_split(f, w);
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) *reinterpret_cast<v8bf*>(lds + p * C * CHUNKS * 16 + lin_at(row, chunk, CHUNKS)) = w[p];
+    }
+  }
+};
+
+// What a lane fetches of a chunk's rows: 16 bytes of every STEP'th row.
+template <int CHUNKS>
+struct LinLane {
+  static constexpr int STEP = 64 * kLinWaves / CHUNKS;
+  static_assert(STEP % 8 == 0, "a lane has one chunk of all its rows");
+  unsigned at;  // of the first row
+  bool have;
+  __device__ LinLane(size_t stride, int width) {
+    const int row = (int)threadIdx.x / CHUNKS, chunk = lin_at(row, (int)threadIdx.x % CHUNKS, CHUNKS) / 16 - row * CHUNKS;
+    at = (unsigned)row * (unsigned)stride * 2u + 16u * (unsigned)chunk;
+    have = 8 * chunk < width;
+  }
+};
+
+// A chunk's rows straight from memory into LDS (bf16 rows of whole and aligned
+// eights): `pad` rows of zeros, then those of `from`, `width` values of each and
+// zeros past them.  The caller waits for them.
+template <class E, int C, int CHUNKS>
+__device__ __forceinline__ void lin_fetch(char* lds, const LinLane<CHUNKS>& lane, const E* from, size_t stride, int pad, int width) {
+  constexpr int THREADS = 64 * kLinWaves, STEP = LinLane<CHUNKS>::STEP;
+  const auto r = row_buffer<E>(from, 0, stride, C - pad, width);
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // (rows before the first wrap around to past the buffer's end)
+  const unsigned each = (unsigned)stride * 2u;
+#pragma unroll
+  for (int i = 0; i < C / STEP; ++i)
+    fetch_to_lds(r, lane.have ? lane.at + (unsigned)(i * STEP - pad) * each : kLinNowhere, 0, lds + (i * THREADS + 64 * wv) * 16);
 }
 
 // Four outputs from column `at` of `width` on, of the row that begins at `row` of
@@ -348,6 +371,8 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 
   LinDecay whole(decay * C);
   const unsigned out_row = (unsigned)c.y_stride * (unsigned)sizeof(E);
+  const LinLane<KC> keys_lane(c.k_stride, c.K), queries_lane(c.q_stride, c.K);
+  const LinLane<VC> values_lane(c.v_stride, c.V - v0);
   // rows of chunk k, counted from the sequence's end
   int r0 = 0, pad = 0;
   auto locate = [&](int k) {
@@ -355,20 +380,20 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
     r0 = max(end - C, t0);
     pad = C - (end - r0);
   };
-  auto stage_keys = [&](int k) {
+  auto keys_of = [&]() { return static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride + (size_t)g * c.K; };
+  auto values_of = [&]() { return static_cast<const E*>(c.v) + (size_t)r0 * c.v_stride + (size_t)g * c.V + v0; };
+  auto queries_of = [&](int h) { return static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K; };
+  auto fetch_keys = [&](int k) {
     locate(k);
-    lin_stage<E, C, KC, DIRECT>(lds + (DIRECT ? k % 2 * Lds::KEYS : 0), static_cast<const E*>(c.k) + (size_t)r0 * c.k_stride +
-                                (size_t)g * c.K, c.k_stride, pad, c.K);
+    if constexpr (DIRECT) lin_fetch<E, C, KC>(lds + k % 2 * Lds::KEYS, keys_lane, keys_of(), c.k_stride, pad, c.K);
   };
-  auto stage_values = [&](int k) {
+  auto fetch_values = [&](int k) {
     locate(k);
-    lin_stage<E, C, VC, DIRECT>(lv + (DIRECT && !OUT ? k % 2 * Lds::VALUES : 0), static_cast<const E*>(c.v) +
-                                (size_t)r0 * c.v_stride + (size_t)g * c.V + v0, c.v_stride, pad, c.V - v0);
+    if constexpr (DIRECT) lin_fetch<E, C, VC>(lv + (OUT ? 0 : k % 2 * Lds::VALUES), values_lane, values_of(), c.v_stride, pad, c.V - v0);
   };
-  auto stage_queries = [&](int k, int h) {
+  auto fetch_queries = [&](int k, int h) {
     locate(k);
-    lin_stage<E, C, KC, DIRECT>(lq, static_cast<const E*>(c.q) + (size_t)r0 * c.q_stride + ((size_t)g * heads + h) * c.K,
-                                c.q_stride, pad, c.K);
+    if constexpr (DIRECT) lin_fetch<E, C, KC>(lq, queries_lane, queries_of(h), c.q_stride, pad, c.K);
   };
   // (the compiler does not wait for transfers straight into LDS)
   auto arrived = [&]() {
@@ -380,25 +405,31 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
       reinterpret_cast<v4u*>(lp)[i] = v4u{0, 0, 0, 0};
   }
   if (DIRECT && k0 < k1) {
-    stage_keys(k0);
-    stage_values(k0);
-    if (OUT) stage_queries(k0, 0);
+    fetch_keys(k0);
+    fetch_values(k0);
+    if (OUT) fetch_queries(k0, 0);
   }
   for (int k = k0; k < k1; ++k) {
     const char* lk = lds + (DIRECT ? k % 2 * Lds::KEYS : 0);
     const char* values = lv + (DIRECT && !OUT ? k % 2 * Lds::VALUES : 0);
-    if (!DIRECT) {
+    if constexpr (!DIRECT) {
+      locate(k);
+      LinRaw<E, C, KC> rk, rq;
+      LinRaw<E, C, VC> rv;
+      rk.load(keys_of(), c.k_stride, pad, c.K);
+      rv.load(values_of(), c.v_stride, pad, c.V - v0);
+      if (OUT) rq.load(queries_of(0), c.q_stride, pad, c.K);
       barrier_for_lds();  // the chunk before has been read
-      stage_keys(k);
-      stage_values(k);
-      if (OUT) stage_queries(k, 0);
+      rk.put(lds);
+      rv.put(lv);
+      if (OUT) rq.put(lq);
     }
     arrived();
     // DIRECT: the next chunk's keys (and values) go where those before these were,
     // which all waves have passed
     if (DIRECT && k + 1 < k1) {
-      stage_keys(k + 1);
-      if (!OUT) stage_values(k + 1);
+      fetch_keys(k + 1);
+      if (!OUT) fetch_values(k + 1);
     }
     locate(k);
     // values as an operand: 32 positions a block, slots 4 q ..+3 and 16 + 4 q ..+3
@@ -427,9 +458,11 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
       const bool any = __ballot(most[0] >= 0x7f80 || most[1] >= 0x7f80) != 0;
       for (int h = 0; h < heads; ++h) {
         if (h > 0) {
-          if (!DIRECT) {
+          if constexpr (!DIRECT) {
+            LinRaw<E, C, KC> rq;
+            rq.load(queries_of(h), c.q_stride, pad, c.K);
             barrier_for_lds();
-            stage_queries(k, h);
+            rq.put(lq);
           }
           arrived();
         }
@@ -499,10 +532,10 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
         barrier_for_lds();  // the scores are there; queries and values have been read
         if (DIRECT) {
           if (h + 1 < heads)
-            stage_queries(k, h + 1);
+            fetch_queries(k, h + 1);
           else if (k + 1 < k1)
-            stage_queries(k + 1, 0);
-          if (h == 0 && k + 1 < k1) stage_values(k + 1);
+            fetch_queries(k + 1, 0);
+          if (h == 0 && k + 1 < k1) fetch_values(k + 1);
           locate(k);
         }
         auto scores_times = [&](const v8bf (&x)[2][IN], int b) {
