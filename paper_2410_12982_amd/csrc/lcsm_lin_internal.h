@@ -55,13 +55,9 @@ struct LinDecay {
   __device__ float operator()(float s) const { return fmaf(s, by, keep != 0.f ? s : 0.f); }
 };
 
-// Positions of a chunk.
-template <class E>
-constexpr int lin_chunk(int KT) {
-  return sizeof(E) == 4 ? 32 : KT > 4 ? 32 : 64;
-}
+// Positions of a chunk (the kernels' lin_chunk).
 inline int lin_blocks_of(int K) { return K <= 32 ? 1 : K <= 64 ? 2 : K <= 128 ? 4 : 8; }
-inline int lin_chunk_of(int dtype, int K) { return dtype == LCSM_F32 || K > 128 ? 32 : 64; }
+inline int lin_chunk_of(int dtype, int K) { return dtype == LCSM_BF16 && K <= 128 ? 64 : 32; }
 // Waves of a workgroup, 32 values of a state each.
 constexpr int kLinWaves = 4;
 

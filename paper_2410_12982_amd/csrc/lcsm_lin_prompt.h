@@ -62,15 +62,39 @@ struct LinParts<float> {
   static constexpr int IN = 3, MID = 3;
 };
 
-// c += a b with both in parts: those products whose parts' numbers add up to at
-// most LAST, the small ones first.
+// Positions of a chunk: 64 where keys and values are one bf16 part and the chunk's
+// rows leave room for two workgroups a compute unit, else 32 (fp16, 32 heads of 128
+// x 128 and 16384 tokens: 449 us in chunks of 32, 705 us in those of 64; of 64 x 128,
+// 311 and 317 us).
+template <class E>
+constexpr int lin_chunk(int KT) {
+  return LinParts<E>::IN == 1 && KT <= 4 ? 64 : 32;
+}
+
+// c[e] += a b[e] (or a[e] b), both in parts: those products whose parts' numbers add
+// up to at most LAST, the small ones first.  The two sums take turns: a product
+// that waits for the one before it takes twice as long.
 template <int LAST, int P, int Q>
-__device__ __forceinline__ void lin_mul(const v8bf (&a)[P], const v8bf (&b)[Q], v4f& c) {
+__device__ __forceinline__ void lin_mul(const v8bf (&a)[P], const v8bf (&b)[2][Q], v4f (&c)[2]) {
 #pragma unroll
   for (int sum = LAST; sum >= 0; --sum)
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (sum - i >= 0 && sum - i < Q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[sum - i], c, 0, 0, 0);
+      if (sum - i >= 0 && sum - i < Q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) c[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[e][sum - i], c[e], 0, 0, 0);
+      }
+}
+template <int LAST, int P, int Q>
+__device__ __forceinline__ void lin_mul(const v8bf (&a)[2][P], const v8bf (&b)[Q], v4f (&c)[2]) {
+#pragma unroll
+  for (int sum = LAST; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (sum - i >= 0 && sum - i < Q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) c[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e][i], b[sum - i], c[e], 0, 0, 0);
+      }
 }
 
 // Values as parts: each the bf16 nearest to what the parts before it leave.
@@ -470,7 +494,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll 1
         for (int n = wv; n < TT * (TT + 1) / 2; n += kLinWaves) {
           const int tt = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3, jt = n - tt * (tt + 1) / 2, apart = tt - jt;
-          v4f s = {0.f, 0.f, 0.f, 0.f};
+          v4f two[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
           for (int kb = 0; kb < KT; ++kb) {
             v8bf qf[IN], kf[IN];
@@ -479,8 +503,17 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
               qf[p] = lin_read(lq, p * KPART + plain(16 * tt, kb, KC));
               kf[p] = lin_read(lk, p * KPART + plain(16 * jt, kb, KC));
             }
-            lin_mul<MID - 1>(kf, qf, s);
+            int turn = kb;
+#pragma unroll
+            for (int sum = MID - 1; sum >= 0; --sum)
+#pragma unroll
+              for (int i = 0; i < IN; ++i)
+                if (sum - i >= 0 && sum - i < IN) {
+                  two[turn & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[sum - i], two[turn & 1], 0, 0, 0);
+                  ++turn;
+                }
           }
+          const v4f s = two[0] + two[1];
           const float between = apart < 2 ? 1.f : apart == 2 ? tile[1] : tile[TT - 2];
           float v[4];
 #pragma unroll
@@ -500,28 +533,32 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) y[tt][e] = v4f{0.f, 0.f, 0.f, 0.f};
+        // (fragments are read from LDS one ahead of their products, the state's parts made
+        // meanwhile)
+        v8bf qf[2][IN], sp[2][MID];
+        auto read_queries = [&](int f) {
 #pragma unroll
-        for (int kb = 0; kb < KT; ++kb) {
-          v8bf sp[2][MID];
+          for (int p = 0; p < IN; ++p) qf[f % 2][p] = lin_read(lq, p * KPART + plain(f % TT * 16, f / TT, KC));
+        };
+        read_queries(0);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v[8];
-            // (the parts of all states, made before the loop over the heads, would take
-            // more registers than there are)
-            asm volatile("" : "+v"(S[2 * kb][e]), "+v"(S[2 * kb + 1][e]));
+        for (int f = 0; f < KT * TT; ++f) {
+          const int kb = f / TT, tt = f % TT;
+          if (f + 1 < KT * TT) read_queries(f + 1);
+          if (tt == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = S[2 * kb][e][i], v[4 + i] = S[2 * kb + 1][e][i];
-            lin_split(v, sp[e]);
+            for (int e = 0; e < 2; ++e) {
+              float v[8];
+              // (the parts of all states, made before the loop over the heads, would take
+              // more registers than there are)
+              asm volatile("" : "+v"(S[2 * kb][e]), "+v"(S[2 * kb + 1][e]));
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v[i] = S[2 * kb][e][i], v[4 + i] = S[2 * kb + 1][e][i];
+              lin_split(v, sp[e]);
+            }
           }
-#pragma unroll
-          for (int tt = 0; tt < TT; ++tt) {
-            __builtin_amdgcn_sched_barrier(0);
-            v8bf qf[IN];
-#pragma unroll
-            for (int p = 0; p < IN; ++p) qf[p] = lin_read(lq, p * KPART + plain(16 * tt, kb, KC));
-#pragma unroll
-            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(sp[e], qf, y[tt][e]);
-          }
+          __builtin_amdgcn_sched_barrier(0);
+          lin_mul<MID - 1>(sp, qf[f % 2], y[tt]);
         }
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt) {
@@ -546,8 +583,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll
             for (int p = 0; p < MID; ++p)
               pf[p] = *reinterpret_cast<const v8bf*>(lp + (p * Lds::FRAGS + (tt < 2 ? tt : 2 * tt - 2 + b)) * 1024 + lane * 16);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) lin_mul<MID - 1>(x[e], pf, y[tt][e]);
+            lin_mul<MID - 1>(x, pf, y[tt]);
           }
         };
         if (!any) {
@@ -605,6 +641,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
           for (int e = 0; e < 2; ++e) lin_store<E>(r, to + 16 * tt * out_row, column + 16 * e, c.V, y[tt][e], w.quads);
       }
     }
+    if (OUT && k + 1 == k1 && !(last && dst >= 0)) break;  // nothing asks for the state after it
     // the state after the chunk
     const LinDecay d = pad == 0 ? whole : LinDecay(decay * (C - pad));
     if (d.keep != 0.f) {
@@ -620,33 +657,35 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
 #pragma unroll
         for (int e = 0; e < 2; ++e) S[a][e] *= d.by;
     }
+    v8bf kf[2][IN], xf[2][3];
+    auto read_keys = [&](int f) {
 #pragma unroll
-    for (int b = 0; b < PB; ++b) {
-      v8bf xf[2][3];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float x = (float)vf[b][e][IN - 1][j];
-#pragma unroll
-          for (int p = IN - 2; p >= 0; --p) x += (float)vf[b][e][p][j];
-          v[j] = x * back[j % 4] * tile[TT - 1 - 2 * b - j / 4];
-        }
-        lin_split(v, xf[e]);
+      for (int p = 0; p < IN; ++p) {
+        const int a = f % (2 * KT), at = p * KPART + turned(f / (2 * KT) * 32, a / 2, KC) + a % 2 * 8;
+        kf[f % 2][p] = lin_join(lin_read_turned(lk, at), lin_read_turned(lk, at + 16 * KC * 16));
       }
+    };
+    read_keys(0);
 #pragma unroll
-      for (int a = 0; a < 2 * KT; ++a) {
-        __builtin_amdgcn_sched_barrier(0);
-        v8bf kf[IN];
+    for (int f = 0; f < PB * 2 * KT; ++f) {
+      const int b = f / (2 * KT), a = f % (2 * KT);
+      if (f + 1 < PB * 2 * KT) read_keys(f + 1);
+      if (a == 0) {
 #pragma unroll
-        for (int p = 0; p < IN; ++p) {
-          const int at = p * KPART + turned(32 * b, a / 2, KC) + a % 2 * 8;
-          kf[p] = lin_join(lin_read_turned(lk, at), lin_read_turned(lk, at + 16 * KC * 16));
+        for (int e = 0; e < 2; ++e) {
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float x = (float)vf[b][e][IN - 1][j];
+#pragma unroll
+            for (int p = IN - 2; p >= 0; --p) x += (float)vf[b][e][p][j];
+            v[j] = x * back[j % 4] * tile[TT - 1 - 2 * b - j / 4];
+          }
+          lin_split(v, xf[e]);
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) lin_mul<2>(kf, xf[e], S[a][e]);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      lin_mul<2>(kf[f % 2], xf, S[a]);
     }
   }
   float* to = nullptr;
