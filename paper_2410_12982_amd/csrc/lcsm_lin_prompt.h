@@ -428,12 +428,16 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
     for (int i = (int)threadIdx.x; i < MID * Lds::FRAGS * 64; i += 64 * kLinWaves)
       reinterpret_cast<v4u*>(lp)[i] = v4u{0, 0, 0, 0};
   }
+  // a segment's own contribution is summed from its end, so that what was read last is
+  // what the outputs' kernel reads first, and as one product, not decayed by the chunk
+  constexpr int AHEAD = OUT ? 1 : -1;
+  const int first = OUT ? k0 : k1 - 1, end = OUT ? k1 : k0 - 1;
   if (DIRECT && k0 < k1) {
-    fetch_keys(k0);
-    fetch_values(k0);
-    if (OUT) fetch_queries(k0, 0);
+    fetch_keys(first);
+    fetch_values(first);
+    if (OUT) fetch_queries(first, 0);
   }
-  for (int k = k0; k < k1; ++k) {
+  for (int k = first; k != end; k += AHEAD) {
     const char* lk = lds + (DIRECT ? k % 2 * Lds::KEYS : 0);
     const char* values = lv + (DIRECT && !OUT ? k % 2 * Lds::VALUES : 0);
     if constexpr (!DIRECT) {
@@ -451,9 +455,9 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
     arrived();
     // DIRECT: the next chunk's keys (and values) go where those before these were,
     // which all waves have passed
-    if (DIRECT && k + 1 < k1) {
-      fetch_keys(k + 1);
-      if (!OUT) fetch_values(k + 1);
+    if (DIRECT && k + AHEAD != end) {
+      fetch_keys(k + AHEAD);
+      if (!OUT) fetch_values(k + AHEAD);
     }
     locate(k);
     // values as an operand: 32 positions a block, slots 4 q ..+3 and 16 + 4 q ..+3
@@ -642,20 +646,25 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
       }
     }
     if (OUT && k + 1 == k1 && !(last && dst >= 0)) break;  // nothing asks for the state after it
-    // the state after the chunk
-    const LinDecay d = pad == 0 ? whole : LinDecay(decay * (C - pad));
-    if (d.keep != 0.f) {
+    // the state after the chunk, or what the chunk adds to that after the segment
+    float later = 1.f;  // from the chunk's end to the segment's
+    if constexpr (OUT) {
+      const LinDecay d = pad == 0 ? whole : LinDecay(decay * (C - pad));
+      if (d.keep != 0.f) {
 #pragma unroll
-      for (int a = 0; a < 2 * KT; ++a)
+        for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+          for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], d.by, S[a][e][i]);
-    } else {
+            for (int i = 0; i < 4; ++i) S[a][e][i] = fmaf(S[a][e][i], d.by, S[a][e][i]);
+      } else {
 #pragma unroll
-      for (int a = 0; a < 2 * KT; ++a)
+        for (int a = 0; a < 2 * KT; ++a)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) S[a][e] *= d.by;
+          for (int e = 0; e < 2; ++e) S[a][e] *= d.by;
+      }
+    } else if (k + 1 < k1) {
+      later = (float)exp(decay * ((k1 - 1 - k) * C));
     }
     v8bf kf[2][IN], xf[2][3];
     auto read_keys = [&](int f) {
@@ -679,7 +688,8 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
             float x = (float)vf[b][e][IN - 1][j];
 #pragma unroll
             for (int p = IN - 2; p >= 0; --p) x += (float)vf[b][e][p][j];
-            v[j] = x * back[j % 4] * tile[TT - 1 - 2 * b - j / 4];
+            const float far_back = tile[TT - 1 - 2 * b - j / 4];
+            v[j] = OUT ? x * back[j % 4] * far_back : x * (back[j % 4] * (far_back * later));
           }
           lin_split(v, xf[e]);
         }
