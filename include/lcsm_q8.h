@@ -15,6 +15,7 @@
  * The sum is exact (32-bit integers), so that it does not depend on how it is
  * taken; y is rounded once to x's type.  A row of x with a value that is not
  * finite gives a row of y that is not finite; other rows are not touched by it.
+ * Scales of outputs stay below 2^96 in magnitude.
  *
  * Conventions as in lcsm.h: device pointers, asynchronous on the context's
  * stream, LCSM_* return codes, arguments validated before any device work is

@@ -19,7 +19,8 @@
  * and the values from `rotary` on as they are in v.  One pass: a head is read
  * once and written once.  Sums and values are fp32, an output is rounded once;
  * the angle is taken modulo a turn in fp64, so that far positions lose nothing.
- * Heads do not touch each other.
+ * Heads do not touch each other; where there is a norm, a head's sum of squares
+ * stays below 2^128.
  *
  * A context holds the weights of M layers and the frequencies f_j that they
  * share.  Conventions as in lcsm.h: device pointers, asynchronous on the

@@ -266,17 +266,17 @@ __global__ __launch_bounds__(512) void k_q8_row(const void* x, size_t x_stride, 
 __global__ __launch_bounds__(256) void k_q8_quantize(const float* __restrict__ w, int rows, int K,
                                                      char* __restrict__ codes, float* __restrict__ scales) {
   const int lane = (int)threadIdx.x & 63;
-  const long long row = (long long)blockIdx.x * 4 + threadIdx.x / 64;
-  if (row >= rows) return;
-  const float* p = w + (size_t)row * K;
-  unsigned most = 0;
   auto larger = [](unsigned a, unsigned b) { return b > a ? b : a; };
-  for (int k = lane; k < K; k += 64) most = larger(most, __builtin_bit_cast(unsigned, fabsf(p[k])));
+  for (long long row = (long long)blockIdx.x * 4 + threadIdx.x / 64; row < rows; row += (long long)gridDim.x * 4) {
+    const float* p = w + (size_t)row * K;
+    unsigned most = 0;
+    for (int k = lane; k < K; k += 64) most = larger(most, __builtin_bit_cast(unsigned, fabsf(p[k])));
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
-  const Codes code(__builtin_bit_cast(float, most));
-  if (lane == 0) scales[row] = code.s;
-  for (int k = lane; k < K; k += 64) codes[(size_t)row * K + k] = (char)code(p[k]);
+    for (int m = 1; m < 64; m *= 2) most = larger(most, __shfl_xor(most, m));
+    const Codes code(__builtin_bit_cast(float, most));
+    if (lane == 0) scales[row] = code.s;
+    for (int k = lane; k < K; k += 64) codes[(size_t)row * K + k] = (char)code(p[k]);
+  }
 }
 
 // Weights [M][N][K] as tiles [M][nts][kb][64][16], zeros past N and K.
@@ -822,7 +822,8 @@ int lcsm_q8_quantize(const float* w, int rows, int K, void* codes, float* scales
   if (rows < 0 || K < 1 || K > (1 << 24)) return LCSM_EINVAL;
   if (!rows) return LCSM_OK;
   if (!w || !codes || !scales) return LCSM_EINVAL;
-  hipLaunchKernelGGL(lcsm::k_q8_quantize, dim3((unsigned)(((long long)rows + 3) / 4)), dim3(256), 0, (hipStream_t)stream, w,
+  const long long blocks = ((long long)rows + 3) / 4;  // (a launch has less than 2^32 threads)
+  hipLaunchKernelGGL(lcsm::k_q8_quantize, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0, (hipStream_t)stream, w,
                      rows, K, (char*)codes, scales);
   return hipGetLastError() == hipSuccess ? LCSM_OK : LCSM_EDEVICE;
 }

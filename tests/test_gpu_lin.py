@@ -271,6 +271,43 @@ def test_wrong_offsets_and_slots_stay_in_bounds():
         assert not states[3].any() and not states[0].any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_segments_of_many_chunks(dtype):
+    """Many states, so that a long prompt is cut in two or three pieces of tens of chunks, under all kinds of decays: what a
+    piece adds to the state is summed over all of them at once."""
+    G = 200
+    lay = Layer(G, G, 8, 12, dtype=dtype, slots=2, max_tokens=3100, seed=12, decay=-np.exp2(-16 + 18 * np.arange(G) / G))
+    lay.set_states()
+    x = lay.inputs(3100)
+    say(f"[lin] long segments {dtype}")
+    lay.check(lay.ctx.prompt(0, *x), lay.want(x, [0, 3100]))
+
+
+def test_two_graphs_of_one_context():
+    """Two prompts' graphs share the context's workspace: replayed one after another, in either order, each is right."""
+    stream = torch.cuda.Stream(dev())
+    lay = Layer(4, 2, 64, 32, dtype="bf16", slots=2, seed=13, max_tokens=1500, stream=stream)
+    xs = [lay.inputs(T) for T in (1500, 900)]
+    src, nowhere = ints([-1]), ints([-1])
+    wants = [lay.want(x, [0, len(x[0])], src=[-1], dst=[-1]) for x in xs]
+    with torch.cuda.stream(stream):
+        ys = [torch.empty((len(x[0]), 4 * 32), dtype=torch.bfloat16, device=dev()) for x in xs]
+        torch.cuda.synchronize()
+        graphs = []
+        for x, y in zip(xs, ys):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                lay.ctx.prompt(0, *x, y=y, src=src, dst=nowhere)
+        for order in ((0, 1), (1, 0), (1, 1), (0, 1)):
+            for y in ys:
+                y.zero_()
+            for i in order:
+                graphs[i].replay()
+            torch.cuda.synchronize()
+            for i in set(order):
+                close(ys[i], *wants[i])
+
+
 @pytest.mark.parametrize("T", [60, 1500])
 def test_another_stream_and_a_graph(T):
     stream = torch.cuda.Stream(dev())

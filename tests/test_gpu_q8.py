@@ -204,6 +204,17 @@ def test_quantize():
     assert codes.shape == (0, 4) and scales.shape == (0,)
 
 
+def test_quantize_very_many_rows():
+    rows = (1 << 26) + 70  # more waves than a launch has
+    w = torch.ones((rows, 1), device=dev())
+    w[-3], w[5] = -2.0, 0.0
+    codes, scales = lcsm_mod().Q8.quantize(w)
+    want = torch.full_like(codes, 127)
+    want[-3], want[5] = -127, 0
+    assert torch.equal(codes, want)
+    assert torch.equal(scales, w.abs().squeeze(1) / 127)
+
+
 def test_refusals():
     lcsm = lcsm_mod()
     m = Matrix(20, 30, 8, seed=9)
