@@ -3,7 +3,15 @@
 // Codes of weights and of rows are kept as tiles of 16 rows x 64 inputs, 16
 // bytes a lane: lane l has inputs 16 (l / 16) ..+15 of row l % 16, which is its
 // share of either operand of a 16x16x64 integer product.  A call quantizes its
-// rows into such tiles first, a wave a row.
+// rows into such tiles first, in a launch of its own, or with few rows in the
+// product's.  A codes' sum is exact in 32 bits, so that it may be taken in any
+// order; what is rounded is its float, twice times a scale, the bias and the output.
+//
+// Few rows are bound by the weights' bytes and by launches, many by the matrix
+// units: 16384 rows of 2048 inputs to 8192 outputs, bf16, take 297 us, 25 us
+// of them for the rows' codes (241 us at the rate that a large library product of
+// 8-bit integers reaches, 509 us at that of 16-bit floats); a row of 2048 to 8192 outputs takes 4.7 us,
+// 3.7 us of it to read the weights at the rate of a large copy.
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -154,112 +162,73 @@ struct Raw {
   }
 };
 
-// Rows into tiles, 16 rows a workgroup; a wave takes every so many'th tile, of which
-// the first HELD stay in its registers while the rows' largest magnitudes are
-// found (the others are read again).
-template <class E>
+// Rows into tiles, WAVES waves a row, eight inputs a thread at a time, of which the
+// first HELD times stay in registers while the row's largest magnitude is found
+// (the others are read again).  Workgroup b runs on XCD b % 8: those of the rows of
+// a tile are on one, whose L2 puts their codes of 16 bytes together.
+template <class E, int WAVES>
 __global__ __launch_bounds__(256) void k_q8_rows(const void* x, size_t x_stride, int rows, int K, int kb,
                                                  char* __restrict__ codes, float* __restrict__ scales) {
-  constexpr int HELD = 8;
-  typedef Raw<E, 16> R;
-  __shared__ unsigned part[4][16];  // [waves][rows]
-  const int lane = (int)threadIdx.x & 63, nw = (int)blockDim.x >> 6;
-  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int q = lane >> 4, l = lane & 15;
-  const size_t row = (size_t)blockIdx.x * 16 + l;
-  // (rows past the last one are the last one again, and not stored)
-  const E* p = static_cast<const E*>(x) + (row < (size_t)rows ? row : (size_t)rows - 1) * x_stride;
-  auto load = [&](int t, R& to) {
-    const int k = t * kTileK + 16 * q;
-    to.load(p + min(k, K - 1), K - k);
-  };
-  R held[HELD];
-  unsigned most = 0;
-#pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (wv + i * nw < kb) load(wv + i * nw, held[i]);
-#pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (wv + i * nw < kb) most = held[i].larger(most);
-  for (int t = wv + HELD * nw; t < kb; t += nw) {
-    R v;
-    load(t, v);
-    most = v.larger(most);
-  }
-  most = R::both(most, __shfl_xor(most, 16));
-  most = R::both(most, __shfl_xor(most, 32));
-  if (q == 0) part[wv][l] = most;
-  __syncthreads();
-  for (int w = 0; w < nw; ++w) most = R::both(most, part[w][l]);
-  const Codes code(R::magnitude(most));
-  if (threadIdx.x < 16 && row < (size_t)rows) scales[row] = code.s;
-  v4i* to = reinterpret_cast<v4i*>(codes) + (size_t)blockIdx.x * kb * 64 + lane;
-  auto store = [&](int t, const R& raw) {
-    float v[16];
-    raw.values(v);
-    int w[4];
-    code.words(v, w);
-    to[(size_t)t * 64] = v4i{w[0], w[1], w[2], w[3]};
-  };
-#pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (wv + i * nw < kb) store(wv + i * nw, held[i]);
-  for (int t = wv + HELD * nw; t < kb; t += nw) {
-    R v;
-    load(t, v);
-    store(t, v);
-  }
-}
-
-// The same where there are few rows: a workgroup a row, four inputs a thread.
-template <class E>
-__global__ __launch_bounds__(512) void k_q8_row(const void* x, size_t x_stride, int K, int kb,
-                                                char* __restrict__ codes, float* __restrict__ scales) {
-  constexpr int HELD = 4, THREADS = 512;
-  typedef Raw<E, 4> R;
-  __shared__ unsigned part[THREADS / 64];
-  const size_t row = blockIdx.x;
+  constexpr int HELD = WAVES > 1 ? 4 : 2, STEP = 8 * 64 * WAVES;
+  constexpr int EACH = 4 / WAVES, GROUPS = 16 / EACH;  // rows a workgroup, workgroups a tile
+  typedef Raw<E, 8> R;
+  __shared__ unsigned part[4];
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, tile = id / (8 * GROUPS) * 8 + id % 8;
+  const size_t row = (size_t)tile * 16 + id / 8 % GROUPS * EACH + threadIdx.x / (64 * WAVES);
+  if (row >= (size_t)rows) return;  // (whole workgroups where there is a barrier)
   const E* p = static_cast<const E*>(x) + row * x_stride;
-  const int first = 4 * (int)threadIdx.x, end = kb * kTileK;
+  const int first = 8 * ((int)threadIdx.x % (64 * WAVES)), end = kb * kTileK;
   R held[HELD];
   unsigned most = 0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
-    const int k = first + i * 4 * THREADS;
+    const int k = first + i * STEP;
     if (k < end) held[i].load(p + min(k, K - 1), K - k);
   }
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
-    if (first + i * 4 * THREADS < end) most = held[i].larger(most);
-  for (int k = first + HELD * 4 * THREADS; k < end; k += 4 * THREADS) {
+    if (first + i * STEP < end) most = held[i].larger(most);
+  for (int k = first + HELD * STEP; k < end; k += STEP) {
     R v;
     v.load(p + min(k, K - 1), K - k);
     most = v.larger(most);
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) most = R::both(most, __shfl_xor(most, m));
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
-  __syncthreads();
+  if constexpr (WAVES > 1) {
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) most = R::both(most, part[w]);
+    for (int w = 0; w < WAVES; ++w) most = R::both(most, part[w]);
+  }
   const Codes code(R::magnitude(most));
-  if (threadIdx.x == 0) scales[row] = code.s;
+  if (first == 0) scales[row] = code.s;
   char* to = codes + row / 16 * kb * 1024 + row % 16 * 16;
   auto store = [&](int k, const R& raw) {
-    float v[4];
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    float v[8];
     raw.values(v);
-    int w[1];
+    int w[2];
     code.words(v, w);
-    *reinterpret_cast<int*>(to + (size_t)(k / kTileK) * 1024 + k % kTileK / 16 * 256 + k % 16) = w[0];
+    *reinterpret_cast<v2i*>(to + (size_t)(k / kTileK) * 1024 + k % kTileK / 16 * 256 + k % 16) = v2i{w[0], w[1]};
   };
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
-    if (first + i * 4 * THREADS < end) store(first + i * 4 * THREADS, held[i]);
-  for (int k = first + HELD * 4 * THREADS; k < end; k += 4 * THREADS) {
+    if (first + i * STEP < end) store(first + i * STEP, held[i]);
+  for (int k = first + HELD * STEP; k < end; k += STEP) {
     R v;
     v.load(p + min(k, K - 1), K - k);
     store(k, v);
   }
+}
+
+template <class E, int WAVES>
+hipError_t launch_rows(const Q8Call& c, hipStream_t st) {
+  const int each = 8 * 16 * WAVES / 4, tiles = ((c.rows + 15) / 16 + 7) / 8;  // workgroups for eight tiles
+  const int x = tiles < 4096 ? tiles : 4096;
+  hipLaunchKernelGGL((k_q8_rows<E, WAVES>), dim3((unsigned)(x * each), (unsigned)((tiles + x - 1) / x)), dim3(256), 0, st, c.x,
+                     c.x_stride, c.rows, c.K, c.kb, c.row_codes, c.row_scales);
+  return hipGetLastError();
 }
 
 // Weights: a wave a row, the codes one after another.
@@ -317,7 +286,7 @@ __device__ __forceinline__ void store_quad(__amdgpu_buffer_rsrc_t r, unsigned at
 // are few, that is less than a launch of its own.
 constexpr int kAhead = 4;   // tiles along K on their way
 constexpr int kPiece = 256;  // inputs of a row that a wave quantizes at once
-constexpr int kPieces = 4;   // and how many of them
+constexpr int kPieces = 2;   // and how many of them
 
 template <class E, int RT, int NT, bool OWN>
 __global__ __launch_bounds__(512) void k_q8_few(Q8Call c) {
@@ -646,20 +615,18 @@ hipError_t launch_many(const Q8Call& c, hipStream_t st) {
   return hipGetLastError();
 }
 
-constexpr int kRowsAlone = 2048;
-
 template <class E>
 hipError_t launch_q8(const Q8Call& c, hipStream_t st) {
   const int few = c.kb < 8 ? c.kb : 8;  // waves
+  // Rows quantized in the product's launch: us with and without, rows x inputs -> 2048 outputs:
+  //   1 x 2048  3.8  5.5   2 x 2048  4.7  5.7   3 x 2048  5.6  5.6   4 x 2048  6.4  5.6   4 x 512  3.8  5.2
+  //   1 x 4096  5.2  6.4   2 x 4096  6.6  6.4   1 x 8192  8.0  8.4 (to 8192 outputs, 4 x 2048: 8.7 and 6.1)
   if (c.rows <= 16 && (long long)c.rows * ((c.K + kPiece - 1) / kPiece) <= kPieces * few)
     return launch_few<E, 1, 1, true>(c, few, st);
-  if (c.rows < kRowsAlone)
-    hipLaunchKernelGGL((k_q8_row<E>), dim3((unsigned)c.rows), dim3(512), 0, st, c.x, c.x_stride, c.K, c.kb, c.row_codes,
-                       c.row_scales);
-  else
-    hipLaunchKernelGGL((k_q8_rows<E>), dim3((unsigned)((c.rows + 15) / 16)), dim3(64 * (c.kb < 4 ? c.kb : 4)), 0, st, c.x,
-                       c.x_stride, c.rows, c.K, c.kb, c.row_codes, c.row_scales);
-  const hipError_t e = hipGetLastError();
+  // Waves a row: us of 1 and 4, for rows of bf16 x inputs with a small product:
+  //   64 x 512    5.9   5.9    4096 x 512    9.4  11.5    16384 x 512   17.6  24.9    64 x 1000    6.9   6.0
+  //   4096 x 1000 12.5  14.2   512 x 2048    9.2   6.9    4096 x 2048   19.9  18.4    16384 x 4096 58.9  50.8
+  const hipError_t e = c.kb <= 16 ? launch_rows<E, 1>(c, st) : launch_rows<E, 4>(c, st);
   if (e != hipSuccess) return e;
   // Pieces of outputs and rows: the largest that still are workgroups enough, in tiles of 16.  us for
   // rows x inputs -> outputs, bf16, both launches, as few<RT, NT> 1,1 2,1 2,2, many 64 x 64, 128 x 64, 128 x 128, 256 x 256:

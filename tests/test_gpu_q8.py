@@ -189,6 +189,19 @@ def test_another_stream_and_a_graph(R):
             m.check(y, x, "bf16")
 
 
+@pytest.mark.parametrize("K", [9, 1100])
+def test_very_many_rows(K):
+    """Rows whose codes take more than one line of workgroups: the first, those around the line's end and the last."""
+    R, line = 600_000, 4096 * 128
+    m = Matrix(7, K, R, seed=K)
+    x = torch.randn((1000, K), generator=torch.Generator().manual_seed(3)).bfloat16().to(dev()).repeat(R // 1000, 1)
+    x *= torch.exp2((torch.arange(R, device=dev()) % 7).float())[:, None].bfloat16()
+    say(f"[q8] {R} x {K}")
+    y = m.ctx.matmul(0, x)
+    for a, b in ((0, 300), (line - 150, line + 150), (R - 300, R)):
+        m.check(y[a:b], x[a:b], "bf16")
+
+
 def test_quantize():
     lcsm = lcsm_mod()
     r = np.random.default_rng(8)
