@@ -17,11 +17,15 @@ constexpr int kLinMaxK = 256;
 constexpr int kLinMaxV = 4096;
 constexpr int kLinMaxSlots = 32768;
 
-// One token of each sequence.  A workgroup takes 4 VL values of a state, a thread
-// four of them and every 256 / VL'th key, J keys in all: the state is read once,
-// changed in registers, and written.  The sums over the keys of a head's outputs
-// are taken over the lanes of a wave that have the same values, then over the
-// waves in LDS.
+// One token of each sequence: S' = d S + k v^T and y = scale q S'.  A workgroup
+// takes 4 VL values of a state, a thread four of them and every 256 / VL'th key, J
+// keys in all: the state is read once, changed in registers, and written.  The
+// sums over the keys of a head's outputs are taken over the lanes of a wave that
+// have the same values, then over the waves in LDS.
+//
+// Bound by the states: 64 tokens of 32 states of 128 x 128 take 46 us, 5.9 TB/s of
+// reads and writes together, part of them in the memory's cache; one token of 16
+// states takes 4.4 us, a launch and a round trip.
 template <class E, int VL, int J>
 __global__ __launch_bounds__(256) void k_lin_step(LinCall c) {
   constexpr int KR = 256 / VL, VB = 4 * VL;
@@ -109,6 +113,10 @@ hipError_t launch_step_of(const LinCall& c, hipStream_t st) {
                      dim3(256), 0, st, c);
   return hipGetLastError();
 }
+// Workgroups of 128 values where these are enough for the card, else of 32.  us of
+// 128 and 32 by their number, states of 128 x 128, bf16:
+//     16  8.2  4.4   256   9.8   7.4    512  11.5  11.1
+//   1024 20.3 26.0  2048  46.9  51.7   8192 205   200
 template <class E>
 hipError_t launch_step(const LinCall& c, hipStream_t st) {
   if (c.V > 32 && (long long)c.n * c.G * ((c.V + 127) / 128) >= 1024)
@@ -118,8 +126,14 @@ hipError_t launch_step(const LinCall& c, hipStream_t st) {
 
 // How a prompt call is cut: segments of `per` chunks so that about as many
 // workgroups are on their way as there is room for at once (two or one a compute
-// unit); sequences that are that many by themselves are not cut.
-constexpr int kLinCutChunks = 4;  // calls of up to so many chunks are not cut
+// unit; half, one and a half and twice as many are slower at 16384 tokens);
+// sequences that are that many by themselves are not cut.
+//
+// Calls of up to so many chunks are not cut either, since cutting takes two more
+// launches.  us cut and uncut, 32 states of 128 x 128, bf16 (chunks of 64): 96 tokens
+// 25.2 and 18.6, 160 27.3 and 24.1, 256 29.5 and 28.4; fp32 (chunks of 32): 48 tokens
+// 25.0 and 17.2, 96 27.1 and 22.3, fp16 96 26.0 and 19.9.
+constexpr int kLinCutChunks = 4;
 int lin_want(int G, int K, int V) {
   const long long wgs = (long long)G * ((V + 32 * kLinWaves - 1) / (32 * kLinWaves));
   return (int)((K > 128 ? 256 : 512) / (wgs < 512 ? wgs : 512));
