@@ -196,9 +196,9 @@ __device__ __forceinline__ bool lin_piece(const LinCall& c, int want, int per, i
     if (want < base + total) {
       const unsigned long long past = __ballot(base + sum > want);
       const int who = __ffsll(past) - 1;
-      seq = __builtin_amdgcn_readfirstlane(i0 + who);
-      num = __builtin_amdgcn_readfirstlane(want - base - __shfl(sum - mine, who));
-      chunks = __builtin_amdgcn_readfirstlane(__shfl(ch, who));
+      seq = i0 + who;
+      num = want - base - __shfl(sum - mine, who);
+      chunks = __shfl(ch, who);
       return true;
     }
     base += total;  // (offsets that do not rise: at most 64 T / C and `want` at a time)
@@ -346,7 +346,14 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   const int segment = (int)blockIdx.y, heads = c.H / c.G;
   int seq, num, chunks;
   if (!lin_piece<C>(c, segment, w.per, seq, num, chunks)) return;
-  const bool last = (num + 1) * (long long)w.per >= chunks;
+  // (the same for all lanes, which the compiler does not see past that loop: all that
+  // follows from these would be vector work)
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  num = __builtin_amdgcn_readfirstlane(num);
+  chunks = __builtin_amdgcn_readfirstlane(chunks);
+  // (at most 2^26 / 32 chunks and as many again)
+  const int k0 = num * w.per;
+  const bool last = k0 + w.per >= chunks;
   if (!OUT && last) return;
   int t0, t1;
   lin_rows(c, seq, t0, t1);
@@ -354,7 +361,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
   t1 = __builtin_amdgcn_readfirstlane(t1);
   const int src = __builtin_amdgcn_readfirstlane(lin_slot(c.src, seq, c.slots));
   const int dst = __builtin_amdgcn_readfirstlane(lin_slot(c.dst, seq, c.slots));
-  const int k0 = num * w.per, k1 = last ? chunks : k0 + w.per;
+  const int k1 = min(k0 + w.per, chunks);
   const double decay = (double)c.decay[g];
   float g2 = (float)(decay * 1.4426950408889634);
   if (g2 < -1e30f) g2 = -1e30f;  // (d = 0: finite, so that d^0 is 1; NaN stays)
