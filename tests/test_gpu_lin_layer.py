@@ -177,3 +177,15 @@ def test_stack(layers, dim, batch, T, conv_every, lin_every, dtype):
     whole = torch.cat(whole, 1).double()
     assert torch.isfinite(single).all()
     assert ((whole - single).norm() / single.norm()).item() < 0.05
+
+
+def test_no_rows():
+    """Calls without rows give outputs without rows and leave the states as they are; a sequence of none moves its state."""
+    s = Served(64, 4, 2, 16, 24, "bf16", 3, 32, seed=3)
+    s.lin.state(0).copy_(torch.randn(s.lin.state(0).shape, device=dev()))
+    state = s.lin.state(0).clone()
+    x, none = torch.empty((0, 64), dtype=torch.bfloat16, device=dev()), torch.empty(0, dtype=torch.int32, device=dev())
+    assert s(x, none, s.lin.step).shape == (0, 64)
+    assert s(x, none, lambda m, q, k, v: s.lin.prompt(m, q, k, v, src=torch.tensor([2], dtype=torch.int32, device=dev()),
+                                                      dst=torch.tensor([0], dtype=torch.int32, device=dev()))).shape == (0, 64)
+    assert torch.equal(s.lin.state(0)[1:], state[1:]) and torch.equal(s.lin.state(0)[0], state[2])
