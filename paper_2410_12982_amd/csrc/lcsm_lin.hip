@@ -152,7 +152,7 @@ hipError_t launch_prompt(const LinCall& c, int dtype, float* states, hipStream_t
     return (uintptr_t)p % (n * e) == 0 && stride % n == 0 && width % n == 0;
   };
   w.direct = e == 2 && aligned(c.q, c.q_stride, c.K, 8) && aligned(c.k, c.k_stride, c.K, 8) && aligned(c.v, c.v_stride, c.V, 8);
-  w.quads = aligned(c.y, c.y_stride, c.V, 4);
+  w.wide = e == 2 && aligned(c.y, c.y_stride, c.V, 8) ? 8 : aligned(c.y, c.y_stride, c.V, 4) ? 4 : 1;
   return dtype == LCSM_F32 ? lin_prompt_f32(c, w, st) : dtype == LCSM_BF16 ? lin_prompt_bf16(c, w, st) : lin_prompt_f16(c, w, st);
 }
 

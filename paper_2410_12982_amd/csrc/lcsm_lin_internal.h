@@ -24,7 +24,7 @@ struct LinCut {
   float* states;  // [segments][G][K][V]: what a segment adds to the state after it, then the state before it
   int per, segments;  // segments: an upper bound
   int direct;         // rows are whole and aligned eights: they can go from memory straight into LDS
-  int quads;          // four outputs are whole and aligned as one
+  int wide;           // so many outputs are whole and aligned as one: 8 (of 16 bits), 4 or 1
 };
 
 __device__ __forceinline__ int lin_slot(const int* list, int i, int slots) {

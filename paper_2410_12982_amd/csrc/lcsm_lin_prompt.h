@@ -288,31 +288,46 @@ __device__ __forceinline__ void lin_fetch(char* lds, const LinLane<CHUNKS>& lane
     fetch_to_lds(r, lane.have ? lane.at + (unsigned)(i * STEP - pad) * each : kLinNowhere, 0, lds + (i * THREADS + 64 * wv) * 16);
 }
 
-// Four outputs from column `at` of `width` on, of the row that begins at `row` of
-// a buffer.  quads: four are whole and aligned as one.
+// Outputs of a row that begins at `row` of a buffer: `width` values, of which a lane
+// has four from column `at` on and four 16 behind those.  wide: so many are whole and
+// aligned as one (8 of 16 bits, 4 or 1).
 template <class E>
-__device__ __forceinline__ void lin_store(__amdgpu_buffer_rsrc_t r, unsigned row, int at, int width, v4f v, bool quads) {
+__device__ __forceinline__ void lin_store(__amdgpu_buffer_rsrc_t r, unsigned row, int at, int width, const v4f (&v)[2], int wide) {
+  typedef E v4e __attribute__((ext_vector_type(4)));
+  const v4e out[2] = {__builtin_convertvector(v[0], v4e), __builtin_convertvector(v[1], v4e)};
   typedef unsigned v2u __attribute__((ext_vector_type(2)));
-  struct {
-    E e[4];
-  } out;
+  if (wide == 8) {
+    if constexpr (sizeof(E) == 2) {
+      // lanes 16 apart exchange halves, so that each has eight values: 64 bytes of a row
+      // a store in place of 32
+      const v2u a = __builtin_bit_cast(v2u, out[0]), b = __builtin_bit_cast(v2u, out[1]);
+      const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+      const int odd = (int)threadIdx.x >> 4 & 1, first = at + 12 * odd;
+      __builtin_amdgcn_raw_buffer_store_b128(v4u{lo[0], hi[0], lo[1], hi[1]}, r,
+                                             (int)(first < width ? row + (unsigned)first * 2u : kLinNowhere), 0, 0);
+    }
+  } else if (wide == 4) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) out.e[i] = (E)v[i];
-  if (quads) {
-    const unsigned to = at < width ? row + (unsigned)at * (unsigned)sizeof(E) : kLinNowhere;
-    if constexpr (sizeof(E) == 4)
-      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, out), r, (int)to, 0, 0);
-    else
-      __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), r, (int)to, 0, 0);
+    for (int e = 0; e < 2; ++e) {
+      const unsigned to = at + 16 * e < width ? row + (unsigned)(at + 16 * e) * (unsigned)sizeof(E) : kLinNowhere;
+      if constexpr (sizeof(E) == 4)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, out[e]), r, (int)to, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out[e]), r, (int)to, 0, 0);
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned to = at + i < width ? row + (unsigned)(at + i) * (unsigned)sizeof(E) : kLinNowhere;
-      if constexpr (sizeof(E) == 4)
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, out.e[i]), r, (int)to, 0, 0);
-      else
-        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, out.e[i]), r, (int)to, 0, 0);
-    }
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = at + 16 * e + i;
+        const unsigned to = n < width ? row + (unsigned)n * (unsigned)sizeof(E) : kLinNowhere;
+        if constexpr (sizeof(E) == 4)
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)out[e][i]), r, (int)to, 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (E)out[e][i]), r, (int)to, 0, 0);
+      }
   }
 }
 
@@ -657,9 +672,7 @@ __global__ __launch_bounds__(64 * kLinWaves, KT > 4 ? 1 : 2) void k_lin_chunks(L
         const unsigned to = lin_here((unsigned)(l - pad) * out_row);
         const int column = (int)lin_here((unsigned)(vc + 4 * q));
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) lin_store<E>(r, to + 16 * tt * out_row, column + 16 * e, c.V, y[tt][e], w.quads);
+        for (int tt = 0; tt < TT; ++tt) lin_store<E>(r, to + 16 * tt * out_row, column, c.V, y[tt], w.wide);
       }
     }
     if (OUT && k + 1 == k1 && !(last && dst >= 0)) break;  // nothing asks for the state after it

@@ -8,7 +8,7 @@
 // order; what is rounded is its float, twice times a scale, the bias and the output.
 //
 // Few rows are bound by the weights' bytes and by launches, many by the matrix
-// units: 16384 rows of 2048 inputs to 8192 outputs, bf16, take 293 us, some 28 of
+// units: 16384 rows of 2048 inputs to 8192 outputs, bf16, take 278 us, some 28 of
 // them for the rows' codes (241 us at the rate that a large library product of 8-bit
 // integers reaches, 509 us at that of 16-bit floats); a row of 2048 to 8192 outputs
 // takes 4.7 us, 3.7 us of it to read the weights at the rate of a large copy.
@@ -40,7 +40,7 @@ struct Q8Call {
   const float *scales, *bias;  // bias NULL: none
   char* row_codes;
   float* row_scales;
-  int quads;  // four outputs are aligned as one, rows of them reach less than 2^32 bytes
+  int wide;  // 16 bytes of outputs are aligned as one, 16 rows of them reach less than 2^32 bytes
 };
 
 // ---- quantizing
@@ -269,17 +269,6 @@ __global__ __launch_bounds__(256) void k_q8_codes(const int8_t* __restrict__ src
 
 // ---- products
 
-// Four outputs as one.
-template <class T>
-__device__ __forceinline__ void store_quad(__amdgpu_buffer_rsrc_t r, unsigned at, const T& out) {
-  typedef unsigned v2u __attribute__((ext_vector_type(2)));
-  typedef unsigned v4u __attribute__((ext_vector_type(4)));
-  if constexpr (sizeof(T) == 16)
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, out), r, (int)at, 0, 0);
-  else
-    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, out), r, (int)at, 0, 0);
-}
-
 // A workgroup takes NT tiles of 16 outputs and RT of 16 rows; its waves take
 // every so many'th tile along K, and their sums meet in LDS.  OWN: the workgroup
 // quantizes the rows itself, into LDS, under the weights' loads: as long as they
@@ -410,10 +399,12 @@ hipError_t launch_few(const Q8Call& c, int waves, hipStream_t st) {
 // outputs are made and stored.
 //
 // In pieces of 256 x 256 with four stages, 8192 rows of 8192 inputs to 8192 outputs
-// take 399 us, 2.8 POP/s, where a library product reaches 2.3; with 2048 inputs the
-// outputs' conversion and stores after every 32 stages cost a fifth, and the matrix
-// units are busy 45 % of the time.  Two workgroups of 256 x 128 a compute unit, five
-// stages, and stores past the caches were slower.
+// take 485 to 510 us with the rows' codes (a library product of 8-bit integers alone
+// 460 to 490), and 16384 rows of 2048 inputs 278 (293).  There the outputs' conversion
+// and stores after every 32 stages cost a fifth: stores of 32 bytes of a row took 5 %
+// of the whole time more than those of 64, those of 128, for which rows have to change
+// lanes too, the same as 64.  Two workgroups of 256 x 128 a compute unit, five stages,
+// and stores past the caches were slower.
 template <class E, int WN, int WX, int NT, int RT, int KT, int STAGES>
 __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
   constexpr int WAVES = WN * WX, TN = WN * NT, TX = WX * RT, EACH = (TN + TX) / WAVES;  // rows of tiles that a wave fetches
@@ -556,20 +547,39 @@ __global__ __launch_bounds__(64 * WN * WX, 2) void k_q8_many(Q8Call c) {
     struct Out {
       E e[4];
     };
+    struct Two {
+      unsigned w[2];
+    };
     auto make = [&](int t, int r) {
       Out out;
 #pragma unroll
       for (int i = 0; i < 4; ++i) out.e[i] = (E)((float)acc[t][r][i] * scale[t][i] * by[r]);
       return out;
     };
-    if (whole && !c.bias && c.quads && (px * TX + wx * RT + RT) * 16 <= c.rows) {
+    if (whole && !c.bias && c.wide && (px * TX + wx * RT + RT) * 16 <= c.rows) {
       const unsigned each = (unsigned)c.y_stride * (unsigned)sizeof(E);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const auto y = uniform_buffer(static_cast<E*>(c.y) + (size_t)(px * TX + wx * RT + r) * 16 * c.y_stride +
                                           (pn * TN + wn * NT) * 16, 15 * each + NT * 16 * (unsigned)sizeof(E));
 #pragma unroll
-        for (int t = 0; t < NT; ++t) store_quad(y, l * each + (16 * t + 4 * q) * (unsigned)sizeof(E), make(t, r));
+        for (int t = 0; t < NT; t += 2) {
+          typedef unsigned v4u __attribute__((ext_vector_type(4)));
+          if constexpr (sizeof(E) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, make(t + i, r)), y, (int)(l * each + 64 * (t + i) + 16 * q),
+                                                     0, 0);
+          } else {
+            // lanes 16 apart exchange halves of two tiles, so that each has eight outputs of
+            // one: 64 bytes of a row a store in place of 32
+            const Two a = __builtin_bit_cast(Two, make(t, r)), b = __builtin_bit_cast(Two, make(t + 1, r));
+            const auto lo = __builtin_amdgcn_permlane16_swap(a.w[0], b.w[0], false, false);
+            const auto hi = __builtin_amdgcn_permlane16_swap(a.w[1], b.w[1], false, false);
+            __builtin_amdgcn_raw_buffer_store_b128(v4u{lo[0], hi[0], lo[1], hi[1]}, y,
+                                                   (int)(l * each + 32 * (t + (q & 1)) + 16 * (q >> 1)), 0, 0);
+          }
+        }
       }
     } else {
       E* y = static_cast<E*>(c.y) + (size_t)row0 * c.y_stride + n0;
@@ -785,7 +795,7 @@ int lcsm_q8_matmul(lcsm_q8* ctx, int layer, int rows, int dtype, const void* x, 
   const lcsm::Q8Call c{rows, s.N, s.K, ctx->kb, x, y, x_stride, y_stride, ctx->codes + m * ctx->nts * ctx->kb * 1024,
                        ctx->scales + m * s.N, ctx->bias ? ctx->bias + m * s.N : nullptr, ctx->row_codes,
                        ctx->row_scales,
-                       (uintptr_t)y % (4 * lcsm::dtype_size(dtype)) == 0 && y_stride % 4 == 0 && y_stride <= lcsm::kMaxStride};
+                       (uintptr_t)y % 16 == 0 && y_stride * lcsm::dtype_size(dtype) % 16 == 0 && y_stride <= lcsm::kMaxStride};
   const hipError_t e = lcsm::with_dtype(dtype, [&](auto v) { return lcsm::launch_q8<decltype(v)>(c, ctx->stream); });
   return e == hipSuccess ? LCSM_OK : q8_fail(ctx, LCSM_EDEVICE, "product launch", e);
 }
