@@ -35,8 +35,8 @@
 // Long calls are cut into segments of chunks: what each adds to the state after it,
 // the states between them, then the outputs, three launches.  Bound by memory and
 // by instructions, which do not quite hide under each other: 16384 rows of 32 states of
-// 128 x 128, bf16, take 242 us, outputs 176 us (3.0 TB/s; the vector units are busy 40 %
-// of it and the matrix units 26 %), contributions 74 us (3.6 TB/s), the join 14 us.
+// 128 x 128, bf16, take 231 to 242 us, outputs 175 us (3.0 TB/s; the vector units are
+// busy 40 % of it and the matrix units 26 %), contributions 74 us (3.6 TB/s), the join 14.
 // Two workgroups a compute unit fill its registers, so that a chunk's loads are
 // started a chunk ahead, into the LDS of the keys before them, or of queries and values
 // once these have been read.  Four stages of 32 rows in place of two of 64 for the
