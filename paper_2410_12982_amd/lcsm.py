@@ -318,6 +318,9 @@ if _current_raw is None:
     def _current_raw(index):
         return torch.cuda.current_stream(index).cuda_stream
 
+# (without the check that the runtime is up, which a context has behind it)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
 _F32 = torch.float32
 
 
@@ -874,7 +877,7 @@ class _LayerContext:
     _kind = ""
 
     def _open(self, device, stream):
-        self.device = device
+        self.device, self._index = device, device.index
         self.stream = stream if stream is not None else torch.cuda.current_stream(device)
         self._order = _Order(self.stream, device)
         self._ctx = _vp()
@@ -899,9 +902,7 @@ class _LayerContext:
         _handed_over(self.stream, device, params)
 
     def _on_device(self, call, *args):
-        """A call of the library, which queues work and allocates on the current device, on the context's."""
-        if torch.cuda.current_device() == self.device.index:
-            return call(*args)
+        """A call that queues work, and allocates, on the current device: on the context's."""
         with torch.cuda.device(self.device):
             return call(*args)
 
@@ -915,7 +916,9 @@ class _LayerContext:
 
     def _rows(self, tensor, rows, width, dtype, name):
         """(address, stride between rows) of a tensor [rows, width] whose rows are contiguous."""
-        if tensor.dtype is dtype and tensor.shape == (rows, width) and tensor.device == self.device:
+        if tensor.dtype is dtype and tensor.shape == (rows, width) and tensor.get_device() == self._index:
+            if tensor.is_contiguous():
+                return tensor.data_ptr(), width
             a, b = tensor.stride()
             if b == 1 or width == 1 or rows == 0:
                 return tensor.data_ptr(), a if rows > 1 else width
@@ -995,7 +998,7 @@ class Ssm(_LayerContext):
     def _slots(self, t, n, name):
         if t is None:
             return None
-        if t.dtype is torch.int32 and t.shape == (n,) and t.device == self.device and t.is_contiguous():
+        if t.dtype is torch.int32 and t.shape == (n,) and t.get_device() == self._index and t.is_contiguous():
             return t.data_ptr()
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
 
@@ -1187,6 +1190,8 @@ class Q8(_LayerContext):
 
     def matmul(self, layer, x, y=None):
         """y [rows, N] = x [rows, K] times the layer's matrix, in x's type."""
+        if _current_device() != self._index:
+            return self._on_device(self.matmul, layer, x, y)
         rows, dtype = x.shape[0], x.dtype
         px, sx = self._rows(x, rows, self.K, dtype, "x")
         if y is None:
@@ -1196,8 +1201,7 @@ class Q8(_LayerContext):
             py, sy = self._rows(y, rows, self.N, dtype, "y")
         if self._order():
             _used_on(self.stream, (x, y))
-        r = self._on_device(_lib.lcsm_q8_matmul, self._ctx, self._layer(layer), _int(rows, "rows"), _dtype_code(dtype), px, sx,
-                            py, sy)
+        r = _lib.lcsm_q8_matmul(self._ctx, self._layer(layer), _int(rows, "rows"), _dtype_code(dtype), px, sx, py, sy)
         if r:
             self._check(r, "lcsm_q8_matmul")
         return y
@@ -1255,7 +1259,7 @@ class Lin(_LayerContext):
     def _list(self, t, n, name):
         if t is None:
             return None
-        if t.dtype is torch.int32 and t.shape == (n,) and t.device == self.device and t.is_contiguous():
+        if t.dtype is torch.int32 and t.shape == (n,) and t.get_device() == self._index and t.is_contiguous():
             return t.data_ptr()
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on {self.device}")
 
@@ -1279,9 +1283,11 @@ class Lin(_LayerContext):
         """One token of each of n sequences: q [n, heads keys], k [n, G keys], v [n, G values], y [n, heads values].
         ``src``, ``dst``: int32 [n], the slots that states are read from (-1: zero) and written to (-1: not kept); None:
         slot i for sequence i."""
+        if _current_device() != self._index:
+            return self._on_device(self.step, layer, q, k, v, y, src, dst)
         n = q.shape[0]
         y = self._fill(n, n, q, k, v, y, src, dst)
-        r = self._on_device(_lib.lcsm_lin_step_layer, self._ctx, self._layer(layer), _int(n, "rows"), self._io_ref)
+        r = _lib.lcsm_lin_step_layer(self._ctx, self._layer(layer), _int(n, "rows"), self._io_ref)
         if r:
             self._check(r, "lcsm_lin_step_layer")
         return y
@@ -1289,13 +1295,14 @@ class Lin(_LayerContext):
     def prompt(self, layer, q, k, v, y=None, offsets=None, src=None, dst=None):
         """The tokens of n sequences one after another, q [T, heads keys] and so on: sequence i is rows offsets[i] ..
         offsets[i+1] (int32 [n + 1]; None: one sequence of all rows)."""
+        if _current_device() != self._index:
+            return self._on_device(self.prompt, layer, q, k, v, y, offsets, src, dst)
         T, n, at = q.shape[0], 1, None
         if offsets is not None:
             n = offsets.shape[0] - 1
             at = self._list(offsets, n + 1, "offsets")
         y = self._fill(T, n, q, k, v, y, src, dst, offsets)
-        r = self._on_device(_lib.lcsm_lin_prompt_layer, self._ctx, self._layer(layer), _int(T, "rows"), _int(n, "sequences"), at,
-                            self._io_ref)
+        r = _lib.lcsm_lin_prompt_layer(self._ctx, self._layer(layer), _int(T, "rows"), _int(n, "sequences"), at, self._io_ref)
         if r:
             self._check(r, "lcsm_lin_prompt_layer")
         return y
@@ -1338,6 +1345,8 @@ class Rot(_LayerContext):
         """(q, k) normed and turned: q [rows, q_heads P] and k [rows, k_heads P] (None without heads of keys), positions
         int32 [rows] (None where nothing is turned).  ``q_out`` and ``k_out`` receive them where given (q and k themselves
         may)."""
+        if _current_device() != self._index:
+            return self._on_device(self.apply, layer, q, k, positions, q_out, k_out)
         rows, P, io = q.shape[0], self.P, self._io
         qw, kw = self.q_heads * P, self.k_heads * P
         io.q, io.q_stride = self._rows(q, rows, qw, self.dtype, "q")
@@ -1359,14 +1368,14 @@ class Rot(_LayerContext):
                 io.k_out, io.k_out_stride = self._rows(k_out, rows, kw, self.dtype, "k_out")
         if positions is None:
             io.positions = None
-        elif (positions.dtype is torch.int32 and positions.shape == (rows,) and positions.device == self.device
+        elif (positions.dtype is torch.int32 and positions.shape == (rows,) and positions.get_device() == self._index
               and positions.is_contiguous()):
             io.positions = positions.data_ptr()
         else:
             raise ValueError(f"positions must be a contiguous int32 tensor of shape {(rows,)} on {self.device}")
         if self._order():
             _used_on(self.stream, (q, k, q_out, k_out, positions))
-        r = self._on_device(_lib.lcsm_rot_apply, self._ctx, self._layer(layer), rows, self._io_ref)
+        r = _lib.lcsm_rot_apply(self._ctx, self._layer(layer), rows, self._io_ref)
         if r:
             self._check(r, "lcsm_rot_apply")
         return q_out, k_out
