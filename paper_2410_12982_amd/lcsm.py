@@ -1375,7 +1375,7 @@ class Rot(_LayerContext):
             raise ValueError(f"positions must be a contiguous int32 tensor of shape {(rows,)} on {self.device}")
         if self._order():
             _used_on(self.stream, (q, k, q_out, k_out, positions))
-        r = _lib.lcsm_rot_apply(self._ctx, self._layer(layer), rows, self._io_ref)
+        r = _lib.lcsm_rot_apply(self._ctx, self._layer(layer), _int(rows, "rows"), self._io_ref)
         if r:
             self._check(r, "lcsm_rot_apply")
         return q_out, k_out
