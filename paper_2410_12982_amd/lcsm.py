@@ -927,7 +927,7 @@ class _LayerContext:
 
     def reset(self):
         self._order()
-        self._check(self._reset(self._ctx), f"lcsm_{self._kind}_reset")
+        self._check(self._on_device(self._reset, self._ctx), f"lcsm_{self._kind}_reset")
 
     def close(self):
         if getattr(self, "_ctx", None):

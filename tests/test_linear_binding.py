@@ -29,3 +29,25 @@ def test_rotations_of_more_rows_than_an_int(rows, monkeypatch):
     ctx = bare(lcsm.Rot, monkeypatch, P=1, q_heads=1, k_heads=0, dtype=torch.bfloat16, _io=io, _io_ref=lcsm.ctypes.byref(io))
     with pytest.raises(ValueError, match="rows"):
         ctx.apply(0, one_value(rows), None, None, q_out=one_value(rows))
+
+
+@pytest.mark.parametrize("cls", [lcsm.Lin, lcsm.Rot, lcsm.Q8, lcsm.Ssm, lcsm.Norm, lcsm.Q4])
+def test_resets_on_their_own_device(cls, monkeypatch):
+    """A reset queues work on the context's stream: with another device current it goes to the context's."""
+    current = ["another"]
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            current.append(self.device)
+
+        def __exit__(self, *exc):
+            current.pop()
+
+    monkeypatch.setattr(lcsm.torch.cuda, "device", Device)
+    at = []
+    ctx = bare(cls, monkeypatch, _reset=lambda handle: at.append(current[-1]) or 0)
+    ctx.reset()
+    assert at == [ctx.device] and current == ["another"]
