@@ -15,8 +15,16 @@
  * A context holds, for each of M layers, `slots` sequences' states in fp32.
  * Calls name the slot that each sequence is read from and the one it is
  * written to, so that a sequence is continued in place, begun, or continued in
- * a copy.  Sums, decays and states are fp32 whatever the type of queries, keys
- * and values; outputs are rounded to it once.
+ * a copy.  Sums, decays and states are held in fp32 whatever the type of
+ * queries, keys and values; outputs are rounded to it once.  Prompts make their
+ * products on the matrix units, of parts of 16 bits: those that states are
+ * made of, and all of fp32, to some 2^-24 of the factors.  Where outputs have
+ * 16 bits, the scores q k and the states that queries are multiplied with
+ * enter their products rounded to 2^-16, and of two fp16 values' product (and
+ * of their products with scores and states) that of the lower parts, up to
+ * 2^-16, is left out: shares of the magnitudes that are summed, which stay
+ * below the outputs' rounding unless the sum is far smaller than those.  Single
+ * tokens are fp32 throughout.
  *
  * A value that is not finite makes only those outputs and states not finite
  * that depend on it: no earlier token, no other sequence, no other head.
