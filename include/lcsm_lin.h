@@ -69,9 +69,11 @@ int lcsm_lin_workspace_bytes(const lcsm_lin_shape* shape, size_t* bytes);
 
 /* Create a context with all states zero.  decay: device fp32 [M][G], the
  * natural logarithms g of the states' decays (at most 0 for a decay; minus
- * infinity: a state holds its last token only), copied during the call's
- * stream work; the caller may free them once the stream has passed
- * lcsm_lin_init.  stream: hipStream_t (NULL = the null stream).  workspace: at
+ * infinity: a state holds its last token only).  With g above 0 a state grows:
+ * prompts are right while e^(g n) is below 2^127, n the tokens of the call's
+ * longest sequence rounded up to 64; beyond, outputs and states may be not
+ * finite where the formula's are.  They are copied during the call's stream
+ * work; the caller may free them once the stream has passed lcsm_lin_init.  stream: hipStream_t (NULL = the null stream).  workspace: at
  * least lcsm_lin_workspace_bytes bytes, 256-byte aligned, owned by the caller
  * until lcsm_lin_destroy; NULL makes the library allocate it.
  * Errors: LCSM_EINVAL, LCSM_ENOMEM, LCSM_EDEVICE; *out is NULL on failure. */
