@@ -127,7 +127,10 @@ hipError_t launch_step(const LinCall& c, hipStream_t st) {
 // How a prompt call is cut: segments of `per` chunks so that about as many
 // workgroups are on their way as there is room for at once (two or one a compute
 // unit; half, one and a half and twice as many are slower at 16384 tokens);
-// sequences that are that many by themselves are not cut.
+// sequences that are that many by themselves are not cut, however unequal they are: 32
+// states of 128 x 128, bf16, one of 16384 tokens beside fourteen of 33 253 to 259 us,
+// beside fifteen, which is the limit there, 1515 (sixteen of 1024, uncut, 166 to 184,
+// fifteen, cut, 174 to 182).
 //
 // Calls of up to so many chunks are not cut either, since cutting takes two more
 // launches.  us cut and uncut, 32 states of 128 x 128, bf16 (chunks of 64): 96 tokens

@@ -37,15 +37,17 @@
 // 2.4e-6 of its norm for bf16 and 3.7e-6 for fp16, where fp32 is by 2e-7; outputs of
 // 16 bits are rounded by up to 2^-8 and 2^-11, a hundred times as much.
 //
-// Long calls are cut into segments of chunks: what each adds to the state after it,
-// the states between them, then the outputs, three launches.  Bound by memory and
-// by instructions, which do not quite hide under each other: 16384 rows of 32 states of
+// Long calls are cut into segments of chunks: what each adds to the state after it, the
+// states between them, then the outputs, three launches.  Bound by memory and by
+// instructions, which do not quite hide under each other: 16384 rows of 32 states of
 // 128 x 128, bf16, take 231 to 242 us, outputs 175 us (3.0 TB/s; the vector units are
-// busy 40 % of it and the matrix units 26 %), contributions 74 us (3.6 TB/s), the join 14.
-// Two workgroups a compute unit fill its registers, so that a chunk's loads are
-// started a chunk ahead, into the LDS of the keys before them, or of queries and values
-// once these have been read.  Four stages of 32 rows in place of two of 64 for the
-// contributions: 79 us against 74.
+// busy 40 % of it and the matrix units 26 %), contributions 74 us (3.6 TB/s), the join
+// 14.  Two workgroups a compute unit fill its registers (of 128 keys, bf16 and fp32,
+// outputs spill 16 to 24 a lane), so that a chunk's loads are started a chunk ahead,
+// into the LDS of the keys before them, or of queries and values once these have been
+// read.  Four stages of 32 rows in place of two of 64 for the contributions: 79 us
+// against 74.  More than 128 keys take 432 to 472 registers and spill 20: one workgroup
+// a unit, and 256 x 128 in bf16 518 to 550 us, fp16 1130, fp32 1040.
 //
 // A product with a value v_j that is not finite reaches positions before j as 0 *
 // inf; where there is one, the products of the scores are made without it, and
@@ -80,7 +82,7 @@ struct LinParts<float> {
 // Positions of a chunk: 64 where keys and values are one bf16 part and the chunk's
 // rows leave room for two workgroups a compute unit, else 32 (fp16, 32 heads of 128
 // x 128 and 16384 tokens: 449 us in chunks of 32, 705 us in those of 64; of 64 x 128,
-// 311 and 317 us).
+// 311 and 317 us; later steps brought the first to 427).
 template <class E>
 constexpr int lin_chunk(int KT) {
   return LinParts<E>::IN == 1 && KT <= 4 ? 64 : 32;
